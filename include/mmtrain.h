@@ -392,4 +392,6 @@ MMTRAIN_API int mmtrain_adam_step(const mmtrain_adam_desc *desc, int64_t n, floa
 #ifdef __cplusplus
 }
 #endif
+/* rotary positions, norms with gate and residual scale, gradient norm and clipping */
+#include "mmtrain_ops.h"
 #endif /* MMTRAIN_H */

@@ -32,6 +32,15 @@ EXPORTS = ("mmtrain_layer_ctx_bytes", "mmtrain_layer_workspace_bytes", "mmtrain_
            "mmtrain_stack_ctx_bytes", "mmtrain_stack_workspace_bytes", "mmtrain_stack_fwd", "mmtrain_stack_bwd",
            "mmtrain_pipeline_1f1b", "mmtrain_inter_reorder", "mmtrain_profile_attn_busy",
            "mmtrain_profile_gemm_clock", "mmtrain_attn_bwd_noalloc")
+# declared in include/mmtrain_ops.h
+OPS_EXPORTS = ("mmtrain_rope", "mmtrain_residual_norm_workspace_bytes", "mmtrain_residual_norm_fwd", "mmtrain_residual_norm_bwd",
+               "mmtrain_grad_norm_workspace_bytes", "mmtrain_grad_norm", "mmtrain_grad_clip", "mmtrain_adam_step_clipped")
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_WAVELENGTH, ROPE_RAMP = range(4)
+ROPE_GRADIENT = 1
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+GATE_NONE, GATE_CHANNEL, GATE_SEGMENT = range(3)
+GRAD_NORM_ADD = 1
 PROF_GEMM_NT, PROF_GEMM_NN, PROF_GEMM_TN, PROF_ATTN_FWD, PROF_ATTN_BWD = range(5)
 PROF_NORM_FWD, PROF_NORM_BWD, PROF_ROPE, PROF_ACT_FWD, PROF_ACT_BWD = range(5, 10)
 
@@ -68,6 +77,38 @@ class Weights(C.Structure):
 
 class Grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_FIELDS]
+
+
+RESIDUAL_NORM_FIELDS = ("post_w", "post_b", "gate", "pre_w", "pre_b")
+RESIDUAL_NORM_STATS = ("post_mean", "post_rstd", "pre_mean", "pre_rstd")
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("base", C.c_float), ("factor", C.c_float),
+                ("low", C.c_float), ("high", C.c_float), ("orig_context", C.c_float), ("magnitude", C.c_float)]
+
+
+class ResidualNormDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("hidden", C.c_int32), ("post_norm", C.c_int32),
+                ("pre_norm", C.c_int32), ("gate", C.c_int32), ("post_eps", C.c_float), ("pre_eps", C.c_float),
+                ("residual_scale", C.c_float), ("branch_scale", C.c_float)]
+
+
+class ResidualNormWeights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in RESIDUAL_NORM_FIELDS]
+
+
+class ResidualNormGrads(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in RESIDUAL_NORM_FIELDS]
+
+
+class ResidualNormStats(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in RESIDUAL_NORM_STATS]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 _lib = None
@@ -129,6 +170,23 @@ def load_library() -> C.CDLL:
     lib.mmtrain_pipeline_1f1b.argtypes = [P, P, I, I, P, C.POINTER(C.c_double), P]
     lib.mmtrain_inter_reorder.restype = C.c_int
     lib.mmtrain_inter_reorder.argtypes = [P, P, I, I, P, P, P, C.POINTER(C.c_int32)]
+    L = C.c_int64
+    lib.mmtrain_rope.restype = C.c_int
+    lib.mmtrain_rope.argtypes = [P, I, P, P, P, L, P, L, U, P]
+    lib.mmtrain_residual_norm_workspace_bytes.restype = S
+    lib.mmtrain_residual_norm_workspace_bytes.argtypes = [P, I]
+    lib.mmtrain_residual_norm_fwd.restype = C.c_int
+    lib.mmtrain_residual_norm_fwd.argtypes = [P, I, P, P, P, P, P, P, P, P]
+    lib.mmtrain_residual_norm_bwd.restype = C.c_int
+    lib.mmtrain_residual_norm_bwd.argtypes = [P, I, P, P, P, P, P, P, P, P, P, P, U, P, S, P]
+    lib.mmtrain_grad_norm_workspace_bytes.restype = S
+    lib.mmtrain_grad_norm_workspace_bytes.argtypes = [I]
+    lib.mmtrain_grad_norm.restype = C.c_int
+    lib.mmtrain_grad_norm.argtypes = [P, I, C.c_float, U, P, P, S, P]
+    lib.mmtrain_grad_clip.restype = C.c_int
+    lib.mmtrain_grad_clip.argtypes = [P, I, P, P]
+    lib.mmtrain_adam_step_clipped.restype = C.c_int
+    lib.mmtrain_adam_step_clipped.argtypes = [P, L, P, P, P, P, P, I, P, P]
     _lib = lib
     return lib
 
@@ -384,3 +442,92 @@ def mmtrain_profile_read(kind: int, reset: bool = True):
     if rc != OK:
         raise RuntimeError(f"mmtrain_profile_read: {mmtrain_status_string(rc)}")
     return ms.value, n.value
+
+
+# ----------------------------------------------------------------------------
+# include/mmtrain_ops.h: rotary positions, the join of branch and residual stream, gradient norm and clipping
+# ----------------------------------------------------------------------------
+def make_rope_desc(dtype, n_heads, head_dim, rot_dim=None, layout=ROPE_HALF, base=10000.0, scaling=ROPE_PLAIN, factor=1.0,
+                   low=0.0, high=0.0, orig_context=0.0, magnitude=0.0) -> RopeDesc:
+    """rot_dim None: the whole head."""
+    return RopeDesc(C.sizeof(RopeDesc), dtype, n_heads, head_dim, head_dim if rot_dim is None else rot_dim, layout, scaling, base,
+                    factor, low, high, orig_context, magnitude)
+
+
+def mmtrain_rope(desc, n_tokens, batch, positions, x, ld_x, y, ld_y, flags=0, stream=None) -> int:
+    b = batch.struct if isinstance(batch, PackedBatch) else batch
+    return load_library().mmtrain_rope(_ref(desc), n_tokens, _ref(b), _ptr(positions), _ptr(x), ld_x, _ptr(y), ld_y, flags,
+                                       _stream(stream))
+
+
+def make_residual_norm_desc(dtype, hidden, post_norm=NORM_NONE, pre_norm=NORM_NONE, gate=GATE_NONE, post_eps=1e-5, pre_eps=1e-5,
+                            residual_scale=1.0, branch_scale=1.0) -> ResidualNormDesc:
+    return ResidualNormDesc(C.sizeof(ResidualNormDesc), dtype, hidden, post_norm, pre_norm, gate, post_eps, pre_eps,
+                            residual_scale, branch_scale)
+
+
+def make_residual_norm_weights(tensors: Dict[str, object]) -> ResidualNormWeights:
+    return ResidualNormWeights(*[_ptr(tensors.get(n)) for n in RESIDUAL_NORM_FIELDS])
+
+
+def make_residual_norm_grads(tensors: Dict[str, object]) -> ResidualNormGrads:
+    return ResidualNormGrads(*[_ptr(tensors.get(n)) for n in RESIDUAL_NORM_FIELDS])
+
+
+def make_residual_norm_stats(tensors: Dict[str, object]) -> ResidualNormStats:
+    return ResidualNormStats(*[_ptr(tensors.get(n)) for n in RESIDUAL_NORM_STATS])
+
+
+def mmtrain_residual_norm_workspace_bytes(desc, n_tokens: int) -> int:
+    return load_library().mmtrain_residual_norm_workspace_bytes(_ref(desc), n_tokens)
+
+
+def mmtrain_residual_norm_fwd(desc, n_tokens, batch, weights, x, branch, y, h, stats=None, stream=None) -> int:
+    b = batch.struct if isinstance(batch, PackedBatch) else batch
+    return load_library().mmtrain_residual_norm_fwd(_ref(desc), n_tokens, _ref(b), _ref(weights), _ptr(x), _ptr(branch), _ptr(y),
+                                                    _ptr(h), _ref(stats), _stream(stream))
+
+
+def mmtrain_residual_norm_bwd(desc, n_tokens, batch, weights, y, branch, stats, dy, dh, dx, d_branch, grads, flags, workspace,
+                              workspace_bytes, stream=None) -> int:
+    b = batch.struct if isinstance(batch, PackedBatch) else batch
+    return load_library().mmtrain_residual_norm_bwd(_ref(desc), n_tokens, _ref(b), _ref(weights), _ptr(y), _ptr(branch), _ref(stats),
+                                                    _ptr(dy), _ptr(dh), _ptr(dx), _ptr(d_branch), _ref(grads), flags, _ptr(workspace),
+                                                    workspace_bytes, _stream(stream))
+
+
+def _grad_dtype(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_contiguous():
+        raise ValueError("gradients are contiguous float32 or bfloat16 tensors")
+    return F32 if t.dtype == torch.float32 else BF16
+
+
+def make_grad_tensors(grads, outs=None):
+    """The list that mmtrain_grad_norm and mmtrain_grad_clip take, from torch tensors; outs: where each clipped gradient goes
+    (None, or None in a place: in place).  It holds addresses: keep the tensors alive."""
+    outs = [None] * len(grads) if outs is None else outs
+    if len(outs) != len(grads) or any(o is not None and o.numel() != g.numel() for g, o in zip(grads, outs)):
+        raise ValueError("one output of the same size for each gradient")
+    return (GradTensor * len(grads))(*[GradTensor(_ptr(g), _ptr(o), g.numel(), _grad_dtype(g), _grad_dtype(g if o is None else o))
+                                       for g, o in zip(grads, outs)])
+
+
+def mmtrain_grad_norm_workspace_bytes(n_tensors: int) -> int:
+    return load_library().mmtrain_grad_norm_workspace_bytes(n_tensors)
+
+
+def mmtrain_grad_norm(tensors, max_norm, result, workspace, workspace_bytes, flags=0, stream=None) -> int:
+    """tensors: make_grad_tensors(...), or None for none.  result: 16 bytes of device memory (float64 sum of squares, float32 norm,
+    float32 factor)."""
+    return load_library().mmtrain_grad_norm(tensors, 0 if tensors is None else len(tensors), max_norm, flags, _ptr(result),
+                                            _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def mmtrain_grad_clip(tensors, result, stream=None) -> int:
+    return load_library().mmtrain_grad_clip(tensors, 0 if tensors is None else len(tensors), _ptr(result), _stream(stream))
+
+
+def mmtrain_adam_step_clipped(desc, n, master, grad, exp_avg, exp_avg_sq, param_out, param_dtype, result, stream=None) -> int:
+    return load_library().mmtrain_adam_step_clipped(_ref(desc), n, _ptr(master), _ptr(grad), _ptr(exp_avg), _ptr(exp_avg_sq),
+                                                    _ptr(param_out), param_dtype, _ptr(result), _stream(stream))

@@ -3,6 +3,8 @@
 #include "../../include/mmtrain.h"
 #include "kernels.h"
 #include "reduce.h"
+#include "api_checks.h"
+#include "../../include/mmtrain_ops.h"
 #include <cmath>
 #include <initializer_list>
 #include <mutex>
@@ -73,32 +75,6 @@ int check_desc(const mmtrain_layer_desc *desc, Dims &D) {
     D.eps = desc->norm_eps; D.rope_base = desc->rope_base;
     D.scale = desc->softmax_scale > 0.f ? desc->softmax_scale : 1.0f / sqrtf((float)D.d);
     return MMTRAIN_OK;
-}
-
-int check_batch(const mmtrain_batch *b) {
-    if (!b) return MMTRAIN_ERR_INVALID_ARG;
-    if (b->total_tokens < 0 || b->n_segments < 0) return MMTRAIN_ERR_INVALID_ARG;
-    if (b->mask_mode != MMTRAIN_MASK_CAUSAL && b->mask_mode != MMTRAIN_MASK_BIDIR) return MMTRAIN_ERR_INVALID_ARG;
-    if (!b->cu_seqlens_host) return MMTRAIN_ERR_INVALID_ARG;
-    if ((b->seg_mask_dev == nullptr) != (b->seg_mask_host == nullptr)) return MMTRAIN_ERR_INVALID_ARG;
-    const int32_t *cu = b->cu_seqlens_host;
-    if (cu[0] != 0) return MMTRAIN_ERR_BAD_SEGMENTS;
-    for (int s = 0; s < b->n_segments; ++s)
-        if (cu[s + 1] < cu[s]) return MMTRAIN_ERR_BAD_SEGMENTS;
-    if (cu[b->n_segments] != b->total_tokens) return MMTRAIN_ERR_BAD_SEGMENTS;
-    if (b->seg_mask_host)
-        for (int s = 0; s < b->n_segments; ++s)
-            if (b->seg_mask_host[s] > 1) return MMTRAIN_ERR_INVALID_ARG;
-    if (b->total_tokens > 0 && !b->cu_seqlens_dev) return MMTRAIN_ERR_INVALID_ARG;
-    return MMTRAIN_OK;
-}
-
-// The kernels move 16 bytes per lane (vector loads and stores, direct-to-LDS copies): every tensor pointer must be
-// 16-byte aligned.  A misaligned one (a view such as tensor[1:]) is an argument error, not a memory fault.
-bool misaligned(std::initializer_list<const void *> ptrs) {
-    uintptr_t bits = 0;
-    for (const void *p : ptrs) bits |= (uintptr_t)p;
-    return (bits & 15) != 0;
 }
 
 int check_weights(const Dims &D, const mmtrain_layer_weights *w) {
@@ -207,7 +183,6 @@ AttnArgs mk_attn(const Dims &D, const mmtrain_batch *b, const Ctx &c) {
     return a;
 }
 
-#define HIP_TRY(expr) do { hipError_t e_ = (expr); if (e_ != hipSuccess) return MMTRAIN_ERR_HIP; } while (0)
 // the same with the launch bracketed by the events of profiling class `kind` (when that class is enabled)
 #define HIP_TRY_TIMED(kind, st, expr) do { ProfScope ps_((kind), (st)); hipError_t e_ = (expr); if (e_ != hipSuccess) return MMTRAIN_ERR_HIP; } while (0)
 
@@ -827,8 +802,9 @@ int mmtrain_inter_reorder(const double *fwd, const double *bwd, int32_t p, int32
     return MMTRAIN_OK;
 }
 
-int mmtrain_adam_step(const mmtrain_adam_desc *d, int64_t n, float *master, float *grad, float *exp_avg,
-                      float *exp_avg_sq, void *param_out, int32_t param_dtype, void *hip_stream) {
+// clip: device, what the gradient is multiplied with besides grad_scale (null: nothing)
+static int adam_common(const mmtrain_adam_desc *d, int64_t n, float *master, float *grad, float *exp_avg,
+                       float *exp_avg_sq, void *param_out, int32_t param_dtype, const float *clip, void *hip_stream) {
     if (!d || d->struct_size != sizeof(mmtrain_adam_desc) || n < 0) return MMTRAIN_ERR_INVALID_ARG;
     if (param_dtype != MMTRAIN_F32 && param_dtype != MMTRAIN_BF16) return MMTRAIN_ERR_INVALID_ARG;
     if (!(d->lr >= 0.f) || !(d->beta1 >= 0.f && d->beta1 < 1.f) || !(d->beta2 >= 0.f && d->beta2 < 1.f) || !(d->eps > 0.f) ||
@@ -847,8 +823,20 @@ int mmtrain_adam_step(const mmtrain_adam_desc *d, int64_t n, float *master, floa
     a.inv_bias1 = (float)(1.0 / (1.0 - pow((double)d->beta1, (double)d->step)));
     a.inv_bias2 = (float)(1.0 / (1.0 - pow((double)d->beta2, (double)d->step)));
     a.zero_grad = d->zero_grad ? 1 : 0;
+    a.clip = clip;
     HIP_TRY(adam_step(param_dtype, (size_t)n, master, grad, exp_avg, exp_avg_sq, param_out, a, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
+}
+
+int mmtrain_adam_step(const mmtrain_adam_desc *d, int64_t n, float *master, float *grad, float *exp_avg,
+                      float *exp_avg_sq, void *param_out, int32_t param_dtype, void *hip_stream) {
+    return adam_common(d, n, master, grad, exp_avg, exp_avg_sq, param_out, param_dtype, nullptr, hip_stream);
+}
+
+int mmtrain_adam_step_clipped(const mmtrain_adam_desc *d, int64_t n, float *master, float *grad, float *exp_avg, float *exp_avg_sq,
+                              void *param_out, int32_t param_dtype, const mmtrain_grad_norm_result *result, void *hip_stream) {
+    if (!result || misaligned({result})) return MMTRAIN_ERR_INVALID_ARG;
+    return adam_common(d, n, master, grad, exp_avg, exp_avg_sq, param_out, param_dtype, &result->factor, hip_stream);
 }
 
 // ---- for the tests: which form a call takes (host decisions only; not declared in mmtrain.h) -----------------------------

@@ -74,6 +74,16 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
     return s;
 }
 
+// The segment that holds token t: s with cu[s] <= t < cu[s+1].
+__device__ __forceinline__ int find_segment(const int *__restrict__ cu, int S, int t) {
+    int lo = 0, hi = S;               // last s in [0, S) with cu[s] <= t
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu[mid] <= t) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
 static inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
 }  // namespace mmt

@@ -191,6 +191,7 @@ hipError_t gelu_bwd_colsum(int dtype, const void *d_a, const void *z, void *d_z,
 struct AdamArgs {
     float lr, beta1, beta2, omb1, omb2, eps, weight_decay, grad_scale, inv_bias1, inv_bias2;
     int zero_grad;
+    const float *clip;          // device, or null: a further factor of the gradient; NaN: no step
 };
 // whether a shard of n elements is streamed (param_bytes: per element of the working copy, 0 without one)
 bool adam_streams(size_t n, size_t param_bytes);

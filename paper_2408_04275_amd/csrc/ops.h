@@ -1,0 +1,64 @@
+// Internal launch interface of the operators in mmtrain_ops.h (see kernels.h for the conventions).
+#pragma once
+#include "kernels.h"
+
+namespace mmt {
+
+// rope.hip.  turns[i] = frequency of pair i in turns per position.
+constexpr int ROPE_MAX_HALF = 128;
+struct RopeArgs {
+    int T, heads, d, half;          // half = rot_dim / 2
+    bool interleaved;
+    const int *positions;           // device [T], or null: from cu
+    const int *cu; int S;
+    const void *x; long ldx;
+    void *y; long ldy;
+    float cos_scale, sin_scale;     // magnitude, and magnitude with the direction's sign
+    double turns[ROPE_MAX_HALF];
+};
+hipError_t rope(int dtype, const RopeArgs &a, hipStream_t st);
+
+// residual_norm.hip: n = norm_post(b); y = alpha x + beta gate n; h = norm_pre(y)
+enum { NORM_NONE = 0, NORM_RMS = 1, NORM_LAYER = 2 };
+enum { GATE_NONE = 0, GATE_CHANNEL = 1, GATE_SEGMENT = 2 };
+struct JoinArgs {
+    int T, H, post, pre, gate;
+    float post_eps, pre_eps, alpha, beta;
+    const int *cu; int S;           // segment gates
+    const void *post_w, *post_b, *gate_v, *pre_w, *pre_b;
+    float *post_mean, *post_rstd, *pre_mean, *pre_rstd;
+    const void *b;                  // null: no branch
+    const void *x;                  // forward; y and h may be null
+    void *y, *h;
+    const void *dy, *dh;            // backward (y is read); dy, dx, db may be null
+    void *dx, *db;
+    // backward: partial sums, null where not wanted.  post_w, post_b, pre_w, pre_b and a channel's gate: [join_bwd_blocks][H];
+    // a segment's gate: [2 * join_bwd_blocks][H], see there
+    float *p_post_w, *p_post_b, *p_gate, *p_pre_w, *p_pre_b;
+    void *d_gate;                   // a segment's gate: its gradient [S][H]
+    int grad_f32, accumulate;       // type of d_gate, and whether it is added to
+};
+hipError_t join_fwd(int dtype, const JoinArgs &a, hipStream_t st);
+// Workgroup b of the backward kernel has rows join_row(b) .. join_row(b + 1) - 1
+int join_bwd_blocks(int T, int H);
+hipError_t join_bwd(int dtype, const JoinArgs &a, hipStream_t st);
+
+// grad_norm.hip
+constexpr int GRAD_BATCH = 128;     // tensors a launch
+struct GradBatch {
+    const void *in[GRAD_BATCH];
+    void *out[GRAD_BATCH];
+    long n[GRAD_BATCH];
+    int first[GRAD_BATCH + 1];      // first chunk of each tensor; [count] = all
+    unsigned char in_f32[GRAD_BATCH], out_f32[GRAD_BATCH];
+    int count;
+};
+constexpr int GRAD_CHUNK = 16384;   // elements
+constexpr int GRAD_BLOCKS = 1024;   // partial sums a launch leaves at most
+struct GradResult { double sum_sq; float norm, factor; };
+int grad_norm_blocks(const GradBatch &b);
+hipError_t grad_sum_sq(const GradBatch &b, double *part, hipStream_t st);
+hipError_t grad_norm_finish(const double *part, int n, float max_norm, bool add, GradResult *result, hipStream_t st);
+hipError_t grad_clip(const GradBatch &b, const GradResult *result, hipStream_t st);
+
+}  // namespace mmt

@@ -4,6 +4,7 @@
 // (AdamW).  Memory-bound: per element it reads 16 bytes and writes 12 + the working copy (+ 4 when the
 // gradient is cleared for the next accumulation), 16 bytes per lane per access.
 #include "kernels.h"
+#include <type_traits>
 
 namespace mmt {
 
@@ -36,12 +37,22 @@ __device__ __forceinline__ void store(T *p, V v) {
 }
 
 // QUADS groups of four elements per thread, all requested before the first is updated.  STREAM: nontemporal accesses, except for
-// the gradient's load: the backward pass has just written it, so the memory-side cache may still hold it.
-template <typename TP, bool STREAM, int QUADS>
+// the gradient's load: the backward pass has just written it, so the memory-side cache may still hold it.  CLIP: a.clip is given.
+template <typename TP, bool STREAM, int QUADS, bool CLIP>
 __global__ __launch_bounds__(256) void adam_kernel(size_t n, float *__restrict__ w, float *__restrict__ g,
                                                    float *__restrict__ m, float *__restrict__ v, TP *__restrict__ p,
                                                    AdamArgs a) {
     const size_t first = ((size_t)blockIdx.x * QUADS * 256 + threadIdx.x) * 4;
+    if constexpr (CLIP) {
+        const float f = *a.clip;
+        if (f != f) {                               // a norm that is not finite: the step is skipped
+            if (!a.zero_grad) return;
+            for (int k = 0; k < QUADS; ++k)
+                for (size_t j = first + k * 1024; j < n && j < first + k * 1024 + 4; ++j) g[j] = 0.f;
+            return;
+        }
+        a.grad_scale *= f;
+    }
     f32x4 wv[QUADS], gv[QUADS], mv[QUADS], vv[QUADS];
 #pragma unroll
     for (int k = 0; k < QUADS; ++k) {
@@ -82,8 +93,13 @@ __global__ __launch_bounds__(256) void adam_kernel(size_t n, float *__restrict__
 
 template <typename TP>
 hipError_t launch(size_t n, float *w, float *g, float *m, float *v, TP *p, const AdamArgs &a, hipStream_t st) {
-    if (adam_streams(n, p ? sizeof(TP) : 0)) adam_kernel<TP, true, 2><<<(unsigned)((n + 2047) / 2048), 256, 0, st>>>(n, w, g, m, v, p, a);
-    else adam_kernel<TP, false, 1><<<(unsigned)((n + 1023) / 1024), 256, 0, st>>>(n, w, g, m, v, p, a);
+    auto go = [&](auto CLIP_) {
+        constexpr bool CLIP = decltype(CLIP_)::value;
+        if (adam_streams(n, p ? sizeof(TP) : 0)) adam_kernel<TP, true, 2, CLIP><<<(unsigned)((n + 2047) / 2048), 256, 0, st>>>(n, w, g, m, v, p, a);
+        else adam_kernel<TP, false, 1, CLIP><<<(unsigned)((n + 1023) / 1024), 256, 0, st>>>(n, w, g, m, v, p, a);
+    };
+    if (a.clip) go(std::true_type{});
+    else go(std::false_type{});
     return hipGetLastError();
 }
 
