@@ -1,43 +1,135 @@
 // Rotary positions of whole heads or their front part.
+//
+// Memory-bound: each feature is read and written once, and the 2 half numbers of a token's rotation serve all its heads.  So a
+// workgroup takes whole tokens: its threads first put the rotations of its tokens into LDS (an angle in fp64 each, reduced to a
+// turn, then sine and cosine in fp32), the data of their first heads already on its way, and then walk over the heads in chunks of up to 16
+// bytes.  No table in memory, no launch before this one.
 #include "ops.h"
 
 namespace mmt {
 namespace {
 
-template <typename T>
-__global__ __launch_bounds__(256) void rope_heads_kernel(RopeArgs a) {
-    const int units = a.half + (a.x == a.y ? 0 : a.d - 2 * a.half);         // pairs, then features that pass through
-    const long idx = (long)blockIdx.x * 256 + threadIdx.x;
-    if (idx >= (long)a.T * a.heads * units) return;
-    const int u = (int)(idx % units), h = (int)(idx / units % a.heads);
-    const long t = idx / ((long)units * a.heads);
-    const T *x = (const T *)a.x + t * a.ldx + (long)h * a.d;
-    T *y = (T *)a.y + t * a.ldy + (long)h * a.d;
-    if (u >= a.half) {
-        y[u + a.half] = x[u + a.half];
-        return;
+// V neighbouring elements as loaded
+template <int BYTES> struct Bytes;
+template <> struct Bytes<16> { typedef u32x4 type; };
+template <> struct Bytes<8> { typedef u32x2 type; };
+template <> struct Bytes<4> { typedef uint32_t type; };
+template <> struct Bytes<2> { typedef uint16_t type; };
+
+template <typename T, int V> struct Chunk {
+    typedef typename Bytes<V * sizeof(T)>::type raw;
+    union { raw r; T e[V]; };
+    __device__ __forceinline__ void load(const T *p) { r = *reinterpret_cast<const raw *>(p); }
+    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<raw *>(p) = r; }
+    __device__ __forceinline__ float get(int i) const { return Elem<T>::load(&e[i]); }
+    __device__ __forceinline__ void set(const float (&v)[V]) {
+        if constexpr (sizeof(T) == 4 || V == 1) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) Elem<T>::store(&e[i], v[i]);
+        } else {
+            uint32_t w[V / 2];
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            __builtin_memcpy(&r, w, sizeof(r));
+        }
     }
-    const int pos = a.positions ? a.positions[t] : (int)t - a.cu[find_segment(a.cu, a.S, (int)t)];
-    const double turn = pos * a.turns[u];
-    float s, c;
-    sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
-    c *= a.cos_scale; s *= a.sin_scale;
-    const int i0 = a.interleaved ? 2 * u : u, i1 = a.interleaved ? 2 * u + 1 : u + a.half;
-    const float v0 = Elem<T>::load(x + i0), v1 = Elem<T>::load(x + i1);
-    Elem<T>::store(y + i0, v0 * c - v1 * s);
-    Elem<T>::store(y + i1, v1 * c + v0 * s);
+};
+
+struct RopeShape {
+    int tile;                   // tokens a workgroup
+    int units;                  // chunk pairs of a head: first the rotated ones, then those that pass through
+    int rot_units, copy_chunks;
+    int group;                  // heads a workgroup has at work at once: 256 / units
+    int step_tokens, step_heads;// group = step_tokens * heads + step_heads
+};
+
+// A unit is two chunks of V elements: the two halves of V pairs, or 2 V features that pass through (of which the last unit may have V).
+template <typename T, int V, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_heads_kernel(RopeArgs a, RopeShape s) {
+    extern __shared__ float2 turned[];                       // [tile][half]: cosine, sine
+    const int t0 = blockIdx.x * s.tile, tokens = min(s.tile, a.T - t0);
+    const int u = threadIdx.x % s.units, g = threadIdx.x / s.units;
+    const bool rotates = u < s.rot_units;
+    const int pair = u * V, copied = 2 * (u - s.rot_units);
+    const int o0 = rotates ? (INTERLEAVED ? 2 * pair : pair) : 2 * a.half + copied * V;
+    const int o1 = rotates ? (INTERLEAVED ? 2 * pair + V : pair + a.half) : o0 + V;
+    const bool second = rotates || copied + 1 < s.copy_chunks;
+    int tok = g / a.heads, head = g % a.heads;
+    const bool active = g < s.group;
+    Chunk<T, V> c0, c1;
+    auto request = [&] {
+        const T *x = (const T *)a.x + (t0 + tok) * a.ldx + (long)head * a.d;
+        c0.load(x + o0);
+        if (second) c1.load(x + o1);
+    };
+    if (active && tok < tokens) request();
+    for (int k = threadIdx.x; k < tokens * a.half; k += 256) {
+        const int t = t0 + k / a.half;
+        const int pos = a.positions ? a.positions[t] : t - a.cu[find_segment(a.cu, a.S, t)];
+        const double turn = pos * a.turns[k % a.half];
+        float si, co;
+        sincospif(2.f * (float)(turn - rint(turn)), &si, &co);
+        turned[k] = make_float2(co * a.cos_scale, si * a.sin_scale);
+    }
+    __syncthreads();
+    if (!active) return;
+    while (tok < tokens) {
+        T *y = (T *)a.y + (t0 + tok) * a.ldy + (long)head * a.d;
+        const float2 *cs = turned + tok * a.half + pair;
+        Chunk<T, V> d0 = c0, d1 = c1;
+        tok += s.step_tokens; head += s.step_heads;
+        if (head >= a.heads) { head -= a.heads; ++tok; }
+        if (tok < tokens) request();
+        if (rotates) {
+            float v[2 * V], w[2 * V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) { v[i] = d0.get(i); v[V + i] = d1.get(i); }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int i0 = INTERLEAVED ? 2 * i : i, i1 = INTERLEAVED ? 2 * i + 1 : V + i;
+                const float2 r = cs[i];
+                w[i0] = v[i0] * r.x - v[i1] * r.y;
+                w[i1] = v[i1] * r.x + v[i0] * r.y;
+            }
+            float lo[V], hi[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) { lo[i] = w[i]; hi[i] = w[V + i]; }
+            d0.set(lo); d1.set(hi);
+        }
+        d0.store(y + o0);
+        if (second) d1.store(y + o1);
+    }
+}
+
+template <typename T, int V>
+hipError_t launch(const RopeArgs &a, hipStream_t st) {
+    RopeShape s;
+    s.rot_units = a.half / V;
+    s.copy_chunks = a.x == a.y ? 0 : (a.d - 2 * a.half) / V;
+    s.units = s.rot_units + (s.copy_chunks + 1) / 2;         // at most 128
+    s.group = 256 / s.units;
+    s.step_tokens = s.group / a.heads;
+    s.step_heads = s.group % a.heads;
+    // Tokens a workgroup: one angle per thread, and enough workgroups for the chip
+    const int by_angles = a.half < 256 ? 256 / a.half : 1, by_tokens = a.T / 2048;
+    s.tile = by_tokens < 1 ? 1 : by_tokens < by_angles ? by_tokens : by_angles;
+    const size_t lds = (size_t)s.tile * a.half * sizeof(float2);
+    const int blocks = ceil_div(a.T, s.tile);
+    if (a.interleaved) rope_heads_kernel<T, V, true><<<blocks, 256, lds, st>>>(a, s);
+    else rope_heads_kernel<T, V, false><<<blocks, 256, lds, st>>>(a, s);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t rope(int dtype, const RopeArgs &a, hipStream_t st) {
-    const long total = (long)a.T * a.heads * (a.half + (a.x == a.y ? 0 : a.d - 2 * a.half));
-    if (total == 0) return hipSuccess;
-    const long blocks = (total + 255) / 256;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    if (dtype == DT_F32) rope_heads_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a);
-    else rope_heads_kernel<bf16_t><<<(unsigned)blocks, 256, 0, st>>>(a);
-    return hipGetLastError();
+    if (a.T == 0) return hipSuccess;
+    // elements that every chunk's place is a multiple of: the widest chunk that all accesses are aligned for
+    const long places = a.half | a.d | a.ldx | a.ldy;
+    const int v = dtype == DT_F32 ? (places % 4 == 0 ? 4 : places % 2 == 0 ? 2 : 1)
+                                  : (places % 8 == 0 ? 8 : places % 4 == 0 ? 4 : places % 2 == 0 ? 2 : 1);
+    if (dtype == DT_F32) return v == 4 ? launch<float, 4>(a, st) : v == 2 ? launch<float, 2>(a, st) : launch<float, 1>(a, st);
+    return v == 8 ? launch<bf16_t, 8>(a, st) : v == 4 ? launch<bf16_t, 4>(a, st) : v == 2 ? launch<bf16_t, 2>(a, st) : launch<bf16_t, 1>(a, st);
 }
 
 }  // namespace mmt
