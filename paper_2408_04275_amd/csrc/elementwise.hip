@@ -5,6 +5,7 @@
 #include "kernels.h"
 #include "reduce.h"
 #include "vec8.h"
+#include "resident.h"
 #include <algorithm>
 #include <type_traits>
 #include <atomic>
@@ -193,22 +194,7 @@ __global__ __launch_bounds__(256) void norm_fwd_wave_kernel(const T *__restrict_
     }
 }
 
-// One launch of norm_fwd_rows_kernel or norm_fwd_wave_kernel: exactly as many workgroups as the device keeps resident at once (a grid one
-// workgroup per compute unit larger runs a second, nearly empty round: 22.9 -> 26.9 us at the 7B shape).
-template <typename K>
-hipError_t resident_workgroups(std::atomic<int> &cached, K kern, int &grid) {
-    grid = cached.load(std::memory_order_relaxed);
-    if (grid) return hipSuccess;
-    int dev = 0, cus = 0, per_cu = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-    if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kern, 256, 0);
-    if (e != hipSuccess) return e;
-    grid = (cus > 0 ? cus : 256) * (per_cu > 0 ? per_cu : 4);
-    cached.store(grid, std::memory_order_relaxed);
-    return hipSuccess;
-}
-// WAVE_ROWS: a wavefront per row (four per workgroup), otherwise a workgroup per row
+// One launch of norm_fwd_rows_kernel or norm_fwd_wave_kernel.  WAVE_ROWS: a wavefront per row (four per workgroup), otherwise a workgroup per row
 template <typename T, bool LN, int MAXC, bool WAVE_ROWS>
 hipError_t launch_norm_fwd_rows(const void *x, const void *g, const void *b, void *out, float *mean, float *rstd, int nrows,
                                 int H, float eps, const TokenPrep *prep, hipStream_t st) {
