@@ -62,6 +62,7 @@ int join_common(const mmtrain_residual_norm_desc *d, int32_t T, const mmtrain_ba
     if (d->gate == MMTRAIN_GATE_SEGMENT) {
         if ((rc = check_batch(batch))) return rc;
         if (batch->total_tokens != T) return MMTRAIN_ERR_BAD_SEGMENTS;
+        if (batch->n_segments > JOIN_MAX_SEGMENTS) return MMTRAIN_ERR_UNSUPPORTED;
         a.cu = batch->cu_seqlens_dev; a.S = batch->n_segments;
         if (a.S > 0 && !a.cu) return MMTRAIN_ERR_INVALID_ARG;
     }
@@ -259,16 +260,8 @@ int mmtrain_residual_norm_bwd(const mmtrain_residual_norm_desc *desc, int32_t n_
     a.y = const_cast<void *>(y); a.b = branch; a.dy = dy; a.dh = dh; a.dx = dx; a.db = d_branch;
     a.grad_f32 = desc->dtype == MMTRAIN_F32 || (flags & MMTRAIN_BWD_WGRAD_F32);
     a.accumulate = (flags & MMTRAIN_BWD_ACCUMULATE_WGRAD) != 0;
-    if (desc->gate == MMTRAIN_GATE_SEGMENT) a.d_gate = g.gate;
-    hipStream_t st = (hipStream_t)hip_stream;
-    HIP_TRY(join_bwd(desc->dtype, a, st));
-    if (!any) return MMTRAIN_OK;
-    const int rows = join_bwd_blocks(n_tokens, desc->hidden), H = desc->hidden;
-    const ReduceJob jobs[5] = {{a.p_post_w, g.post_w, rows, H}, {a.p_post_b, g.post_b, rows, H}, {a.p_pre_w, g.pre_w, rows, H},
-                               {a.p_pre_b, g.pre_b, rows, H}, {desc->gate == MMTRAIN_GATE_CHANNEL ? a.p_gate : nullptr, g.gate, rows, H}};
-    bool left = false;
-    for (const ReduceJob &j : jobs) left = left || (j.part && j.out);
-    if (left) HIP_TRY(reduce_jobs(a.grad_f32 ? DT_F32 : DT_BF16, jobs, 5, a.accumulate, st));
+    a.d_post_w = g.post_w; a.d_post_b = g.post_b; a.d_gate = g.gate; a.d_pre_w = g.pre_w; a.d_pre_b = g.pre_b;
+    HIP_TRY(join_bwd(desc->dtype, a, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 

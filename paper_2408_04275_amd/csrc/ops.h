@@ -35,11 +35,12 @@ struct JoinArgs {
     // backward: partial sums, null where not wanted.  post_w, post_b, pre_w, pre_b and a channel's gate: [join_bwd_blocks][H];
     // a segment's gate: [2 * join_bwd_blocks][H], see there
     float *p_post_w, *p_post_b, *p_gate, *p_pre_w, *p_pre_b;
-    void *d_gate;                   // a segment's gate: its gradient [S][H]
-    int grad_f32, accumulate;       // type of d_gate, and whether it is added to
+    void *d_post_w, *d_post_b, *d_gate, *d_pre_w, *d_pre_b;     // the gradients, null where not wanted
+    int grad_f32, accumulate;       // their type, and whether they are added to
 };
+constexpr int JOIN_MAX_SEGMENTS = 1 << 20;      // with a segment gate: [segments][H] are the gates alone
 hipError_t join_fwd(int dtype, const JoinArgs &a, hipStream_t st);
-// Workgroup b of the backward kernel has rows join_row(b) .. join_row(b + 1) - 1
+// workgroups of the backward kernel: never fewer for more rows
 int join_bwd_blocks(int T, int H);
 hipError_t join_bwd(int dtype, const JoinArgs &a, hipStream_t st);
 

@@ -7,64 +7,149 @@
 // time, the next ones requested before the present ones are reduced.  Gains, biases and gates stay in registers; so do backward's
 // sums over tokens, which leave the workgroup as one partial row.
 #include "ops.h"
+#include "reduce.h"
 #include "vec8.h"
 #include "resident.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace mmt {
 namespace {
 
-// first row of workgroup b of `blocks`
-__device__ __forceinline__ int join_row(int T, int blocks, int b) { return (int)((long)T * b / blocks); }
+// first row of workgroup b: the first T % blocks workgroups have one row more
+__device__ __forceinline__ int join_row(int T, int blocks, int b) { return b * (T / blocks) + min(b, T % blocks); }
 
-// Sums over the G threads of a row.  red: two buffers, used in turn, so that one barrier per sum is enough (a thread that writes a buffer
-// again has passed the barrier behind its last reading).  All threads of the workgroup call it together.
-template <int G, int NT> struct RowSum {
-    float (*red)[NT / 64][2];
-    int turn = 0;
+// Sum over the wavefront, the same in all lanes.  Lanes are added with DPP moves, which stay in the vector ALU: with shuffles, each of which
+// goes through the LDS unit, a row's sums were a chain of 6 x 100 clocks.  Quads, half rows and rows of 16 lanes are folded by permutations,
+// then rows 0 and 2 are added to 1 and 3, and row 1 to 3.
+template <int CTRL, int ROWS> __device__ __forceinline__ float add_dpp(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_total(float v) {
+    v = add_dpp<0xb1, 0xf>(v);          // quad_perm 1 0 3 2
+    v = add_dpp<0x4e, 0xf>(v);          // quad_perm 2 3 0 1
+    v = add_dpp<0x141, 0xf>(v);         // row_half_mirror
+    v = add_dpp<0x140, 0xf>(v);         // row_mirror
+    v = add_dpp<0x142, 0xa>(v);         // row_bcast 15 to rows 1 and 3
+    v = add_dpp<0x143, 0xc>(v);         // row_bcast 31 to rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Sums over the G threads of a row, MC chunks of 8 columns each.  red: two buffers, used in turn, so that one barrier per sum is enough (a
+// thread that writes a buffer again has passed the barrier behind its last reading).  All threads of the workgroup call it together.
+template <int G, int MC, int NT> struct RowSum {
+    float2 (*red)[NT / 64];
+    int H, turn = 0;
     __device__ __forceinline__ void operator()(float &a, float &b) {
-        a = wave_sum(a); b = wave_sum(b);
-        if constexpr (G == 64) return;
-        const int wave = threadIdx.x >> 6, first = (threadIdx.x / G) * (G / 64);
-        if ((threadIdx.x & 63) == 0) { red[turn][wave][0] = a; red[turn][wave][1] = b; }
-        __syncthreads();
-        a = b = 0.f;
+        a = wave_total(a); b = wave_total(b);
+        if constexpr (G > 64) {
+            const float2 *all = share(make_float2(a, b));
+            a = b = 0.f;
 #pragma unroll
-        for (int i = 0; i < G / 64; ++i) { a += red[turn][first + i][0]; b += red[turn][first + i][1]; }
-        turn ^= 1;
+            for (int i = 0; i < G / 64; ++i) { a += all[i].x; b += all[i].y; }
+        }
     }
-    __device__ __forceinline__ float operator()(float a) {
-        a = wave_sum(a);
-        if constexpr (G == 64) return a;
-        const int wave = threadIdx.x >> 6, first = (threadIdx.x / G) * (G / 64);
-        if ((threadIdx.x & 63) == 0) red[turn][wave][0] = a;
-        __syncthreads();
-        a = 0.f;
+    __device__ __forceinline__ void operator()(float &a) {
+        a = wave_total(a);
+        if constexpr (G > 64) {
+            const float2 *all = share(make_float2(a, 0.f));
+            a = 0.f;
 #pragma unroll
-        for (int i = 0; i < G / 64; ++i) a += red[turn][first + i][0];
+            for (int i = 0; i < G / 64; ++i) a += all[i].x;
+        }
+    }
+    __device__ __forceinline__ const float2 *share(float2 mine) {
+        if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = mine;
+        __syncthreads();
+        const float2 *all = &red[turn][threadIdx.x / G * (G / 64)];
         turn ^= 1;
-        return a;
+        return all;
+    }
+    // columns of wavefront i of the row
+    __device__ __forceinline__ float columns(int i) const {
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < MC; ++k) n += min(max(H - (i * 64 + k * G) * 8, 0), 512);
+        return (float)n;
+    }
+    // Mean and 1 / deviation of the row of which this thread holds v (zero outside of it).  With a mean: first about each wavefront's own mean, then
+    // joined, so that nothing cancels however far the row is from zero and one barrier is enough.
+    template <typename In>
+    __device__ __forceinline__ void statistics(const float (&v)[MC][8], bool layer, float eps, In inside, float &mu, float &r) {
+        const float inv_h = 1.f / H;
+        float q = 0.f;
+        mu = 0.f;
+        if (layer) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < MC; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += v[i][j];
+            const float n = columns(threadIdx.x % G / 64);
+            mu = n > 0.f ? wave_total(sum) / n : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < MC; ++i)
+            if (inside(i)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q += (v[i][j] - mu) * (v[i][j] - mu);
+            }
+        q = wave_total(q);
+        if constexpr (G > 64) {
+            const float2 *all = share(make_float2(mu, q));
+            q = mu = 0.f;
+            if (layer) {
+#pragma unroll
+                for (int i = 0; i < G / 64; ++i) mu += columns(i) * all[i].x;
+                mu *= inv_h;
+            }
+#pragma unroll
+            for (int i = 0; i < G / 64; ++i) q += all[i].y + (layer ? columns(i) * (all[i].x - mu) * (all[i].x - mu) : 0.f);
+        }
+        r = 1.f / sqrtf(q * inv_h + eps);
     }
 };
+
+// A parameter's chunk as loaded: keeps the compiler from holding it widened to fp32 over the whole loop, twice the registers in bf16.  For the
+// kernels that would spill otherwise (9000 x 8192, two LayerNorms and a gate, 295 -> 243 us); the others are slower for it (two RMSNorms 192 -> 214).
+__device__ __forceinline__ void as_loaded(Raw8<bf16_t> &r) { asm("" : "+v"(r.a.x), "+v"(r.a.y), "+v"(r.a.z), "+v"(r.a.w)); }
+__device__ __forceinline__ void as_loaded(Raw8<float> &) {}
 
 template <typename T> __device__ __forceinline__ void zero8(Raw8<T> &r) { __builtin_memset(&r, 0, sizeof(r)); }
 
 // LN: one of the norms is a LayerNorm (gains only otherwise)
 template <typename T, int G, int MC, int NT, bool LN>
-__global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
+__global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd_kernel(JoinArgs a) {
     constexpr int R = NT / G;
-    __shared__ float red_[2][NT / 64][2];
-    RowSum<G, NT> row_sum{red_};
-    const int lane = threadIdx.x % G, grp = threadIdx.x / G, H = a.H;
+    constexpr bool IN_LDS = LN && MC > 1 && G > 256 && sizeof(T) == 2, TIGHT = LN && MC > 1 && !IN_LDS;
+    __shared__ float2 red[2][NT / 64];
+    // a wavefront has one row's columns: rows are scalars, and addresses a scalar and a column
+    const int lane = threadIdx.x % G, grp = __builtin_amdgcn_readfirstlane(threadIdx.x / G), H = a.H;
+    RowSum<G, MC, NT> row_sum{red, H};
     const int r0 = join_row(a.T, gridDim.x, blockIdx.x), r1 = join_row(a.T, gridDim.x, blockIdx.x + 1);
-    const float inv_h = 1.f / H;
     auto col = [&](int i) { return (lane + i * G) * 8; };
-    Raw8<T> nx[MC], nb[MC], w2[MC], w1[MC], gt[MC], b2[LN ? MC : 1], b1[LN ? MC : 1];
+    // IN_LDS: gains and biases wait in LDS, each thread's own, where registers for them would cost a workgroup per compute unit
+    __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 4 : 1][IN_LDS ? G * MC * 8 : 8];
+    constexpr int HELD = IN_LDS ? 1 : MC;
+    Raw8<T> nx[MC], nb[MC], w2[HELD], w1[HELD], gt[MC], b2[LN ? HELD : 1], b1[LN ? HELD : 1];
+    auto keep = [&](Raw8<T> *held, int slot, int i, const void *from) {
+        const Raw8<T> v = load_plain8((const T *)from + col(i));
+        if constexpr (IN_LDS) *reinterpret_cast<Raw8<T> *>(&parked[slot][col(i)]) = v;
+        else held[i] = v;
+    };
+    auto kept = [&](Raw8<T> *held, int slot, int i) {
+        if constexpr (IN_LDS) return *reinterpret_cast<const Raw8<T> *>(&parked[slot][col(i)]);
+        if constexpr (TIGHT) as_loaded(held[i]);
+        return held[i];
+    };
+    // what is outside of the row stays zero from here on
+#pragma unroll
+    for (int i = 0; i < MC; ++i) { zero8(nx[i]); zero8(nb[i]); }
     auto request = [&](int row) {
+        if (row >= r1) return;
 #pragma unroll
         for (int i = 0; i < MC; ++i) {
-            zero8(nx[i]); zero8(nb[i]);
-            if (col(i) >= H || row >= r1) continue;
+            if (col(i) >= H) continue;
             const size_t at = (size_t)row * H + col(i);
             load_raw8((const T *)a.x + at, nx[i]);
             if (a.b) load_raw8((const T *)a.b + at, nb[i]);
@@ -74,37 +159,21 @@ __global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
 #pragma unroll
     for (int i = 0; i < MC; ++i) {
         if (col(i) >= H) continue;
-        if (a.post != NORM_NONE) w2[i] = load_plain8((const T *)a.post_w + col(i));
-        if (a.pre != NORM_NONE) w1[i] = load_plain8((const T *)a.pre_w + col(i));
-        if (LN && a.post == NORM_LAYER) b2[i] = load_plain8((const T *)a.post_b + col(i));
-        if (LN && a.pre == NORM_LAYER) b1[i] = load_plain8((const T *)a.pre_b + col(i));
+        if (a.post != NORM_NONE) keep(w2, 0, i, a.post_w);
+        if (a.pre != NORM_NONE) keep(w1, 1, i, a.pre_w);
+        if (LN && a.post == NORM_LAYER) keep(b2, 2, i, a.post_b);
+        if (LN && a.pre == NORM_LAYER) keep(b1, 3, i, a.pre_b);
         if (a.gate == GATE_CHANNEL) gt[i] = load_plain8((const T *)a.gate_v + col(i));
     }
     int seg_end = 0;
     // v <- normalised v, gain and bias applied
-    auto norm = [&](float (&v)[MC][8], int kind, float eps, const Raw8<T> (&w)[MC], const Raw8<T> *bias, float &mu, float &r) {
-        mu = 0.f;
-        if (LN && kind == NORM_LAYER) {
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < MC; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s += v[i][j];
-            mu = row_sum(s) * inv_h;
-        }
-        float q = 0.f;
-#pragma unroll
-        for (int i = 0; i < MC; ++i)
-            if (col(i) < H) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q += (v[i][j] - mu) * (v[i][j] - mu);
-            }
-        r = 1.f / sqrtf(row_sum(q) * inv_h + eps);
+    auto norm = [&](float (&v)[MC][8], int kind, float eps, Raw8<T> *w, Raw8<T> *bias, int slot, float &mu, float &r) {
+        row_sum.statistics(v, LN && kind == NORM_LAYER, eps, [&](int i) { return col(i) < H; }, mu, r);
 #pragma unroll
         for (int i = 0; i < MC; ++i) {
             float g[8], o[8];
-            unpack8(w[i], g);
-            if (LN && kind == NORM_LAYER) unpack8(bias[i], o);
+            unpack8(kept(w, slot, i), g);
+            if (LN && kind == NORM_LAYER) unpack8(kept(bias, slot + 2, i), o);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - mu) * r * g[j] + (LN && kind == NORM_LAYER ? o[j] : 0.f);
         }
@@ -125,7 +194,7 @@ __global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
                     if (col(i) < H) gt[i] = load_plain8((const T *)a.gate_v + (size_t)seg * H + col(i));
             }
             if (a.post != NORM_NONE) {
-                norm(v, a.post, a.post_eps, w2, b2, mu, r);
+                norm(v, a.post, a.post_eps, w2, b2, 0, mu, r);
                 if (lane == 0 && valid) {
                     if (a.post_rstd) a.post_rstd[row] = r;
                     if (LN && a.post == NORM_LAYER && a.post_mean) a.post_mean[row] = mu;
@@ -134,6 +203,7 @@ __global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
                 float g[8];
+                if constexpr (TIGHT) as_loaded(gt[i]);
                 if (a.gate != GATE_NONE) unpack8(gt[i], g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -147,7 +217,7 @@ __global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
                 for (int j = 0; j < 8; ++j) v[i][j] = xv[i][j];
         }
         if (a.pre == NORM_NONE) continue;
-        norm(v, a.pre, a.pre_eps, w1, b1, mu, r);
+        norm(v, a.pre, a.pre_eps, w1, b1, 1, mu, r);
         if (lane == 0 && valid) {
             if (a.pre_rstd) a.pre_rstd[row] = r;
             if (LN && a.pre == NORM_LAYER && a.pre_mean) a.pre_mean[row] = mu;
@@ -159,66 +229,92 @@ __global__ __launch_bounds__(NT) void join_fwd_kernel(JoinArgs a) {
 }
 
 // With hat = (v - mean) r and back = d_out w, a norm's input gradient is r (back - mean(back) [LAYER] - hat mean(back hat)); gain and bias
-// get sum d_out hat and sum d_out.  Gradient of y: d = dy + the pre norm's; then dx = alpha d, the branch gets beta gate d through the
-// post norm, and the gate sum beta n d.
+// get sum d_out hat and sum d_out.  Gradient of y: d = dy + the pre norm's; then dx = alpha d, and the branch gets beta gate d through the
+// post norm.  A gate is the same in all rows of its segment (or in all rows), so the sums A = sum d hat and B = sum d over these rows give all three
+// gradients behind the block: gain beta gate A, bias beta gate B, gate beta (w A + b B), or beta A with hat = branch where there is no post norm.
 //
 // By segment, a workgroup's gate sums go out at the end of each segment's rows: as the gradient where it has all of them, else into its
-// slot 0 if its range begins inside the segment or with it, and into slot 1 otherwise (then the range ends in it).
-template <typename T, int G, int MC, int NT, bool LN, bool GATE>
+// slot 0 if its range begins inside the segment or with it, and into slot 1 otherwise (then the range ends in it); the post norm's sums are added up in
+// LDS.  One workgroup per compute unit: more would leave more partial rows to be added up.
+template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     constexpr int R = NT / G, W = G * MC * 8;
-    __shared__ float red_[2][NT / 64][2];
+    constexpr bool SUM_A = POST || GATE, SUM_B = LN && POST, HEAVY = LN && GATE && POST;
+    constexpr bool IN_LDS = HEAVY && MC > 1, TIGHT = HEAVY && NT > 512;
+    __shared__ float2 red[2][NT / 64];
     __shared__ __attribute__((aligned(16))) float comb[R > 1 ? R : 1][R > 1 ? W : 4];
-    RowSum<G, NT> row_sum{red_};
-    const int lane = threadIdx.x % G, grp = threadIdx.x / G, H = a.H, block = blockIdx.x;
+    __shared__ __attribute__((aligned(16))) float total_w[GATE && POST ? W : 4], total_b[GATE && SUM_B ? W : 4];
+    const int lane = threadIdx.x % G, grp = __builtin_amdgcn_readfirstlane(threadIdx.x / G), H = a.H, block = blockIdx.x;
+    RowSum<G, MC, NT> row_sum{red, H};
     const int r0 = join_row(a.T, gridDim.x, block), r1 = join_row(a.T, gridDim.x, block + 1);
     const float inv_h = 1.f / H;
-    const bool pre = a.pre != NORM_NONE, post = a.post != NORM_NONE, by_segment = GATE && a.gate == GATE_SEGMENT;
+    const bool pre = a.pre != NORM_NONE, by_segment = GATE && a.gate == GATE_SEGMENT;
     auto col = [&](int i) { return (lane + i * G) * 8; };
-    Raw8<T> pdy[MC], pdh[MC], py[MC], pb[MC], w1[MC], w2[MC], gt[GATE ? MC : 1], b2[LN && GATE ? MC : 1];
-    float s_pre_w[MC][8] = {}, s_post_w[MC][8] = {}, s_pre_b[LN ? MC : 1][8] = {}, s_post_b[LN ? MC : 1][8] = {}, s_gate[GATE ? MC : 1][8] = {};
+    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill otherwise
+    __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 2 : 1][IN_LDS ? W : 8];
+    constexpr int HELD = IN_LDS ? 1 : MC;
+    Raw8<T> pdy[MC], pdh[MC], py[MC], pb[MC], w1[HELD], w2[POST ? HELD : 1], gt[GATE ? MC : 1];
+    auto keep = [&](Raw8<T> *held, int slot, int i, const void *from) {
+        const Raw8<T> v = load_plain8((const T *)from + col(i));
+        if constexpr (IN_LDS) *reinterpret_cast<Raw8<T> *>(&parked[slot][col(i)]) = v;
+        else held[i] = v;
+    };
+    auto kept = [&](Raw8<T> *held, int slot, int i) {
+        if constexpr (IN_LDS) return *reinterpret_cast<const Raw8<T> *>(&parked[slot][col(i)]);
+        if constexpr (TIGHT) as_loaded(held[i]);
+        return held[i];
+    };
+    float s_pre_w[MC][8] = {}, s_pre_b[LN ? MC : 1][8] = {}, sum_a[MC][8] = {}, sum_b[MC][8] = {};
     float pr = 0.f, pmu = 0.f, pr2 = 0.f, pmu2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
     auto request = [&](int row, int end) {
-        const bool in = row < end;
-        pr = pmu = pr2 = pmu2 = 0.f;
-        if (in) {
-            if (pre) pr = a.pre_rstd[row];
-            if (post) pr2 = a.post_rstd[row];
-            if (LN && a.pre == NORM_LAYER) pmu = a.pre_mean[row];
-            if (LN && a.post == NORM_LAYER) pmu2 = a.post_mean[row];
+        if (row >= end) {                       // no row: adds nothing to any sum
+            pr = pmu = pr2 = pmu2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
+            return;
         }
+        if (pre) pr = a.pre_rstd[row];
+        if (POST) pr2 = a.post_rstd[row];
+        if (LN && a.pre == NORM_LAYER) pmu = a.pre_mean[row];
+        if (SUM_B && a.post == NORM_LAYER) pmu2 = a.post_mean[row];
 #pragma unroll
         for (int i = 0; i < MC; ++i) {
-            zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]);
-            if (!in || col(i) >= H) continue;
+            if (col(i) >= H) continue;          // (these lanes keep the zeros they begin with)
             const size_t at = (size_t)row * H + col(i);
             if (a.dy) load_raw8((const T *)a.dy + at, pdy[i]);
             if (pre) { load_raw8((const T *)a.dh + at, pdh[i]); load_raw8((const T *)a.y + at, py[i]); }
-            if (post || (GATE && a.b)) load_raw8((const T *)a.b + at, pb[i]);
+            if (SUM_A) load_raw8((const T *)a.b + at, pb[i]);
         }
     };
 #pragma unroll
     for (int i = 0; i < MC; ++i) {
         if (col(i) >= H) continue;
-        if (pre) w1[i] = load_plain8((const T *)a.pre_w + col(i));
-        if (post) w2[i] = load_plain8((const T *)a.post_w + col(i));
-        if (LN && GATE && a.post == NORM_LAYER) b2[i] = load_plain8((const T *)a.post_b + col(i));
+        if (pre) keep(w1, 0, i, a.pre_w);
+        if constexpr (POST) keep(w2, 1, i, a.post_w);
         if (GATE && a.gate == GATE_CHANNEL) gt[i] = load_plain8((const T *)a.gate_v + col(i));
     }
-    // the sums of the groups, added in order, handed out in quads of columns
-    auto flush = [&](const float (&v)[MC][8], auto emit) {
+    // the sums of the groups, added in order, handed out in quads of columns; always the same quads to the same thread
+    auto flush = [&](auto value, auto emit) {
         if constexpr (R == 1) {
 #pragma unroll
             for (int i = 0; i < MC; ++i)
                 if (col(i) < H) {
-                    emit(col(i), f32x4{v[i][0], v[i][1], v[i][2], v[i][3]});
-                    emit(col(i) + 4, f32x4{v[i][4], v[i][5], v[i][6], v[i][7]});
+                    float v[8];
+                    value(i, v);
+                    emit(col(i), f32x4{v[0], v[1], v[2], v[3]});
+                    emit(col(i) + 4, f32x4{v[4], v[5], v[6], v[7]});
                 }
         } else {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < MC; ++i)
-                if (col(i) < H) store8(&comb[grp][col(i)], v[i]);
+                if (col(i) < H) {
+                    float v[8];
+                    value(i, v);
+                    store8(&comb[grp][col(i)], v);
+                }
             __syncthreads();
             for (int c = threadIdx.x * 4; c < H; c += NT * 4) {
                 f32x4 s = *reinterpret_cast<const f32x4 *>(&comb[0][c]);
@@ -227,6 +323,27 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
                 emit(c, s);
             }
         }
+    };
+    auto plain = [](const float (&sum)[MC][8]) {
+        return [&sum](int i, float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = sum[i][j];
+        };
+    };
+    auto gated = [&](const float (&sum)[MC][8]) {               // beta gate sum
+        return [&](int i, float (&v)[8]) {
+            float g[8];
+            if constexpr (GATE) unpack8(gt[i], g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = a.beta * (GATE ? g[j] : 1.f) * sum[i][j];
+        };
+    };
+    auto gate_gradient = [&](int i, float (&v)[8]) {            // beta (w A + b B), or beta A
+        float w[8], o[8];
+        if constexpr (POST) unpack8(kept(w2, 1, i), w);
+        if (SUM_B && a.post == NORM_LAYER) load8((const T *)a.post_b + col(i), o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = a.beta * ((POST ? w[j] : 1.f) * sum_a[i][j] + (SUM_B && a.post == NORM_LAYER ? o[j] * sum_b[i][j] : 0.f));
     };
     auto to_part = [&](float *part, size_t row) {
         return [=](int c, f32x4 s) { *reinterpret_cast<f32x4 *>(part + row * H + c) = s; };
@@ -257,18 +374,19 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
                 for (int i = 0; i < MC; ++i) {
                     if (col(i) >= H) continue;
                     float g[8];
-                    unpack8(w1[i], g);
+                    unpack8(kept(w1, 0, i), g);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         hat[i][j] = (hat[i][j] - mu) * r;
                         s_pre_w[i][j] += back[i][j] * hat[i][j];
                         if (LN) s_pre_b[i][j] += back[i][j];
                         back[i][j] *= g[j];
-                        s0 += back[i][j];
+                        if (LN) s0 += back[i][j];
                         s1 += back[i][j] * hat[i][j];
                     }
                 }
-                row_sum(s0, s1);
+                if constexpr (LN) row_sum(s0, s1);
+                else row_sum(s1);
                 s0 = LN && a.pre == NORM_LAYER ? s0 * inv_h : 0.f;
                 s1 *= inv_h;
 #pragma unroll
@@ -286,31 +404,28 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
                 if (col(i) >= H) continue;
-                float g[8], w[8], o[8], dx[8];
+                float g[8], w[8], dx[8];
+                if constexpr (HEAVY && (MC > 1 || NT > 512)) as_loaded(gt[i]);
                 if constexpr (GATE) unpack8(gt[i], g);
-                if (post) unpack8(w2[i], w);
-                if constexpr (LN && GATE) { if (a.post == NORM_LAYER) unpack8(b2[i], o); }
+                if constexpr (POST) unpack8(kept(w2, 1, i), w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     dx[j] = a.alpha * d[i][j];
-                    const float dn = a.beta * d[i][j];
-                    float n = bv[i][j];
-                    back[i][j] = GATE ? dn * g[j] : dn;
-                    if (post) {
-                        n = hat[i][j] = (n - mu2) * r2;
-                        s_post_w[i][j] += back[i][j] * n;
-                        if (LN) s_post_b[i][j] += back[i][j];
+                    hat[i][j] = POST ? (bv[i][j] - mu2) * r2 : bv[i][j];
+                    if (SUM_A) sum_a[i][j] += d[i][j] * hat[i][j];
+                    if (SUM_B) sum_b[i][j] += d[i][j];
+                    back[i][j] = a.beta * d[i][j] * (GATE ? g[j] : 1.f);
+                    if (POST) {
                         back[i][j] *= w[j];
-                        u0 += back[i][j];
-                        u1 += back[i][j] * n;
-                        if (GATE) n = n * w[j] + (LN && a.post == NORM_LAYER ? o[j] : 0.f);
+                        if (LN) u0 += back[i][j];
+                        u1 += back[i][j] * hat[i][j];
                     }
-                    if (GATE) s_gate[i][j] += dn * n;
                 }
                 if (a.dx && valid) store8((T *)a.dx + (size_t)row * H + col(i), dx);
             }
-            if (post) {
-                row_sum(u0, u1);
+            if constexpr (POST) {
+                if constexpr (LN) row_sum(u0, u1);
+                else row_sum(u1);
                 u0 = LN && a.post == NORM_LAYER ? u0 * inv_h : 0.f;
                 u1 *= inv_h;
 #pragma unroll
@@ -323,59 +438,139 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
                 if (a.db && valid && col(i) < H) store8((T *)a.db + (size_t)row * H + col(i), back[i]);
         }
         if constexpr (GATE) {
-            if (by_segment && a.p_gate) {
-                if (a.cu[seg] >= r0 && a.cu[seg + 1] <= r1) {
-                    flush(s_gate, [&](int c, f32x4 s) {
-                        const size_t at = (size_t)seg * H + c;
+            if (by_segment) {
+                if (a.p_gate) {
+                    if (a.cu[seg] >= r0 && a.cu[seg + 1] <= r1) {
+                        flush(gate_gradient, [&](int c, f32x4 s) {
+                            const size_t at = (size_t)seg * H + c;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (a.grad_f32) ((float *)a.d_gate)[at + j] = s[j] + (a.accumulate ? ((float *)a.d_gate)[at + j] : 0.f);
-                            else Elem<T>::store((T *)a.d_gate + at + j, s[j] + (a.accumulate ? Elem<T>::load((T *)a.d_gate + at + j) : 0.f));
-                        }
-                    });
-                } else {
-                    flush(s_gate, to_part(a.p_gate, 2 * (size_t)block + (start != r0)));
+                            for (int j = 0; j < 4; ++j) {
+                                if (a.grad_f32) ((float *)a.d_gate)[at + j] = s[j] + (a.accumulate ? ((float *)a.d_gate)[at + j] : 0.f);
+                                else Elem<T>::store((T *)a.d_gate + at + j, s[j] + (a.accumulate ? Elem<T>::load((T *)a.d_gate + at + j) : 0.f));
+                            }
+                        });
+                    } else {
+                        flush(gate_gradient, to_part(a.p_gate, 2 * (size_t)block + (start != r0)));
+                    }
                 }
+                auto to_total = [&](float *total) {             // (the thread that adds a quad up also reads it at the end)
+                    return [=](int c, f32x4 s) {
+                        f32x4 *t = reinterpret_cast<f32x4 *>(total + c);
+                        *t = start == r0 ? s : *t + s;
+                    };
+                };
+                if constexpr (POST) { if (a.p_post_w) flush(gated(sum_a), to_total(total_w)); }
+                if constexpr (SUM_B) { if (a.p_post_b) flush(gated(sum_b), to_total(total_b)); }
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s_gate[i][j] = 0.f;
+                    for (int j = 0; j < 8; ++j) sum_a[i][j] = sum_b[i][j] = 0.f;
             }
         }
         start = end;
     }
-    if (a.p_pre_w) flush(s_pre_w, to_part(a.p_pre_w, block));
-    if (a.p_post_w) flush(s_post_w, to_part(a.p_post_w, block));
+    if (a.p_pre_w) flush(plain(s_pre_w), to_part(a.p_pre_w, block));
     if constexpr (LN) {
-        if (a.p_pre_b) flush(s_pre_b, to_part(a.p_pre_b, block));
-        if (a.p_post_b) flush(s_post_b, to_part(a.p_post_b, block));
+        if (a.p_pre_b) flush([&](int i, float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = s_pre_b[i][j];
+        }, to_part(a.p_pre_b, block));
+    }
+    auto from_total = [&](const float *total, float *part) {
+        auto to = to_part(part, block);
+        flush([](int, float (&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.f;
+        }, [&](int c, f32x4) { to(c, *reinterpret_cast<const f32x4 *>(total + c)); });
+    };
+    if constexpr (POST) {
+        if (a.p_post_w) {
+            if (by_segment) from_total(total_w, a.p_post_w);
+            else flush(gated(sum_a), to_part(a.p_post_w, block));
+        }
+    }
+    if constexpr (SUM_B) {
+        if (a.p_post_b) {
+            if (by_segment) from_total(total_b, a.p_post_b);
+            else flush(gated(sum_b), to_part(a.p_post_b, block));
+        }
     }
     if constexpr (GATE) {
-        if (a.p_gate && !by_segment) flush(s_gate, to_part(a.p_gate, block));
+        if (a.p_gate && !by_segment) flush(gate_gradient, to_part(a.p_gate, block));
     }
 }
 
-// The gradient of a segment's gate where several workgroups have rows of the segment: their slots, in order.  No row: zero.
-template <typename G>
-__global__ __launch_bounds__(256) void gate_segments_kernel(const float *part, const int *cu, int T, int H, int blocks, G *out, bool accumulate) {
-    const int s = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x, b0 = cu[s], b1 = cu[s + 1];
-    if (c >= H) return;
-    float sum = 0.f;
-    if (b1 > b0) {
-        // the workgroup of row t: the last one whose first row is t or before
-        auto owner = [&](int t) {
-            int b = (int)((long)t * blocks / T);
-            while (b + 1 < blocks && join_row(T, blocks, b + 1) <= t) ++b;
-            while (join_row(T, blocks, b) > t) --b;
-            return b;
-        };
-        const int first = owner(b0), last = owner(b1 - 1);
-        if (first == last) return;
-        for (int b = first; b <= last; ++b) sum += part[(size_t)(2 * b + (join_row(T, blocks, b) < b0)) * H + c];
+// What the backward kernel's workgroups leave behind, in one launch: the sums over their partial rows (reduce.h), then the gate gradients of the
+// segments that several workgroups have rows of, then the zeros of the empty segments.
+//
+// A segment of the second kind begins in the range of one workgroup and goes on behind it: thread y of each of these workgroups looks at the end of
+// workgroup y's range, the segments found are numbered in that order, and GATE_SHARES workgroups per 32 columns take them in turn.  Summed are
+// slot 1 or 0 where the segment begins and slot 0 of each further workgroup, 32 rows at a time, in a fixed order.
+constexpr int JOIN_BLOCKS = 256, GATE_SHARES = 8, GATE_EMPTY = 64;
+struct GateSums {
+    const float *part;
+    void *out;                      // null: no segment gates
+    const int *cu;
+    int S, T, H, blocks, accumulate;
+};
+template <typename E>
+__global__ __launch_bounds__(256) void join_sums_kernel(ReduceJobSet set, GateSums g) {
+    __shared__ __attribute__((aligned(16))) float red[32][36];
+    __shared__ int4 found[JOIN_BLOCKS];                     // segment, slot it begins in, first and last workgroup that goes on
+    __shared__ int waves[4];
+    const int units = set.units[8], tid = threadIdx.x;
+    if ((int)blockIdx.x < units) return reduce_unit<E>(set, blockIdx.x, red, tid);
+    const int columns = (g.H + 31) / 32, k = (int)blockIdx.x - units, c0 = k % columns * 32, share = k / columns;
+    const int cl = tid & 7, rl = tid >> 3, c = c0 + cl * 4;
+    E *out = (E *)g.out;
+    if (share >= GATE_SHARES) {
+        const int first = (share - GATE_SHARES) * GATE_EMPTY;
+        for (int s = first + rl; s < min(first + GATE_EMPTY, g.S); s += 32)
+            if (g.cu[s + 1] == g.cu[s] && c < g.H && !g.accumulate) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) Elem<E>::store(out + (size_t)s * g.H + c + j, 0.f);
+            }
+        return;
     }
-    const size_t at = (size_t)s * H + c;
-    if (accumulate) sum += Elem<G>::load(out + at);
-    Elem<G>::store(out + at, sum);
+    bool goes_on = false;
+    int4 mine = {};
+    if (tid < g.blocks) {
+        const int r0 = join_row(g.T, g.blocks, tid), r1 = join_row(g.T, g.blocks, tid + 1);
+        const int s = find_segment(g.cu, g.S, r1 - 1), b0 = g.cu[s], b1 = g.cu[s + 1];
+        goes_on = b0 >= r0 && b1 > r1;
+        const int q = g.T / g.blocks, longer = g.T % g.blocks, t = b1 - 1;      // the workgroup of row t
+        mine = make_int4(s, 2 * tid + (b0 > r0), tid + 1, t < longer * (q + 1) ? t / (q + 1) : longer + (t - longer * (q + 1)) / q);
+    }
+    const unsigned long long set_lanes = __ballot(goes_on);
+    if ((tid & 63) == 0) waves[tid >> 6] = __popcll(set_lanes);
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < tid >> 6) before += waves[w];
+        all += waves[w];
+    }
+    if (goes_on) found[before + __popcll(set_lanes & ((1ull << (tid & 63)) - 1))] = mine;
+    __syncthreads();
+    for (int i = share; i < all; i += GATE_SHARES) {
+        const int4 f = found[i];
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (c < g.H) {
+            if (rl == 0) sum = *reinterpret_cast<const f32x4 *>(g.part + (size_t)f.y * g.H + c);
+            for (int b = f.z + rl; b <= f.w; b += 32) sum += *reinterpret_cast<const f32x4 *>(g.part + (size_t)(2 * b) * g.H + c);
+        }
+        __syncthreads();
+        *reinterpret_cast<f32x4 *>(&red[rl][cl * 4]) = sum;
+        __syncthreads();
+        if (tid < 32 && c0 + tid < g.H) {
+            float t = 0.f;
+#pragma unroll
+            for (int r = 0; r < 32; ++r) t += red[r][tid];
+            E *o = out + (size_t)f.x * g.H + c0 + tid;
+            if (g.accumulate) t += Elem<E>::load(o);
+            Elem<E>::store(o, t);
+        }
+    }
 }
 
 template <typename T, int G, int MC, int NT, bool LN>
@@ -392,34 +587,37 @@ hipError_t launch_fwd(const JoinArgs &a, hipStream_t st) {
 
 template <typename T, int G, int MC, int NT>
 hipError_t launch_bwd(const JoinArgs &a, hipStream_t st) {
-    const bool ln = a.post == NORM_LAYER || a.pre == NORM_LAYER, gate = a.gate != GATE_NONE;
     const int blocks = join_bwd_blocks(a.T, a.H);
-    if (ln && gate) join_bwd_kernel<T, G, MC, NT, true, true><<<blocks, NT, 0, st>>>(a);
-    else if (ln) join_bwd_kernel<T, G, MC, NT, true, false><<<blocks, NT, 0, st>>>(a);
-    else if (gate) join_bwd_kernel<T, G, MC, NT, false, true><<<blocks, NT, 0, st>>>(a);
-    else join_bwd_kernel<T, G, MC, NT, false, false><<<blocks, NT, 0, st>>>(a);
+    auto go = [&](auto LN, auto GATE, auto POST) { join_bwd_kernel<T, G, MC, NT, decltype(LN)::value, decltype(GATE)::value, decltype(POST)::value><<<blocks, NT, 0, st>>>(a); };
+    auto with = [&](bool v, auto f) { if (v) f(std::true_type{}); else f(std::false_type{}); };
+    with(a.post == NORM_LAYER || a.pre == NORM_LAYER, [&](auto LN) {
+        with(a.gate != GATE_NONE, [&](auto GATE) { with(a.post != NORM_NONE, [&](auto POST) { go(LN, GATE, POST); }); });
+    });
     return hipGetLastError();
 }
 
 // by width: (threads a row, chunks a thread, threads a workgroup)
-constexpr int BWD_ROWS_WAVE = 4, BWD_ROWS_WIDE = 2;
 template <typename T>
 hipError_t fwd_by_width(const JoinArgs &a, hipStream_t st) {
     const bool ln = a.post == NORM_LAYER || a.pre == NORM_LAYER;
 #define L(G, MC, NT) return ln ? launch_fwd<T, G, MC, NT, true>(a, st) : launch_fwd<T, G, MC, NT, false>(a, st)
-    if (a.H <= 512) L(64, 1, 256);
-    if (a.H <= 1024) L(64, 2, 256);
-    if (a.H <= 2048) L(256, 1, 256);
-    if (a.H <= 4096) L(256, 2, 256);
+    if (a.H <= 64 * 8) L(64, 1, 256);
+    if (a.H <= 128 * 8) L(64, 2, 256);
+    if (a.H <= 192 * 8) L(192, 1, 192);
+    if (a.H <= 256 * 8) L(256, 1, 256);
+    if (a.H <= 512 * 8) L(256, 2, 256);
+    if (a.H <= 640 * 8) L(320, 2, 320);
     L(512, 2, 512);
 #undef L
 }
 template <typename T>
 hipError_t bwd_by_width(const JoinArgs &a, hipStream_t st) {
-    if (a.H <= 512) return launch_bwd<T, 64, 1, 64 * BWD_ROWS_WAVE>(a, st);
-    if (a.H <= 1024) return launch_bwd<T, 64, 2, 64 * BWD_ROWS_WAVE>(a, st);
-    if (a.H <= 2048) return launch_bwd<T, 256, 1, 256 * BWD_ROWS_WIDE>(a, st);
-    if (a.H <= 4096) return launch_bwd<T, 256, 2, 256 * BWD_ROWS_WIDE>(a, st);
+    if (a.H <= 64 * 8) return launch_bwd<T, 64, 1, 512>(a, st);
+    if (a.H <= 128 * 8) return launch_bwd<T, 128, 1, 768>(a, st);
+    if (a.H <= 192 * 8) return launch_bwd<T, 192, 1, 768>(a, st);
+    if (a.H <= 256 * 8) return launch_bwd<T, 256, 1, 768>(a, st);
+    if (a.H <= 512 * 8) return launch_bwd<T, 512, 1, 512>(a, st);
+    if (a.H <= 640 * 8) return launch_bwd<T, 640, 1, 640>(a, st);
     return launch_bwd<T, 512, 2, 512>(a, st);
 }
 
@@ -430,9 +628,10 @@ hipError_t join_fwd(int dtype, const JoinArgs &a, hipStream_t st) {
     return dtype == DT_F32 ? fwd_by_width<float>(a, st) : fwd_by_width<bf16_t>(a, st);
 }
 
+// as many as there are rows at a time, at most one per compute unit
 int join_bwd_blocks(int T, int H) {
-    const int all = H <= 1024 ? ceil_div(T, BWD_ROWS_WAVE) : H <= 4096 ? ceil_div(T, BWD_ROWS_WIDE) : T;
-    return all < 512 ? all : 512;
+    const int at_once = H <= 64 * 8 ? 8 : H <= 128 * 8 ? 6 : H <= 192 * 8 ? 4 : H <= 256 * 8 ? 3 : 1;
+    return std::min(ceil_div(T, at_once), JOIN_BLOCKS);
 }
 
 hipError_t join_bwd(int dtype, const JoinArgs &a, hipStream_t st) {
@@ -441,13 +640,16 @@ hipError_t join_bwd(int dtype, const JoinArgs &a, hipStream_t st) {
         const hipError_t e = dtype == DT_F32 ? bwd_by_width<float>(a, st) : bwd_by_width<bf16_t>(a, st);
         if (e != hipSuccess) return e;
     }
-    if (a.gate != GATE_SEGMENT || !a.d_gate || a.S == 0) return hipSuccess;
-    for (int s = 0; s < a.S; s += 65535) {          // a grid's second dimension ends there
-        const dim3 grid(ceil_div(a.H, 256), a.S - s < 65535 ? a.S - s : 65535);
-        const size_t at = (size_t)s * a.H;
-        if (a.grad_f32) gate_segments_kernel<float><<<grid, 256, 0, st>>>(a.p_gate, a.cu + s, a.T, a.H, blocks, (float *)a.d_gate + at, a.accumulate);
-        else gate_segments_kernel<bf16_t><<<grid, 256, 0, st>>>(a.p_gate, a.cu + s, a.T, a.H, blocks, (bf16_t *)a.d_gate + at, a.accumulate);
-    }
+    const bool by_segment = a.gate == GATE_SEGMENT && a.d_gate && a.S > 0;
+    const ReduceJob jobs[5] = {{a.p_post_w, a.d_post_w, blocks, a.H}, {a.p_post_b, a.d_post_b, blocks, a.H}, {a.p_pre_w, a.d_pre_w, blocks, a.H},
+                               {a.p_pre_b, a.d_pre_b, blocks, a.H}, {a.gate == GATE_CHANNEL ? a.p_gate : nullptr, a.d_gate, blocks, a.H}};
+    ReduceJobSet set;
+    reduce_job_set(jobs, 5, a.accumulate, set);
+    const GateSums g = {a.p_gate, by_segment ? a.d_gate : nullptr, a.cu, a.S, a.T, a.H, blocks, a.accumulate};
+    const int grid = set.units[8] + (by_segment ? ceil_div(a.H, 32) * (GATE_SHARES + ceil_div(a.S, GATE_EMPTY)) : 0);
+    if (grid == 0) return hipSuccess;
+    if (a.grad_f32) join_sums_kernel<float><<<grid, 256, 0, st>>>(set, g);
+    else join_sums_kernel<bf16_t><<<grid, 256, 0, st>>>(set, g);
     return hipGetLastError();
 }
 
