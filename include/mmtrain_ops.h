@@ -127,7 +127,7 @@ MMTRAIN_API int mmtrain_residual_norm_bwd(const mmtrain_residual_norm_desc *desc
 typedef struct {
     const void *grad;               /* device, [n], 16-byte aligned */
     void *out;                      /* device, [n], 16-byte aligned: where the clipped gradient goes; NULL or grad: in place */
-    int64_t n;                      /* >= 0 */
+    int64_t n;                      /* 0 .. 2^36 (more: MMTRAIN_ERR_UNSUPPORTED) */
     int32_t dtype, out_dtype;       /* mmtrain_dtype; in place they have to be the same */
 } mmtrain_grad_tensor;
 

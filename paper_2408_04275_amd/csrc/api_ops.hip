@@ -94,11 +94,13 @@ size_t join_parts(const mmtrain_residual_norm_desc &d, int32_t T, uint8_t *base,
 }
 
 // ---- gradient norm and clipping -----------------------------------------------------------
+constexpr int64_t GRAD_MAX_ELEMENTS = (int64_t)1 << 36;          // a tensor: chunks of a batch are counted in 32 bits
+
 int check_tensors(const mmtrain_grad_tensor *t, int32_t n, bool clip) {
     if (n < 0 || (n > 0 && !t)) return MMTRAIN_ERR_INVALID_ARG;
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].n < 0 || !is_dtype(t[i].dtype)) return MMTRAIN_ERR_INVALID_ARG;
-        if (t[i].n > (int64_t)1 << 40) return MMTRAIN_ERR_UNSUPPORTED;
+        if (t[i].n > GRAD_MAX_ELEMENTS) return MMTRAIN_ERR_UNSUPPORTED;
         if (t[i].n > 0 && !t[i].grad) return MMTRAIN_ERR_INVALID_ARG;
         if (misaligned({t[i].grad})) return MMTRAIN_ERR_INVALID_ARG;
         if (!clip || !t[i].out) continue;
@@ -132,24 +134,21 @@ template <typename F>
 int for_batches(const mmtrain_grad_tensor *t, int32_t n, F launch) {
     GradBatch b;
     b.count = 0;
-    long chunks = 0;
-    for (int32_t i = 0; i < n; ++i) {
-        if (t[i].n == 0) continue;
-        const long more = (long)((t[i].n + GRAD_CHUNK - 1) / GRAD_CHUNK);
-        if (b.count == GRAD_BATCH || (b.count && chunks + more > 0x3fffffff)) {
-            b.first[b.count] = (int)chunks;
-            HIP_TRY(launch(b));
-            b.count = 0; chunks = 0;
-        }
-        const int k = b.count++;
-        b.in[k] = t[i].grad; b.out[k] = t[i].out ? t[i].out : const_cast<void *>(t[i].grad);
-        b.n[k] = t[i].n; b.first[k] = (int)chunks;
-        b.in_f32[k] = t[i].dtype == MMTRAIN_F32;
-        b.out_f32[k] = (t[i].out ? t[i].out_dtype : t[i].dtype) == MMTRAIN_F32;
-        chunks += more;
+    for (int32_t k = 0; k < n; ++k) {
+        const mmtrain_grad_tensor &g = t[k];
+        if (g.n == 0) continue;
+        const int i = b.count++;
+        b.in[i] = g.grad; b.out[i] = g.out ? g.out : const_cast<void *>(g.grad);
+        b.n[i] = g.n;
+        b.in_f32[i] = g.dtype == MMTRAIN_F32;
+        b.out_f32[i] = (g.out ? g.out_dtype : g.dtype) == MMTRAIN_F32;
+        if (b.count < GRAD_BATCH) continue;
+        grad_chunks(b);
+        HIP_TRY(launch(b));
+        b.count = 0;
     }
     if (b.count) {
-        b.first[b.count] = (int)chunks;
+        grad_chunks(b);
         HIP_TRY(launch(b));
     }
     return MMTRAIN_OK;
@@ -299,8 +298,10 @@ int mmtrain_grad_clip(const mmtrain_grad_tensor *tensors, int32_t n_tensors, con
     } catch (...) {                             // no host memory for the list of ranges
         return MMTRAIN_ERR_HIP;
     }
+    size_t written = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) written += (size_t)tensors[i].n * ((tensors[i].out ? tensors[i].out_dtype : tensors[i].dtype) == MMTRAIN_F32 ? 4 : 2);
     return for_batches(tensors, n_tensors, [&](const GradBatch &b) {
-        return grad_clip(b, reinterpret_cast<const GradResult *>(result), (hipStream_t)hip_stream);
+        return grad_clip(b, reinterpret_cast<const GradResult *>(result), grad_clip_streams(written), (hipStream_t)hip_stream);
     });
 }
 

@@ -52,14 +52,16 @@ struct GradBatch {
     long n[GRAD_BATCH];
     int first[GRAD_BATCH + 1];      // first chunk of each tensor; [count] = all
     unsigned char in_f32[GRAD_BATCH], out_f32[GRAD_BATCH];
-    int count;
+    int count, chunk;               // elements a chunk, a multiple of 8
 };
-constexpr int GRAD_CHUNK = 16384;   // elements
-constexpr int GRAD_BLOCKS = 1024;   // partial sums a launch leaves at most
+constexpr int GRAD_BLOCKS = 2048;   // workgroups, and partial sums, of a launch at most: eight of 256 threads on each compute unit
 struct GradResult { double sum_sq; float norm, factor; };
+// Cuts a batch whose in, out, n, types and count are set into chunks (first, chunk)
+void grad_chunks(GradBatch &b);
 int grad_norm_blocks(const GradBatch &b);
 hipError_t grad_sum_sq(const GradBatch &b, double *part, hipStream_t st);
 hipError_t grad_norm_finish(const double *part, int n, float max_norm, bool add, GradResult *result, hipStream_t st);
-hipError_t grad_clip(const GradBatch &b, const GradResult *result, hipStream_t st);
+bool grad_clip_streams(size_t bytes_written);       // by a whole call
+hipError_t grad_clip(const GradBatch &b, const GradResult *result, bool stream, hipStream_t st);
 
 }  // namespace mmt

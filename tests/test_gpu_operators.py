@@ -404,3 +404,19 @@ def test_clipped_adam_is_adam_on_clipped_gradients(n, zero, max_norm):
                                        mm.BF16, result), "adam")
     assert all(torch.equal(a, b) for a, b in zip(state, other)) and torch.equal(p, q)
     assert bool(torch.all(g == 0)) == zero
+
+
+@pytest.mark.parametrize("from_dtype,to_dtype", [(mm.BF16, mm.F32), (mm.F32, mm.BF16), (mm.F32, None)])
+def test_grad_clip_of_more_than_the_caches_hold(from_dtype, to_dtype):
+    # 384 MB and more are written: streamed
+    n = (100 << 20) + 5 if to_dtype != mm.BF16 else (200 << 20) + 5
+    g = torch.randn(n, device="cuda").to(torch_dtype(from_dtype))
+    out = None if to_dtype is None else torch.full((n + 8,), 7.0, dtype=torch_dtype(to_dtype), device="cuda")
+    before = g.clone()
+    tensors = mm.make_grad_tensors([g, g[:0]], None if out is None else [out[:n], out[n:n]])
+    result, _, norm, factor = norm_of(tensors, 2, 1.0)
+    assert np.isclose(norm, float(torch.linalg.vector_norm(before, dtype=torch.float64)), rtol=1e-6)
+    check(mm.mmtrain_grad_clip(tensors, result), "clip")
+    got = g if out is None else out[:n]
+    want = (before.float() * result.view(torch.float32)[3]).to(got.dtype)      # one fp32 product, one rounding
+    assert torch.equal(got, want) and (out is None or torch.all(out[n:] == 7.0))
