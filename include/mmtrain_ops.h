@@ -39,9 +39,9 @@ typedef enum { MMTRAIN_ROPE_PLAIN = 0, MMTRAIN_ROPE_LINEAR = 1, MMTRAIN_ROPE_WAV
 typedef struct {
     uint32_t struct_size;           /* sizeof(mmtrain_rope_desc) */
     int32_t dtype;                  /* mmtrain_dtype of x and y */
-    int32_t n_heads;                /* heads that are rotated */
+    int32_t n_heads;                /* heads that are rotated, 1 .. 65536 */
     int32_t head_dim;               /* 2 .. 256 */
-    int32_t rot_dim;                /* even, 2 .. head_dim */
+    int32_t rot_dim;                /* even, 2 .. head_dim (an odd one, or more heads or features: MMTRAIN_ERR_UNSUPPORTED) */
     int32_t layout;                 /* mmtrain_rope_layout */
     int32_t scaling;                /* mmtrain_rope_scaling */
     float base;                     /* > 1 */

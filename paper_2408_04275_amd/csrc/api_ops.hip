@@ -165,7 +165,7 @@ int mmtrain_rope(const mmtrain_rope_desc *desc, int32_t n_tokens, const mmtrain_
     if (desc->scaling < MMTRAIN_ROPE_PLAIN || desc->scaling > MMTRAIN_ROPE_RAMP) return MMTRAIN_ERR_INVALID_ARG;
     if (desc->n_heads <= 0 || desc->head_dim <= 0 || desc->rot_dim <= 0 || desc->rot_dim > desc->head_dim) return MMTRAIN_ERR_INVALID_ARG;
     if (!(desc->base > 1.f && std::isfinite(desc->base)) || !(desc->magnitude >= 0.f && std::isfinite(desc->magnitude))) return MMTRAIN_ERR_INVALID_ARG;
-    if (desc->rot_dim % 2 || desc->head_dim > 2 * ROPE_MAX_HALF) return MMTRAIN_ERR_UNSUPPORTED;
+    if (desc->rot_dim % 2 || desc->head_dim > 2 * ROPE_MAX_HALF || desc->n_heads > ROPE_MAX_HEADS) return MMTRAIN_ERR_UNSUPPORTED;
     RopeArgs a = {};
     a.half = desc->rot_dim / 2;
     int rc = rope_turns(*desc, a);

@@ -5,7 +5,7 @@
 namespace mmt {
 
 // rope.hip.  turns[i] = frequency of pair i in turns per position.
-constexpr int ROPE_MAX_HALF = 128;
+constexpr int ROPE_MAX_HALF = 128, ROPE_MAX_HEADS = 1 << 16;
 struct RopeArgs {
     int T, heads, d, half;          // half = rot_dim / 2
     bool interleaved;

@@ -19,6 +19,18 @@ namespace {
 // first row of workgroup b: the first T % blocks workgroups have one row more
 __device__ __forceinline__ int join_row(int T, int blocks, int b) { return b * (T / blocks) + min(b, T % blocks); }
 
+// find_segment for a token that is the same in all lanes: 64 boundaries are looked at together, so up to 64 segments take one load's time instead of
+// one per halving
+__device__ __forceinline__ int find_segment_wave(const int *cu, int S, int t) {
+    int lo = 0, hi = S;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, at = lo + (int)(threadIdx.x & 63) * step;
+        lo += (__popcll(__ballot(at < hi && cu[min(at, S)] <= t)) - 1) * step;         // (cu[lo] <= t always)
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
 // Sum over the wavefront, the same in all lanes.  Lanes are added with DPP moves, which stay in the vector ALU: with shuffles, each of which
 // goes through the LDS unit, a row's sums were a chain of 6 x 100 clocks.  Quads, half rows and rows of 16 lanes are folded by permutations,
 // then rows 0 and 2 are added to 1 and 3, and row 1 to 3.
@@ -187,7 +199,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
         request(row + R);
         if (a.b) {
             if (a.gate == GATE_SEGMENT && valid && row >= seg_end) {
-                const int seg = find_segment(a.cu, a.S, row);
+                const int seg = find_segment_wave(a.cu, a.S, row);
                 seg_end = a.cu[seg + 1];
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
@@ -240,7 +252,7 @@ template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     constexpr int R = NT / G, W = G * MC * 8;
     constexpr bool SUM_A = POST || GATE, SUM_B = LN && POST, HEAVY = LN && GATE && POST;
-    constexpr bool IN_LDS = HEAVY && MC > 1, TIGHT = HEAVY && NT > 512;
+    constexpr bool IN_LDS = LN && POST && MC > 1 && (GATE || sizeof(T) == 4), TIGHT = HEAVY && NT > 512;
     __shared__ float2 red[2][NT / 64];
     __shared__ __attribute__((aligned(16))) float comb[R > 1 ? R : 1][R > 1 ? W : 4];
     __shared__ __attribute__((aligned(16))) float total_w[GATE && POST ? W : 4], total_b[GATE && SUM_B ? W : 4];
@@ -268,13 +280,13 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     float pr = 0.f, pmu = 0.f, pr2 = 0.f, pmu2 = 0.f;
 #pragma unroll
     for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
-    auto request = [&](int row, int end) {
-        if (row >= end) {                       // no row: adds nothing to any sum
-            pr = pmu = pr2 = pmu2 = 0.f;
+    auto forget = [&] {                         // no row: adds nothing to any sum
+        pr = pmu = pr2 = pmu2 = 0.f;
 #pragma unroll
-            for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
-            return;
-        }
+        for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
+    };
+    auto request = [&](int row, int end) {
+        if (row >= end) return forget();
         if (pre) pr = a.pre_rstd[row];
         if (POST) pr2 = a.post_rstd[row];
         if (LN && a.pre == NORM_LAYER) pmu = a.pre_mean[row];
@@ -348,18 +360,19 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     auto to_part = [&](float *part, size_t row) {
         return [=](int c, f32x4 s) { *reinterpret_cast<f32x4 *>(part + row * H + c) = s; };
     };
-    for (int start = r0; start < r1;) {
+    request(r0 + grp, r1);
+    for (int start = r0; start < r1;) {                     // start + grp is requested
         int end = r1, seg = 0;
         if constexpr (GATE) {
             if (by_segment) {
-                seg = find_segment(a.cu, a.S, start);
+                seg = find_segment_wave(a.cu, a.S, start);
                 end = min(r1, a.cu[seg + 1]);
+                if (start + grp >= end) forget();           // a row of the next segment: requested again in its turn
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
                     if (col(i) < H) gt[i] = load_plain8((const T *)a.gate_v + (size_t)seg * H + col(i));
             }
         }
-        request(start + grp, end);
         for (int base = start; base < end; base += R) {
             const int row = base + grp;
             const bool valid = row < end;
@@ -367,7 +380,8 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
             float d[MC][8], back[MC][8], hat[MC][8], bv[MC][8];
 #pragma unroll
             for (int i = 0; i < MC; ++i) { unpack8(pdy[i], d[i]); unpack8(pdh[i], back[i]); unpack8(py[i], hat[i]); unpack8(pb[i], bv[i]); }
-            request(row + R, end);
+            const bool more = base + R < end;
+            request(more ? row + R : end + grp, more ? end : r1);
             if (pre) {
                 float s0 = 0.f, s1 = 0.f;
 #pragma unroll

@@ -4,7 +4,11 @@
 // workgroup takes whole tokens: its threads first put the rotations of its tokens into LDS (an angle in fp64 each, reduced to a
 // turn, then sine and cosine in fp32), the data of their first heads already on its way, and then walk over the heads in chunks of up to 16
 // bytes.  No table in memory, no launch before this one.
+// bf16, out of HBM: 8192 tokens of 64 heads of 128 in place 55 us (4.8 TB/s), 16411 of 72 heads, 64 of 128 features interleaved, out of place 115 us
+// (5.3 TB/s).  Streaming accesses would save a tenth of the first (50 us) and cost others up to a half (80-wide fp32 heads 16 -> 27 us): they pay only where a
+// wavefront covers whole lines, and the products that read the result next find less of it in the caches.
 #include "ops.h"
+#include <algorithm>
 
 namespace mmt {
 namespace {
@@ -43,17 +47,20 @@ struct RopeShape {
     int step_tokens, step_heads;// group = step_tokens * heads + step_heads
 };
 
-// A unit is two chunks of V elements: the two halves of V pairs, or 2 V features that pass through (of which the last unit may have V).
+// A unit is two chunks of V elements, and neighbouring threads' first (and second) chunks are neighbours in memory: features u V.. and half + u V.. of
+// the rotated part -- V whole pairs in either layout, but for single features of interleaved pairs -- or, of the features that pass through,
+// chunks k and k + their units (the last unit may have the first alone).
 template <typename T, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_heads_kernel(RopeArgs a, RopeShape s) {
     extern __shared__ float2 turned[];                       // [tile][half]: cosine, sine
     const int t0 = blockIdx.x * s.tile, tokens = min(s.tile, a.T - t0);
     const int u = threadIdx.x % s.units, g = threadIdx.x / s.units;
     const bool rotates = u < s.rot_units;
-    const int pair = u * V, copied = 2 * (u - s.rot_units);
-    const int o0 = rotates ? (INTERLEAVED ? 2 * pair : pair) : 2 * a.half + copied * V;
-    const int o1 = rotates ? (INTERLEAVED ? 2 * pair + V : pair + a.half) : o0 + V;
-    const bool second = rotates || copied + 1 < s.copy_chunks;
+    constexpr bool SINGLE = INTERLEAVED && V == 1;
+    const int copy = u - s.rot_units, copy_units = s.units - s.rot_units;
+    const int o0 = rotates ? (SINGLE ? 2 * u : u * V) : 2 * a.half + copy * V;
+    const int o1 = rotates ? (SINGLE ? o0 + 1 : o0 + a.half) : o0 + copy_units * V;
+    const bool second = rotates || copy + copy_units < s.copy_chunks;
     int tok = g / a.heads, head = g % a.heads;
     const bool active = g < s.group;
     Chunk<T, V> c0, c1;
@@ -75,25 +82,30 @@ __global__ __launch_bounds__(256) void rope_heads_kernel(RopeArgs a, RopeShape s
     if (!active) return;
     while (tok < tokens) {
         T *y = (T *)a.y + (t0 + tok) * a.ldy + (long)head * a.d;
-        const float2 *cs = turned + tok * a.half + pair;
+        const float2 *cs = turned + tok * a.half;
         Chunk<T, V> d0 = c0, d1 = c1;
         tok += s.step_tokens; head += s.step_heads;
         if (head >= a.heads) { head -= a.heads; ++tok; }
         if (tok < tokens) request();
         if (rotates) {
-            float v[2 * V], w[2 * V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) { v[i] = d0.get(i); v[V + i] = d1.get(i); }
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int i0 = INTERLEAVED ? 2 * i : i, i1 = INTERLEAVED ? 2 * i + 1 : V + i;
-                const float2 r = cs[i];
-                w[i0] = v[i0] * r.x - v[i1] * r.y;
-                w[i1] = v[i1] * r.x + v[i0] * r.y;
-            }
             float lo[V], hi[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) { lo[i] = w[i]; hi[i] = w[V + i]; }
+            for (int i = 0; i < V; ++i) { lo[i] = d0.get(i); hi[i] = d1.get(i); }
+            auto turn = [](float &p, float &q, float2 r) {
+                const float v = p;
+                p = v * r.x - q * r.y;
+                q = q * r.x + v * r.y;
+            };
+            if constexpr (INTERLEAVED && !SINGLE) {
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    turn(lo[i], lo[i + 1], cs[(o0 + i) / 2]);
+                    turn(hi[i], hi[i + 1], cs[(o1 + i) / 2]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) turn(lo[i], hi[i], cs[u * V + i]);
+            }
             d0.set(lo); d1.set(hi);
         }
         d0.store(y + o0);
@@ -110,9 +122,11 @@ hipError_t launch(const RopeArgs &a, hipStream_t st) {
     s.group = 256 / s.units;
     s.step_tokens = s.group / a.heads;
     s.step_heads = s.group % a.heads;
-    // Tokens a workgroup: one angle per thread, and enough workgroups for the chip
-    const int by_angles = a.half < 256 ? 256 / a.half : 1, by_tokens = a.T / 2048;
-    s.tile = by_tokens < 1 ? 1 : by_tokens < by_angles ? by_tokens : by_angles;
+    // Tokens a workgroup: two units a thread, and not so many that a short call leaves the chip idle or that LDS fills up.  More tokens share nothing but
+    // the start: 16411 tokens of 72 heads, 8 -> 1 a workgroup 133 -> 115 us; fewer leave threads without work (12000 tokens of 12 heads, 20 features each,
+    // 5 -> 1 10.5 -> 15.6 us).
+    const int by_units = (511 + a.heads * s.units) / (a.heads * s.units), by_angles = 1024 / a.half, by_tokens = a.T / 512;
+    s.tile = std::max(1, std::min({by_units, by_angles, by_tokens}));
     const size_t lds = (size_t)s.tile * a.half * sizeof(float2);
     const int blocks = ceil_div(a.T, s.tile);
     if (a.interleaved) rope_heads_kernel<T, V, true><<<blocks, 256, lds, st>>>(a, s);

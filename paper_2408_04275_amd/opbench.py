@@ -1,7 +1,10 @@
-"""Operator microbenchmarks through the C-ABI: time one GEMM or one attention call in isolation.
+"""Operator microbenchmarks through the C-ABI: time one operator in isolation.
 
     python -m paper_2408_04275_amd.opbench gemm --layout nt --m 8192 --n 22016 --k 4096 [--iters 20]
     python -m paper_2408_04275_amd.opbench attn --config 3 [--iters 20]
+    python -m paper_2408_04275_amd.opbench rope --config 3 [--interleaved] [--rot 64]
+    python -m paper_2408_04275_amd.opbench join --config 3 [--post rms] [--pre rms] [--gate none]
+    python -m paper_2408_04275_amd.opbench clip --config 3 --layers 1 [--dtype f32]
     python -m paper_2408_04275_amd.opbench copy --mb 512          (a plain copy kernel, for counter calibration)
 
 Prints one JSON line per run.  Meant to be run alone or under rocprofv3 (kernel trace or --pmc).
@@ -106,6 +109,75 @@ def bench_adam(a):
                       "frac_of_8TBps": nbytes / ms / 1e6 / 8000.0}))
 
 
+def _segments(config):
+    return wl.make_segments(config, wl.longtail_seed() if config == 4 else 0)[0]
+
+
+def bench_rope(a):
+    """Query and key heads of a workload's packed qkv: positions applied in place, and their gradient."""
+    shape, cu = wl.SHAPES[a.config], _segments(a.config)
+    T, heads = int(cu[-1]), shape.n_heads + shape.n_kv_heads
+    batch = mm.PackedBatch.on_device(cu)
+    desc = mm.make_rope_desc(mm.BF16, heads, shape.head_dim, a.rot, mm.ROPE_INTERLEAVED if a.interleaved else mm.ROPE_HALF)
+    qkv = torch.randn((T, shape.nqkv), device="cuda").to(torch.bfloat16)
+    out = {"op": "rope", "config": a.config, "T": T, "heads": heads, "head_dim": shape.head_dim, "rot_dim": desc.rot_dim, "interleaved": a.interleaved}
+    for name, flags in (("fwd", 0), ("gradient", mm.ROPE_GRADIENT)):
+        ms = _time(lambda: check(mm.mmtrain_rope(desc, T, batch, None, qkv, shape.nqkv, qkv, shape.nqkv, flags), "rope"), a.iters)
+        out[name + "_ms"], out[name + "_GBps"] = ms, 4 * T * heads * desc.rot_dim / ms / 1e6
+    print(json.dumps(out))
+
+
+def bench_join(a):
+    """The join of a workload's branch with its residual stream, forward and backward with every gradient."""
+    shape, cu = wl.SHAPES[a.config], _segments(a.config)
+    T, H = int(cu[-1]), shape.hidden
+    norms = {"none": mm.NORM_NONE, "rms": mm.NORM_RMS, "layer": mm.NORM_LAYER}
+    gates = {"none": mm.GATE_NONE, "channel": mm.GATE_CHANNEL, "segment": mm.GATE_SEGMENT}
+    desc = mm.make_residual_norm_desc(mm.BF16, H, norms[a.post], norms[a.pre], gates[a.gate])
+    batch = mm.PackedBatch.on_device(cu)
+    names = [n + "_w" for n in ("post", "pre") if getattr(a, n) != "none"] + [n + "_b" for n in ("post", "pre") if getattr(a, n) == "layer"]
+    w = {k: torch.ones(H, device="cuda", dtype=torch.bfloat16) for k in names}
+    if a.gate != "none":
+        w["gate"] = torch.ones((len(cu) - 1, H) if a.gate == "segment" else (H,), device="cuda", dtype=torch.bfloat16)
+    x, b, dy, dh, y, h, dx, db = (torch.randn((T, H), device="cuda").to(torch.bfloat16) for _ in range(8))
+    keep = {k: torch.empty(T, device="cuda") for k in mm.RESIDUAL_NORM_STATS}
+    st = mm.make_residual_norm_stats(keep)
+    grads = {k: torch.empty_like(v) for k, v in w.items()}
+    wsb = mm.mmtrain_residual_norm_workspace_bytes(desc, T)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    cw, cg, pre = mm.make_residual_norm_weights(w), mm.make_residual_norm_grads(grads), a.pre != "none"
+    ms_f = _time(lambda: check(mm.mmtrain_residual_norm_fwd(desc, T, batch, cw, x, b, y, h if pre else None, st), "join fwd"), a.iters)
+    ms_b = _time(lambda: check(mm.mmtrain_residual_norm_bwd(desc, T, batch, cw, y, b, st, dy, dh if pre else None, dx, db, cg, 0, ws, wsb), "join bwd"), a.iters)
+    bytes_f = 2 * T * H * (4 if pre else 3)
+    bytes_b = 2 * T * H * (2 + 1 + 2 * pre + (a.post != "none" or a.gate != "none"))
+    print(json.dumps({"op": "join", "config": a.config, "T": T, "hidden": H, "post": a.post, "pre": a.pre, "gate": a.gate, "fwd_ms": ms_f, "bwd_ms": ms_b,
+                      "fwd_GBps": bytes_f / ms_f / 1e6, "bwd_GBps": bytes_b / ms_b / 1e6}))
+
+
+def bench_clip(a):
+    """Norm of the gradients of a workload's layers, their clipping in place and, from fp32, the clipped optimizer step instead."""
+    dtype = torch.float32 if a.dtype == "f32" else torch.bfloat16
+    sizes = [int(np.prod(s)) for s in wl.weight_shapes(wl.SHAPES[a.config]).values()] * a.layers
+    at = np.concatenate([[0], np.cumsum([-(-n // 8) * 8 for n in sizes])])
+    n = int(at[-1])
+    flat = torch.randn(n, device="cuda").to(dtype)
+    tensors = mm.make_grad_tensors([flat[int(p):int(p) + k] for p, k in zip(at, sizes)])
+    wsb = mm.mmtrain_grad_norm_workspace_bytes(len(sizes))
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    result = torch.zeros(2, dtype=torch.float64, device="cuda")
+    ms_n = _time(lambda: check(mm.mmtrain_grad_norm(tensors, 1.0, result, ws, wsb), "grad_norm"), a.iters)
+    result.view(torch.float32)[3] = 0.9999          # clipping in place over and over would run out of something to clip
+    ms_c = _time(lambda: check(mm.mmtrain_grad_clip(tensors, result), "grad_clip"), a.iters)
+    out = {"op": "clip", "config": a.config, "tensors": len(sizes), "n": n, "dtype": a.dtype, "norm_ms": ms_n, "clip_ms": ms_c,
+           "norm_GBps": n * flat.element_size() / ms_n / 1e6, "clip_GBps": 2 * n * flat.element_size() / ms_c / 1e6}
+    if a.dtype == "f32":
+        w, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+        p = torch.empty(n, device="cuda", dtype=torch.bfloat16)
+        desc = mm.make_adam_desc(1e-4, 0.9, 0.95, 1e-8, 0.1, 1.0, 1)
+        out["adam_ms"] = _time(lambda: check(mm.mmtrain_adam_step_clipped(desc, n, w, flat, m, v, p, mm.BF16, result), "adam"), a.iters)
+    print(json.dumps(out))
+
+
 def bench_copy(a):
     n = a.mb * (1 << 20)
     src = torch.empty(n, dtype=torch.uint8, device="cuda").fill_(1)
@@ -132,12 +204,28 @@ def main(argv=None):
     ad = sub.add_parser("adam")
     ad.add_argument("--mparams", type=int, default=202, help="millions of parameters (202 = one 7B layer)")
     ad.add_argument("--iters", type=int, default=20)
+    r = sub.add_parser("rope")
+    r.add_argument("--config", type=int, default=3)
+    r.add_argument("--rot", type=int, default=None, help="rotated features of a head (default: all)")
+    r.add_argument("--interleaved", action="store_true")
+    r.add_argument("--iters", type=int, default=20)
+    j = sub.add_parser("join")
+    j.add_argument("--config", type=int, default=3)
+    j.add_argument("--post", default="rms", choices=["none", "rms", "layer"])
+    j.add_argument("--pre", default="rms", choices=["none", "rms", "layer"])
+    j.add_argument("--gate", default="none", choices=["none", "channel", "segment"])
+    j.add_argument("--iters", type=int, default=20)
+    cl = sub.add_parser("clip")
+    cl.add_argument("--config", type=int, default=3)
+    cl.add_argument("--layers", type=int, default=1)
+    cl.add_argument("--dtype", default="f32", choices=["f32", "bf16"])
+    cl.add_argument("--iters", type=int, default=20)
     c = sub.add_parser("copy")
     c.add_argument("--mb", type=int, default=512)
     c.add_argument("--iters", type=int, default=10)
     a = ap.parse_args(argv)
     mm.load_library()
-    {"gemm": bench_gemm, "attn": bench_attn, "copy": bench_copy, "adam": bench_adam}[a.op](a)
+    {"gemm": bench_gemm, "attn": bench_attn, "copy": bench_copy, "adam": bench_adam, "rope": bench_rope, "join": bench_join, "clip": bench_clip}[a.op](a)
 
 
 if __name__ == "__main__":

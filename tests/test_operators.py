@@ -154,7 +154,7 @@ def rope(desc=None, T=16, batch=None, positions=FAKE, x=FAKE, ldx=512, y=FAKE + 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=2), mm.ERR_INVALID_ARG), (dict(n_heads=0), mm.ERR_INVALID_ARG), (dict(head_dim=0), mm.ERR_INVALID_ARG),
     (dict(rot_dim=130), mm.ERR_INVALID_ARG), (dict(rot_dim=0), mm.ERR_INVALID_ARG), (dict(rot_dim=3), mm.ERR_UNSUPPORTED),
-    (dict(head_dim=258, n_heads=1), mm.ERR_UNSUPPORTED), (dict(layout=2), mm.ERR_INVALID_ARG), (dict(scaling=4), mm.ERR_INVALID_ARG),
+    (dict(head_dim=258, n_heads=1), mm.ERR_UNSUPPORTED), (dict(n_heads=65537), mm.ERR_UNSUPPORTED), (dict(layout=2), mm.ERR_INVALID_ARG), (dict(scaling=4), mm.ERR_INVALID_ARG),
     (dict(scaling=-1), mm.ERR_INVALID_ARG), (dict(base=1.0), mm.ERR_INVALID_ARG), (dict(base=NAN), mm.ERR_INVALID_ARG),
     (dict(base=INF), mm.ERR_INVALID_ARG), (dict(magnitude=-1.0), mm.ERR_INVALID_ARG), (dict(magnitude=NAN), mm.ERR_INVALID_ARG),
     (dict(scaling=mm.ROPE_LINEAR, factor=0.5), mm.ERR_INVALID_ARG), (dict(scaling=mm.ROPE_LINEAR, factor=INF), mm.ERR_INVALID_ARG),
