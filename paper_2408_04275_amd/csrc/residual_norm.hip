@@ -127,6 +127,14 @@ template <int G, int MC, int NT> struct RowSum {
 __device__ __forceinline__ void as_loaded(Raw8<bf16_t> &r) { asm("" : "+v"(r.a.x), "+v"(r.a.y), "+v"(r.a.z), "+v"(r.a.w)); }
 __device__ __forceinline__ void as_loaded(Raw8<float> &) {}
 
+__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+__device__ __forceinline__ f32x4 load4(const bf16_t *p) {
+    const u32x2 r = *reinterpret_cast<const u32x2 *>(p);
+    return {__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16), __uint_as_float(r[1] & 0xffff0000u)};
+}
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
+
 template <typename T> __device__ __forceinline__ void zero8(Raw8<T> &r) { __builtin_memset(&r, 0, sizeof(r)); }
 
 // LN: one of the norms is a LayerNorm (gains only otherwise)
@@ -254,7 +262,7 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     constexpr bool SUM_A = POST || GATE, SUM_B = LN && POST, HEAVY = LN && GATE && POST;
     constexpr bool IN_LDS = LN && POST && MC > 1 && (GATE || sizeof(T) == 4), TIGHT = HEAVY && NT > 512;
     __shared__ float2 red[2][NT / 64];
-    __shared__ __attribute__((aligned(16))) float comb[R > 1 ? R : 1][R > 1 ? W : 4];
+    __shared__ __attribute__((aligned(16))) float comb[LN ? 2 : 1][R > 1 ? R : 1][R > 1 ? W : 4];
     __shared__ __attribute__((aligned(16))) float total_w[GATE && POST ? W : 4], total_b[GATE && SUM_B ? W : 4];
     const int lane = threadIdx.x % G, grp = __builtin_amdgcn_readfirstlane(threadIdx.x / G), H = a.H, block = blockIdx.x;
     RowSum<G, MC, NT> row_sum{red, H};
@@ -276,7 +284,7 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
         if constexpr (TIGHT) as_loaded(held[i]);
         return held[i];
     };
-    float s_pre_w[MC][8] = {}, s_pre_b[LN ? MC : 1][8] = {}, sum_a[MC][8] = {}, sum_b[MC][8] = {};
+    float s_pre_w[MC][8] = {}, s_pre_b[LN ? MC : 1][8] = {}, sum_a[MC][8] = {}, sum_b[LN ? MC : 1][8] = {};
     float pr = 0.f, pmu = 0.f, pr2 = 0.f, pmu2 = 0.f;
 #pragma unroll
     for (int i = 0; i < MC; ++i) { zero8(pdy[i]); zero8(pdh[i]); zero8(py[i]); zero8(pb[i]); }
@@ -307,58 +315,54 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
         if constexpr (POST) keep(w2, 1, i, a.post_w);
         if (GATE && a.gate == GATE_CHANNEL) gt[i] = load_plain8((const T *)a.gate_v + col(i));
     }
-    // the sums of the groups, added in order, handed out in quads of columns; always the same quads to the same thread
-    auto flush = [&](auto value, auto emit) {
+    // two sums over the groups' rows, added in order, handed out in quads of columns, the same quads to the same thread every time
+    auto flush = [&](const float (&p)[MC][8], const float (&q)[LN ? MC : 1][8], auto emit) {
         if constexpr (R == 1) {
 #pragma unroll
             for (int i = 0; i < MC; ++i)
                 if (col(i) < H) {
-                    float v[8];
-                    value(i, v);
-                    emit(col(i), f32x4{v[0], v[1], v[2], v[3]});
-                    emit(col(i) + 4, f32x4{v[4], v[5], v[6], v[7]});
+#pragma unroll
+                    for (int j = 0; j < 8; j += 4) {
+                        const int k = LN ? i : 0;
+                        emit(col(i) + j, f32x4{p[i][j], p[i][j + 1], p[i][j + 2], p[i][j + 3]}, f32x4{q[k][j], q[k][j + 1], q[k][j + 2], q[k][j + 3]});
+                    }
                 }
         } else {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < MC; ++i)
                 if (col(i) < H) {
-                    float v[8];
-                    value(i, v);
-                    store8(&comb[grp][col(i)], v);
+                    store8(&comb[0][grp][col(i)], p[i]);
+                    if constexpr (LN) store8(&comb[1][grp][col(i)], q[i]);
                 }
             __syncthreads();
             for (int c = threadIdx.x * 4; c < H; c += NT * 4) {
-                f32x4 s = *reinterpret_cast<const f32x4 *>(&comb[0][c]);
+                f32x4 s[2] = {};
 #pragma unroll
-                for (int g = 1; g < R; ++g) s += *reinterpret_cast<const f32x4 *>(&comb[g][c]);
-                emit(c, s);
+                for (int k = 0; k < (LN ? 2 : 1); ++k) {
+                    s[k] = *reinterpret_cast<const f32x4 *>(&comb[k][0][c]);
+#pragma unroll
+                    for (int g = 1; g < R; ++g) s[k] += *reinterpret_cast<const f32x4 *>(&comb[k][g][c]);
+                }
+                emit(c, s[0], s[1]);
             }
         }
     };
-    auto plain = [](const float (&sum)[MC][8]) {
-        return [&sum](int i, float (&v)[8]) {
+    auto each_quad = [&](auto f) {                          // ... these quads
+        if constexpr (R == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = sum[i][j];
-        };
+            for (int i = 0; i < MC; ++i)
+                if (col(i) < H) { f(col(i)); f(col(i) + 4); }
+        } else {
+            for (int c = threadIdx.x * 4; c < H; c += NT * 4) f(c);
+        }
     };
-    auto gated = [&](const float (&sum)[MC][8]) {               // beta gate sum
-        return [&](int i, float (&v)[8]) {
-            float g[8];
-            if constexpr (GATE) unpack8(gt[i], g);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = a.beta * (GATE ? g[j] : 1.f) * sum[i][j];
-        };
-    };
-    auto gate_gradient = [&](int i, float (&v)[8]) {            // beta (w A + b B), or beta A
-        float w[8], o[8];
-        if constexpr (POST) unpack8(kept(w2, 1, i), w);
-        if (SUM_B && a.post == NORM_LAYER) load8((const T *)a.post_b + col(i), o);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = a.beta * ((POST ? w[j] : 1.f) * sum_a[i][j] + (SUM_B && a.post == NORM_LAYER ? o[j] * sum_b[i][j] : 0.f));
-    };
-    auto to_part = [&](float *part, size_t row) {
-        return [=](int c, f32x4 s) { *reinterpret_cast<f32x4 *>(part + row * H + c) = s; };
+    auto quad = [](float *p) -> f32x4 & { return *reinterpret_cast<f32x4 *>(p); };
+    // gradient of the gate from A and B: beta (w A + b B), or beta A
+    auto gate_gradient = [&](int c, f32x4 sa, f32x4 sb) {
+        if constexpr (POST) sa *= load4((const T *)a.post_w + c);
+        if (SUM_B && a.post == NORM_LAYER) sa += sb * load4((const T *)a.post_b + c);
+        return a.beta * sa;
     };
     request(r0 + grp, r1);
     for (int start = r0; start < r1;) {                     // start + grp is requested
@@ -453,64 +457,52 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
         }
         if constexpr (GATE) {
             if (by_segment) {
-                if (a.p_gate) {
-                    if (a.cu[seg] >= r0 && a.cu[seg + 1] <= r1) {
-                        flush(gate_gradient, [&](int c, f32x4 s) {
-                            const size_t at = (size_t)seg * H + c;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if (a.grad_f32) ((float *)a.d_gate)[at + j] = s[j] + (a.accumulate ? ((float *)a.d_gate)[at + j] : 0.f);
-                                else Elem<T>::store((T *)a.d_gate + at + j, s[j] + (a.accumulate ? Elem<T>::load((T *)a.d_gate + at + j) : 0.f));
-                            }
-                        });
-                    } else {
-                        flush(gate_gradient, to_part(a.p_gate, 2 * (size_t)block + (start != r0)));
+                const bool whole = a.cu[seg] >= r0 && a.cu[seg + 1] <= r1;
+                const size_t out = (size_t)seg * H, slot = (2 * (size_t)block + (start != r0)) * H;
+                flush(sum_a, sum_b, [&](int c, f32x4 sa, f32x4 sb) {
+                    if (a.p_gate) {
+                        const f32x4 g = gate_gradient(c, sa, sb);
+                        if (!whole) quad(a.p_gate + slot + c) = g;
+                        else if (a.grad_f32) quad((float *)a.d_gate + out + c) = a.accumulate ? quad((float *)a.d_gate + out + c) + g : g;
+                        else store4((T *)a.d_gate + out + c, a.accumulate ? load4((const T *)a.d_gate + out + c) + g : g);
                     }
-                }
-                auto to_total = [&](float *total) {             // (the thread that adds a quad up also reads it at the end)
-                    return [=](int c, f32x4 s) {
-                        f32x4 *t = reinterpret_cast<f32x4 *>(total + c);
-                        *t = start == r0 ? s : *t + s;
-                    };
-                };
-                if constexpr (POST) { if (a.p_post_w) flush(gated(sum_a), to_total(total_w)); }
-                if constexpr (SUM_B) { if (a.p_post_b) flush(gated(sum_b), to_total(total_b)); }
+                    if constexpr (POST) {
+                        const f32x4 g = a.beta * load4((const T *)a.gate_v + out + c);
+                        quad(total_w + c) = start == r0 ? g * sa : quad(total_w + c) + g * sa;
+                        if constexpr (SUM_B) quad(total_b + c) = start == r0 ? g * sb : quad(total_b + c) + g * sb;
+                    }
+                });
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum_a[i][j] = sum_b[i][j] = 0.f;
+                    for (int j = 0; j < 8; ++j) {
+                        sum_a[i][j] = 0.f;
+                        if constexpr (LN) sum_b[i][j] = 0.f;
+                    }
             }
         }
         start = end;
     }
-    if (a.p_pre_w) flush(plain(s_pre_w), to_part(a.p_pre_w, block));
-    if constexpr (LN) {
-        if (a.p_pre_b) flush([&](int i, float (&v)[8]) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = s_pre_b[i][j];
-        }, to_part(a.p_pre_b, block));
-    }
-    auto from_total = [&](const float *total, float *part) {
-        auto to = to_part(part, block);
-        flush([](int, float (&v)[8]) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        }, [&](int c, f32x4) { to(c, *reinterpret_cast<const f32x4 *>(total + c)); });
-    };
-    if constexpr (POST) {
-        if (a.p_post_w) {
-            if (by_segment) from_total(total_w, a.p_post_w);
-            else flush(gated(sum_a), to_part(a.p_post_w, block));
-        }
-    }
-    if constexpr (SUM_B) {
-        if (a.p_post_b) {
-            if (by_segment) from_total(total_b, a.p_post_b);
-            else flush(gated(sum_b), to_part(a.p_post_b, block));
-        }
-    }
-    if constexpr (GATE) {
-        if (a.p_gate && !by_segment) flush(gate_gradient, to_part(a.p_gate, block));
+    const size_t mine = (size_t)block * H;
+    if (a.p_pre_w || a.p_pre_b)
+        flush(s_pre_w, s_pre_b, [&](int c, f32x4 w, f32x4 b) {
+            if (a.p_pre_w) quad(a.p_pre_w + mine + c) = w;
+            if (LN && a.p_pre_b) quad(a.p_pre_b + mine + c) = b;
+        });
+    if (by_segment) {
+        if constexpr (GATE && POST)
+            each_quad([&](int c) {
+                if (a.p_post_w) quad(a.p_post_w + mine + c) = quad(total_w + c);
+                if constexpr (SUM_B) { if (a.p_post_b) quad(a.p_post_b + mine + c) = quad(total_b + c); }
+            });
+    } else if (SUM_A && (a.p_post_w || a.p_post_b || a.p_gate)) {
+        flush(sum_a, sum_b, [&](int c, f32x4 sa, f32x4 sb) {
+            f32x4 g = {a.beta, a.beta, a.beta, a.beta};
+            if constexpr (GATE) g *= load4((const T *)a.gate_v + c);
+            if (POST && a.p_post_w) quad(a.p_post_w + mine + c) = g * sa;
+            if (SUM_B && a.p_post_b) quad(a.p_post_b + mine + c) = g * sb;
+            if (GATE && a.p_gate) quad(a.p_gate + mine + c) = gate_gradient(c, sa, sb);
+        });
     }
 }
 
