@@ -2,10 +2,11 @@
 //     n = norm_post(b);  y = alpha x + beta gate n;  h = norm_pre(y)
 //
 // Memory-bound: forward reads x and b and writes y and h, backward reads dy, dh, y and b and writes dx and db, each once; a row stays in
-// registers from its first use to its last.  A row is worked on by a group of G threads with MC chunks of 8 columns each -- a wavefront
-// up to 1024 columns, where sums need no barrier -- and a workgroup of NT threads walks over a contiguous range of rows, NT / G at a
-// time, the next ones requested before the present ones are reduced.  Gains, biases and gates stay in registers; so do backward's
-// sums over tokens, which leave the workgroup as one partial row.
+// registers from its first use to its last.  A row is worked on by a group of G threads with MC chunks of 8 columns each, and a
+// workgroup of NT threads walks over a contiguous range of rows, NT / G at a time, the next ones requested before the present ones are
+// reduced.  Gains, biases and gates stay in registers; so do backward's sums over tokens, which leave the workgroup as one partial row.
+// 8192 rows of 4096 in bf16, two RMSNorms: forward 55 us (4.9 TB/s), backward 81 us (4.9 TB/s) and 5 us for the sums of the partial rows; a copy
+// of as many bytes runs at 5.0 to 5.4 TB/s.  Below about 2000 rows the launches and the first row's way through the chip bound both.
 #include "ops.h"
 #include "reduce.h"
 #include "vec8.h"
@@ -84,41 +85,46 @@ template <int G, int MC, int NT> struct RowSum {
         for (int k = 0; k < MC; ++k) n += min(max(H - (i * 64 + k * G) * 8, 0), 512);
         return (float)n;
     }
-    // Mean and 1 / deviation of the row of which this thread holds v (zero outside of it).  With a mean: first about each wavefront's own mean, then
-    // joined, so that nothing cancels however far the row is from zero and one barrier is enough.
-    template <typename In>
-    __device__ __forceinline__ void statistics(const float (&v)[MC][8], bool layer, float eps, In inside, float &mu, float &r) {
+    // Mean and 1 / deviation of the row of which this thread holds v, zero outside of it.  MEAN: with the mean, if `layer` (zero otherwise), first
+    // about each wavefront's own mean, then joined, so that nothing cancels however far the row is from zero and one barrier is enough.
+    // inv_columns: 1 / the columns of this wavefront (0 if it has none).
+    template <bool MEAN, typename In>
+    __device__ __forceinline__ void statistics(const float (&v)[MC][8], bool layer, float inv_columns, float eps, In inside, float &mu, float &r) {
         const float inv_h = 1.f / H;
         float q = 0.f;
         mu = 0.f;
-        if (layer) {
+        if constexpr (MEAN) {
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < MC; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum += v[i][j];
-            const float n = columns(threadIdx.x % G / 64);
-            mu = n > 0.f ? wave_total(sum) / n : 0.f;
+            sum = wave_total(sum) * inv_columns;
+            mu = layer ? sum : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < MC; ++i)
-            if (inside(i)) {
+        for (int i = 0; i < MC; ++i) {
+            float t = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) q += (v[i][j] - mu) * (v[i][j] - mu);
-            }
+            for (int j = 0; j < 8; ++j) t += (v[i][j] - mu) * (v[i][j] - mu);
+            q += !MEAN || inside(i) ? t : 0.f;
+        }
         q = wave_total(q);
         if constexpr (G > 64) {
             const float2 *all = share(make_float2(mu, q));
             q = mu = 0.f;
-            if (layer) {
+            if constexpr (MEAN) {
 #pragma unroll
                 for (int i = 0; i < G / 64; ++i) mu += columns(i) * all[i].x;
                 mu *= inv_h;
-            }
 #pragma unroll
-            for (int i = 0; i < G / 64; ++i) q += all[i].y + (layer ? columns(i) * (all[i].x - mu) * (all[i].x - mu) : 0.f);
+                for (int i = 0; i < G / 64; ++i) q += all[i].y + columns(i) * (all[i].x - mu) * (all[i].x - mu);
+            } else {
+#pragma unroll
+                for (int i = 0; i < G / 64; ++i) q += all[i].y;
+            }
         }
-        r = 1.f / sqrtf(q * inv_h + eps);
+        r = rsqrtf(q * inv_h + eps);
     }
 };
 
@@ -137,8 +143,8 @@ __device__ __forceinline__ void store4(bf16_t *p, f32x4 v) { *reinterpret_cast<u
 
 template <typename T> __device__ __forceinline__ void zero8(Raw8<T> &r) { __builtin_memset(&r, 0, sizeof(r)); }
 
-// LN: one of the norms is a LayerNorm (gains only otherwise)
-template <typename T, int G, int MC, int NT, bool LN>
+// LN: one of the norms is a LayerNorm (gains only otherwise); the other may be an RMSNorm, which then has mean and bias zero.
+template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd_kernel(JoinArgs a) {
     constexpr int R = NT / G;
     constexpr bool IN_LDS = LN && MC > 1 && G > 256 && sizeof(T) == 2, TIGHT = LN && MC > 1 && !IN_LDS;
@@ -147,13 +153,19 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
     const int lane = threadIdx.x % G, grp = __builtin_amdgcn_readfirstlane(threadIdx.x / G), H = a.H;
     RowSum<G, MC, NT> row_sum{red, H};
     const int r0 = join_row(a.T, gridDim.x, blockIdx.x), r1 = join_row(a.T, gridDim.x, blockIdx.x + 1);
+    const float wave_columns = row_sum.columns(__builtin_amdgcn_readfirstlane(lane / 64)), inv_columns = wave_columns > 0.f ? 1.f / wave_columns : 0.f;
     auto col = [&](int i) { return (lane + i * G) * 8; };
-    // IN_LDS: gains and biases wait in LDS, each thread's own, where registers for them would cost a workgroup per compute unit
+    auto inside = [&](int i) { return col(i) < H; };
+    // IN_LDS: gains and biases wait in LDS, each thread's own, where registers for them would cost a workgroup per compute unit (9000 rows of
+    // 8192, two LayerNorms and a gate: 205 -> 152 us)
     __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 4 : 1][IN_LDS ? G * MC * 8 : 8];
     constexpr int HELD = IN_LDS ? 1 : MC;
-    Raw8<T> nx[MC], nb[MC], w2[HELD], w1[HELD], gt[MC], b2[LN ? HELD : 1], b1[LN ? HELD : 1];
+    Raw8<T> nx[MC], nb[MC], w1[HELD], w2[POST ? HELD : 1], b1[LN ? HELD : 1], b2[LN && POST ? HELD : 1], gt[GATE ? MC : 1];
+    // a parameter's chunk; zero where there is none, so that what is outside of the row stays zero throughout
     auto keep = [&](Raw8<T> *held, int slot, int i, const void *from) {
-        const Raw8<T> v = load_plain8((const T *)from + col(i));
+        Raw8<T> v;
+        zero8(v);
+        if (from && inside(i)) v = load_plain8((const T *)from + col(i));
         if constexpr (IN_LDS) *reinterpret_cast<Raw8<T> *>(&parked[slot][col(i)]) = v;
         else held[i] = v;
     };
@@ -162,14 +174,13 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
         if constexpr (TIGHT) as_loaded(held[i]);
         return held[i];
     };
-    // what is outside of the row stays zero from here on
 #pragma unroll
     for (int i = 0; i < MC; ++i) { zero8(nx[i]); zero8(nb[i]); }
     auto request = [&](int row) {
         if (row >= r1) return;
 #pragma unroll
         for (int i = 0; i < MC; ++i) {
-            if (col(i) >= H) continue;
+            if (!inside(i)) continue;
             const size_t at = (size_t)row * H + col(i);
             load_raw8((const T *)a.x + at, nx[i]);
             if (a.b) load_raw8((const T *)a.b + at, nb[i]);
@@ -178,43 +189,47 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
     request(r0 + grp);
 #pragma unroll
     for (int i = 0; i < MC; ++i) {
-        if (col(i) >= H) continue;
-        if (a.post != NORM_NONE) keep(w2, 0, i, a.post_w);
-        if (a.pre != NORM_NONE) keep(w1, 1, i, a.pre_w);
-        if (LN && a.post == NORM_LAYER) keep(b2, 2, i, a.post_b);
-        if (LN && a.pre == NORM_LAYER) keep(b1, 3, i, a.pre_b);
-        if (a.gate == GATE_CHANNEL) gt[i] = load_plain8((const T *)a.gate_v + col(i));
+        keep(w1, 0, i, a.pre_w);
+        if constexpr (LN) keep(b1, 1, i, a.pre_b);
+        if constexpr (POST) keep(w2, 2, i, a.post_w);
+        if constexpr (LN && POST) keep(b2, 3, i, a.post_b);
+        if constexpr (GATE) {
+            zero8(gt[i]);
+            if (a.gate == GATE_CHANNEL && inside(i)) gt[i] = load_plain8((const T *)a.gate_v + col(i));
+        }
     }
     int seg_end = 0;
     // v <- normalised v, gain and bias applied
-    auto norm = [&](float (&v)[MC][8], int kind, float eps, Raw8<T> *w, Raw8<T> *bias, int slot, float &mu, float &r) {
-        row_sum.statistics(v, LN && kind == NORM_LAYER, eps, [&](int i) { return col(i) < H; }, mu, r);
+    auto norm = [&](float (&v)[MC][8], bool layer, float eps, Raw8<T> *w, Raw8<T> *bias, int slot, float &mu, float &r) {
+        row_sum.template statistics<LN>(v, layer, inv_columns, eps, inside, mu, r);
 #pragma unroll
         for (int i = 0; i < MC; ++i) {
             float g[8], o[8];
             unpack8(kept(w, slot, i), g);
-            if (LN && kind == NORM_LAYER) unpack8(kept(bias, slot + 2, i), o);
+            if constexpr (LN) unpack8(kept(bias, slot + 1, i), o);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - mu) * r * g[j] + (LN && kind == NORM_LAYER ? o[j] : 0.f);
+            for (int j = 0; j < 8; ++j) v[i][j] = (v[i][j] - mu) * r * g[j] + (LN ? o[j] : 0.f);
         }
     };
     for (int base = r0; base < r1; base += R) {
         const int row = base + grp;
         const bool valid = row < r1;
-        float xv[MC][8], v[MC][8], mu, r;
+        float v[MC][8], n[MC][8], mu, r;
 #pragma unroll
-        for (int i = 0; i < MC; ++i) { unpack8(nx[i], xv[i]); unpack8(nb[i], v[i]); }
+        for (int i = 0; i < MC; ++i) { unpack8(nx[i], v[i]); unpack8(nb[i], n[i]); }
         request(row + R);
         if (a.b) {
-            if (a.gate == GATE_SEGMENT && valid && row >= seg_end) {
-                const int seg = find_segment_wave(a.cu, a.S, row);
-                seg_end = a.cu[seg + 1];
+            if constexpr (GATE) {
+                if (a.gate == GATE_SEGMENT && valid && row >= seg_end) {
+                    const int seg = find_segment_wave(a.cu, a.S, row);
+                    seg_end = a.cu[seg + 1];
 #pragma unroll
-                for (int i = 0; i < MC; ++i)
-                    if (col(i) < H) gt[i] = load_plain8((const T *)a.gate_v + (size_t)seg * H + col(i));
+                    for (int i = 0; i < MC; ++i)
+                        if (inside(i)) gt[i] = load_plain8((const T *)a.gate_v + (size_t)seg * H + col(i));
+                }
             }
-            if (a.post != NORM_NONE) {
-                norm(v, a.post, a.post_eps, w2, b2, 0, mu, r);
+            if constexpr (POST) {
+                norm(n, a.post == NORM_LAYER, a.post_eps, w2, b2, 2, mu, r);
                 if (lane == 0 && valid) {
                     if (a.post_rstd) a.post_rstd[row] = r;
                     if (LN && a.post == NORM_LAYER && a.post_mean) a.post_mean[row] = mu;
@@ -223,28 +238,24 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
                 float g[8];
-                if constexpr (TIGHT) as_loaded(gt[i]);
-                if (a.gate != GATE_NONE) unpack8(gt[i], g);
+                if constexpr (GATE) {
+                    if constexpr (TIGHT) as_loaded(gt[i]);
+                    unpack8(gt[i], g);
+                }
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[i][j] = col(i) < H ? a.alpha * xv[i][j] + a.beta * (a.gate != GATE_NONE ? g[j] : 1.f) * v[i][j] : 0.f;
-                if (valid && col(i) < H) store8((T *)a.y + (size_t)row * H + col(i), v[i]);
+                for (int j = 0; j < 8; ++j) v[i][j] = a.alpha * v[i][j] + a.beta * (GATE ? g[j] * n[i][j] : n[i][j]);
+                if (valid && inside(i)) store8((T *)a.y + (size_t)row * H + col(i), v[i]);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < MC; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = xv[i][j];
         }
         if (a.pre == NORM_NONE) continue;
-        norm(v, a.pre, a.pre_eps, w1, b1, 1, mu, r);
+        norm(v, a.pre == NORM_LAYER, a.pre_eps, w1, b1, 0, mu, r);
         if (lane == 0 && valid) {
             if (a.pre_rstd) a.pre_rstd[row] = r;
             if (LN && a.pre == NORM_LAYER && a.pre_mean) a.pre_mean[row] = mu;
         }
 #pragma unroll
         for (int i = 0; i < MC; ++i)
-            if (valid && col(i) < H) store8((T *)a.h + (size_t)row * H + col(i), v[i]);
+            if (valid && inside(i)) store8((T *)a.h + (size_t)row * H + col(i), v[i]);
     }
 }
 
@@ -255,7 +266,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
 //
 // By segment, a workgroup's gate sums go out at the end of each segment's rows: as the gradient where it has all of them, else into its
 // slot 0 if its range begins inside the segment or with it, and into slot 1 otherwise (then the range ends in it); the post norm's sums are added up in
-// LDS.  One workgroup per compute unit: more would leave more partial rows to be added up.
+// LDS.  One workgroup per compute unit: more leave more partial rows to be added up (two RMSNorms in bf16, 256, 512 and 1024 workgroups: 9000 rows of 1280
+// 41.5, 44.5, 52.9 us, 600 rows of 8192 23.4, 32.1, 34.3; only rows of up to 512 would gain by two, 22.1 and 19.8).
 template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     constexpr int R = NT / G, W = G * MC * 8;
@@ -270,12 +282,18 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     const float inv_h = 1.f / H;
     const bool pre = a.pre != NORM_NONE, by_segment = GATE && a.gate == GATE_SEGMENT;
     auto col = [&](int i) { return (lane + i * G) * 8; };
-    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill otherwise
+    auto inside = [&](int i) { return col(i) < H; };
+    const float alpha = a.b ? a.alpha : 1.f;
+    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill more otherwise (9000 rows of 8192 in fp32, two LayerNorms and
+    // a gate: 485 -> 394 us)
     __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 2 : 1][IN_LDS ? W : 8];
     constexpr int HELD = IN_LDS ? 1 : MC;
     Raw8<T> pdy[MC], pdh[MC], py[MC], pb[MC], w1[HELD], w2[POST ? HELD : 1], gt[GATE ? MC : 1];
+    // a parameter's chunk; zero outside of the row, which keeps what is computed there out of the row's sums
     auto keep = [&](Raw8<T> *held, int slot, int i, const void *from) {
-        const Raw8<T> v = load_plain8((const T *)from + col(i));
+        Raw8<T> v;
+        zero8(v);
+        if (from && inside(i)) v = load_plain8((const T *)from + col(i));
         if constexpr (IN_LDS) *reinterpret_cast<Raw8<T> *>(&parked[slot][col(i)]) = v;
         else held[i] = v;
     };
@@ -310,10 +328,12 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < MC; ++i) {
-        if (col(i) >= H) continue;
-        if (pre) keep(w1, 0, i, a.pre_w);
+        keep(w1, 0, i, a.pre_w);
         if constexpr (POST) keep(w2, 1, i, a.post_w);
-        if (GATE && a.gate == GATE_CHANNEL) gt[i] = load_plain8((const T *)a.gate_v + col(i));
+        if constexpr (GATE) {
+            zero8(gt[i]);
+            if (a.gate == GATE_CHANNEL && inside(i)) gt[i] = load_plain8((const T *)a.gate_v + col(i));
+        }
     }
     // two sums over the groups' rows, added in order, handed out in quads of columns, the same quads to the same thread every time
     auto flush = [&](const float (&p)[MC][8], const float (&q)[LN ? MC : 1][8], auto emit) {
@@ -386,60 +406,50 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
             for (int i = 0; i < MC; ++i) { unpack8(pdy[i], d[i]); unpack8(pdh[i], back[i]); unpack8(py[i], hat[i]); unpack8(pb[i], bv[i]); }
             const bool more = base + R < end;
             request(more ? row + R : end + grp, more ? end : r1);
-            if (pre) {
-                float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                for (int i = 0; i < MC; ++i) {
-                    if (col(i) >= H) continue;
-                    float g[8];
-                    unpack8(kept(w1, 0, i), g);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        hat[i][j] = (hat[i][j] - mu) * r;
-                        s_pre_w[i][j] += back[i][j] * hat[i][j];
-                        if (LN) s_pre_b[i][j] += back[i][j];
-                        back[i][j] *= g[j];
-                        if (LN) s0 += back[i][j];
-                        s1 += back[i][j] * hat[i][j];
-                    }
-                }
-                if constexpr (LN) row_sum(s0, s1);
-                else row_sum(s1);
-                s0 = LN && a.pre == NORM_LAYER ? s0 * inv_h : 0.f;
-                s1 *= inv_h;
-#pragma unroll
-                for (int i = 0; i < MC; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] += r * (back[i][j] - s0 - hat[i][j] * s1);
-            }
-            if (!a.b) {
-#pragma unroll
-                for (int i = 0; i < MC; ++i)
-                    if (a.dx && valid && col(i) < H) store8((T *)a.dx + (size_t)row * H + col(i), d[i]);
-                continue;
-            }
-            float u0 = 0.f, u1 = 0.f;
+            // no pre norm: r, dh and y are zero, and so is all of this
+            float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
-                if (col(i) >= H) continue;
+                float g[8];
+                unpack8(kept(w1, 0, i), g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    hat[i][j] = LN ? (hat[i][j] - mu) * r : hat[i][j] * r;
+                    s_pre_w[i][j] += back[i][j] * hat[i][j];
+                    if (LN) s_pre_b[i][j] += back[i][j];
+                    back[i][j] *= g[j];
+                    if (LN) s0 += back[i][j];
+                    s1 += back[i][j] * hat[i][j];
+                }
+            }
+            if constexpr (LN) row_sum(s0, s1);
+            else row_sum(s1);
+            s0 = LN && a.pre == NORM_LAYER ? s0 * inv_h : 0.f;
+            s1 *= inv_h;
+#pragma unroll
+            for (int i = 0; i < MC; ++i) {
                 float g[8], w[8], dx[8];
-                if constexpr (HEAVY && (MC > 1 || NT > 512)) as_loaded(gt[i]);
-                if constexpr (GATE) unpack8(gt[i], g);
+                if constexpr (GATE) {
+                    if constexpr (HEAVY && (MC > 1 || NT > 512)) as_loaded(gt[i]);
+                    unpack8(gt[i], g);
+                }
                 if constexpr (POST) unpack8(kept(w2, 1, i), w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    dx[j] = a.alpha * d[i][j];
-                    hat[i][j] = POST ? (bv[i][j] - mu2) * r2 : bv[i][j];
+                    d[i][j] += r * ((LN ? back[i][j] - s0 : back[i][j]) - hat[i][j] * s1);
+                    dx[j] = alpha * d[i][j];
+                    hat[i][j] = POST ? (LN ? (bv[i][j] - mu2) * r2 : bv[i][j] * r2) : bv[i][j];
                     if (SUM_A) sum_a[i][j] += d[i][j] * hat[i][j];
                     if (SUM_B) sum_b[i][j] += d[i][j];
-                    back[i][j] = a.beta * d[i][j] * (GATE ? g[j] : 1.f);
+                    back[i][j] = a.beta * d[i][j];
+                    if (GATE) back[i][j] *= g[j];
                     if (POST) {
                         back[i][j] *= w[j];
                         if (LN) u0 += back[i][j];
                         u1 += back[i][j] * hat[i][j];
                     }
                 }
-                if (a.dx && valid) store8((T *)a.dx + (size_t)row * H + col(i), dx);
+                if (a.dx && valid && inside(i)) store8((T *)a.dx + (size_t)row * H + col(i), dx);
             }
             if constexpr (POST) {
                 if constexpr (LN) row_sum(u0, u1);
@@ -449,11 +459,11 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) back[i][j] = r2 * (back[i][j] - u0 - hat[i][j] * u1);
+                    for (int j = 0; j < 8; ++j) back[i][j] = r2 * ((LN ? back[i][j] - u0 : back[i][j]) - hat[i][j] * u1);
             }
 #pragma unroll
             for (int i = 0; i < MC; ++i)
-                if (a.db && valid && col(i) < H) store8((T *)a.db + (size_t)row * H + col(i), back[i]);
+                if (a.db && valid && inside(i)) store8((T *)a.db + (size_t)row * H + col(i), back[i]);
         }
         if constexpr (GATE) {
             if (by_segment) {
@@ -579,43 +589,60 @@ __global__ __launch_bounds__(256) void join_sums_kernel(ReduceJobSet set, GateSu
     }
 }
 
+template <typename F> auto with(bool v, F f) { return v ? f(std::true_type{}) : f(std::false_type{}); }
+
 template <typename T, int G, int MC, int NT, bool LN>
 hipError_t launch_fwd(const JoinArgs &a, hipStream_t st) {
-    static std::atomic<int> resident{0};
-    auto kern = join_fwd_kernel<T, G, MC, NT, LN>;
-    int grid = 0;
-    hipError_t e = resident_workgroups(resident, kern, grid, NT);
-    if (e != hipSuccess) return e;
-    const int all = ceil_div(a.T, NT / G);
-    kern<<<all < grid ? all : grid, NT, 0, st>>>(a);
-    return hipGetLastError();
+    return with(a.gate != GATE_NONE, [&](auto GATE) {
+        return with(a.post != NORM_NONE, [&](auto POST) {
+            static std::atomic<int> resident{0};
+            auto kern = join_fwd_kernel<T, G, MC, NT, LN, decltype(GATE)::value, decltype(POST)::value>;
+            int grid = 0;
+            const hipError_t e = resident_workgroups(resident, kern, grid, NT);
+            if (e != hipSuccess) return e;
+            const int all = ceil_div(a.T, NT / G);
+            kern<<<all < grid ? all : grid, NT, 0, st>>>(a);
+            return hipGetLastError();
+        });
+    });
 }
 
 template <typename T, int G, int MC, int NT>
 hipError_t launch_bwd(const JoinArgs &a, hipStream_t st) {
     const int blocks = join_bwd_blocks(a.T, a.H);
-    auto go = [&](auto LN, auto GATE, auto POST) { join_bwd_kernel<T, G, MC, NT, decltype(LN)::value, decltype(GATE)::value, decltype(POST)::value><<<blocks, NT, 0, st>>>(a); };
-    auto with = [&](bool v, auto f) { if (v) f(std::true_type{}); else f(std::false_type{}); };
-    with(a.post == NORM_LAYER || a.pre == NORM_LAYER, [&](auto LN) {
-        with(a.gate != GATE_NONE, [&](auto GATE) { with(a.post != NORM_NONE, [&](auto POST) { go(LN, GATE, POST); }); });
+    return with(a.post == NORM_LAYER || a.pre == NORM_LAYER, [&](auto LN) {
+        return with(a.gate != GATE_NONE, [&](auto GATE) {
+            return with(a.post != NORM_NONE, [&](auto POST) {
+                join_bwd_kernel<T, G, MC, NT, decltype(LN)::value, decltype(GATE)::value, decltype(POST)::value><<<blocks, NT, 0, st>>>(a);
+                return hipGetLastError();
+            });
+        });
     });
-    return hipGetLastError();
 }
 
-// by width: (threads a row, chunks a thread, threads a workgroup)
+// By width: threads a row, chunks a thread, threads a workgroup.  Few idle lanes in a row, and few enough registers for two workgroups per compute unit or
+// more, so that one's sums go on beside another's loads.  9000 bf16 rows forward, two RMSNorms / two LayerNorms and a gate, us, the row's class against the
+// next best: 1024 (128, 1) 15.0 / 18.3, (64, 2) 15.1 / 21.7; 1280 192 threads a workgroup 21.2 / 23.0, 384 17.7 / 30.8, so the latter where there is no mean;
+// 4096 (512, 1) 60.3 / 63.6, (256, 2) 61.6 / 66.3; 5120 (640, 1) 79.4 / 96.4, (384, 2) 78.9 / 89.7 (fp32 151 / 154, 155 / 165); 8192 (512, 2) 129 / 147, (1024, 1) 122 / 155, so the latter where there is no mean.
 template <typename T>
 hipError_t fwd_by_width(const JoinArgs &a, hipStream_t st) {
     const bool ln = a.post == NORM_LAYER || a.pre == NORM_LAYER;
-#define L(G, MC, NT) return ln ? launch_fwd<T, G, MC, NT, true>(a, st) : launch_fwd<T, G, MC, NT, false>(a, st)
-    if (a.H <= 64 * 8) L(64, 1, 256);
-    if (a.H <= 128 * 8) L(64, 2, 256);
-    if (a.H <= 192 * 8) L(192, 1, 192);
-    if (a.H <= 256 * 8) L(256, 1, 256);
-    if (a.H <= 512 * 8) L(256, 2, 256);
-    if (a.H <= 640 * 8) L(320, 2, 320);
-    L(512, 2, 512);
+#define L(G, MC, NT) (ln ? launch_fwd<T, G, MC, NT, true>(a, st) : launch_fwd<T, G, MC, NT, false>(a, st))
+    if (a.H <= 64 * 8) return L(64, 1, 256);
+    if (a.H <= 128 * 8) return L(128, 1, 256);
+    if (a.H <= 192 * 8) return ln ? launch_fwd<T, 192, 1, 192, true>(a, st) : launch_fwd<T, 192, 1, 384, false>(a, st);
+    if (a.H <= 256 * 8) return ln ? launch_fwd<T, 256, 1, 256, true>(a, st) : launch_fwd<T, 256, 1, 512, false>(a, st);
+    if (a.H <= 512 * 8) return L(512, 1, 512);
+    if (a.H <= 640 * 8) {
+        if (ln && sizeof(T) == 2) return launch_fwd<T, 384, 2, 384, true>(a, st);
+        return L(640, 1, 640);
+    }
+    return ln ? launch_fwd<T, 512, 2, 512, true>(a, st) : launch_fwd<T, 1024, 1, 1024, false>(a, st);
 #undef L
 }
+// Backward, where a workgroup has the compute unit to itself: as many threads as have the registers.  Two RMSNorms / two LayerNorms and a gate, bf16: 1024 (128, 1)
+// 27.7 / 43.5, (64, 2) 27.1 / 49.5 (fp32 / 68, / 100: it spills); 1280 768 threads 31.5 / 50.6, 576 threads 42.7 / 54.4; 4096 (512, 1) 97.6 / 133, (256, 2) 96.8 / 151;
+// 8192 (512, 2) 192 / 295, (1024, 1) 192 / 494.
 template <typename T>
 hipError_t bwd_by_width(const JoinArgs &a, hipStream_t st) {
     if (a.H <= 64 * 8) return launch_bwd<T, 64, 1, 512>(a, st);
