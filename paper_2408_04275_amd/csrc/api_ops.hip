@@ -25,8 +25,9 @@ int rope_turns(const mmtrain_rope_desc &d, RopeArgs &a) {
         first = std::max(std::floor(index(d.high)), 0.0);
         last = std::min(std::ceil(index(d.low)), r - 1.0);
     }
+    const double rate = -2.0 * std::log(base) / r;
     for (int i = 0; i < a.half; ++i) {
-        double theta = std::pow(base, -2.0 * i / r), keep = 1.0;
+        double theta = std::exp(rate * i), keep = 1.0;
         if (d.scaling == MMTRAIN_ROPE_LINEAR) keep = 0.0;
         else if (d.scaling == MMTRAIN_ROPE_WAVELENGTH) keep = (context * theta / two_pi - d.low) / ((double)d.high - d.low);
         else if (d.scaling == MMTRAIN_ROPE_RAMP) keep = 1.0 - (i - first) / std::max(last - first, 1e-3);

@@ -242,6 +242,44 @@ def test_join_a_gate_for_every_token_and_for_all(H):
         join_case(mm.F32, 600, H, "rms", "none", "segment", cu.astype(np.int32), flags=mm.BWD_ACCUMULATE_WGRAD, seed=8)
 
 
+def test_join_many_segments_and_many_rows():
+    cu = np.zeros(70001, dtype=np.int32)
+    cu[30000:] = 40                             # nearly all of them empty, more than a grid's second dimension takes
+    cu[69990:] = 333
+    join_case(mm.BF16, 333, 64, "layer", "rms", "segment", cu, seed=19)
+    join_case(mm.F32, 333, 64, "none", "none", "segment", cu, flags=mm.BWD_ACCUMULATE_WGRAD, seed=20)
+    # (a summand of a column passes through T / 256 additions more than the 2307 rows of the other tests: 60000 rows / 256 = 234)
+    join_case(mm.F32, 60000, 64, "rms", "layer", "channel", wanted=[], seed=21)
+
+
+def test_join_rows_past_32_bits():
+    T, H = (1 << 18) + 8, 8192                  # 2^31 elements and more
+    w = {"post_w": torch.randn(H, device="cuda").bfloat16(), "pre_w": torch.randn(H, device="cuda").bfloat16()}
+    x, b = (torch.zeros((T, H), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, b):
+        t[-8:] = torch.randn((8, H), device="cuda")
+    desc = mm.make_residual_norm_desc(mm.BF16, H, mm.NORM_RMS, mm.NORM_RMS)
+    cw = mm.make_residual_norm_weights(w)
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    st = {k: torch.empty(T, device="cuda") for k in ("post_rstd", "pre_rstd")}
+    check(mm.mmtrain_residual_norm_fwd(desc, T, None, cw, x, b, y, h, mm.make_residual_norm_stats(st)), "fwd")
+    few = [torch.empty((8, H), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    check(mm.mmtrain_residual_norm_fwd(desc, 8, None, cw, x[-8:], b[-8:], few[0], few[1]), "fwd")
+    assert torch.equal(y[-8:], few[0]) and torch.equal(h[-8:], few[1])
+    grads = {k: torch.empty(H, device="cuda") for k in w}
+    wsb = mm.mmtrain_residual_norm_workspace_bytes(desc, T)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    dx, db = torch.empty_like(x), torch.empty_like(x)
+    args = lambda n, v, o, p, q, s, g: mm.mmtrain_residual_norm_bwd(desc, n, None, cw, v, o, mm.make_residual_norm_stats(s), None, o, p, q,  # noqa: E731
+                                                                     mm.make_residual_norm_grads(g), mm.BWD_WGRAD_F32, ws, wsb)
+    check(args(T, y, b, dx, db, st, grads), "bwd")
+    some = {k: torch.empty(H, device="cuda") for k in w}
+    check(args(8, y[-8:], b[-8:], few[0], few[1], {k: v[-8:] for k, v in st.items()}, some), "bwd")
+    assert torch.equal(dx[-8:], few[0]) and torch.equal(db[-8:], few[1])
+    for k in w:                                 # the other rows' gradients are zero: the same eight summands, in another order
+        assert torch.allclose(grads[k], some[k], rtol=1e-5, atol=1e-4)
+
+
 @pytest.mark.parametrize("dtype", [mm.BF16, mm.F32])
 def test_join_other_forms(dtype):
     for pre in ("rms", "layer"):                # the norm in front of the first block: no branch
@@ -339,6 +377,18 @@ def test_grad_clip_writes_nothing_past_its_tensors():
     for a, b in ((0, 5), (8, 17), (1024, 2049)):
         touched[a:b] = True
     assert torch.all(flat[~touched] == 2.0) and torch.all(flat[touched] < 1.0)
+
+
+def test_grad_tensor_past_32_bits():
+    n = (1 << 31) + 21
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-1], g[-13], g[(1 << 31) + 1], g[0] = 3.0, 4.0, 12.0, 84.0
+    tensors = mm.make_grad_tensors([g])
+    result, q, norm, factor = norm_of(tensors, 1, 1.0)
+    assert (q, norm) == (7225.0, 85.0)
+    check(mm.mmtrain_grad_clip(tensors, result), "clip")
+    for i, v in ((-1, 3.0), (-13, 4.0), ((1 << 31) + 1, 12.0), (0, 84.0)):
+        assert abs(float(g[i]) - v / 85.0) <= 2.0 ** -8 * v / 85.0
 
 
 def test_grad_norm_extremes():

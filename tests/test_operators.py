@@ -246,6 +246,14 @@ def test_join_backward_refuses(kw, status):
     assert join_bwd(**kw) == status
 
 
+def test_join_refuses_more_segments_than_it_has_gates_for():
+    n = (1 << 20) + 1
+    cu = np.zeros(n + 1, dtype=np.int32)
+    cu[-1] = 4
+    assert join_fwd(gate=mm.GATE_SEGMENT, w=("post_w", "pre_w", "gate"), batch=pack(cu)) == mm.ERR_UNSUPPORTED
+    assert join_bwd(gate=mm.GATE_SEGMENT, w=("post_w", "pre_w", "gate"), batch=pack(cu)) == mm.ERR_UNSUPPORTED
+
+
 def test_join_takes_no_tokens():
     assert join_fwd(T=0, x=None, branch=None, y=None, h=None) == mm.OK
     assert join_bwd(T=0, y=None, branch=None, stats=None, dy=None, dh=None, dx=None, db=None, grads=None, ws=None) == mm.OK
