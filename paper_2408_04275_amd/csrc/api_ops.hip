@@ -113,20 +113,25 @@ int check_tensors(const mmtrain_grad_tensor *t, int32_t n, bool clip) {
 
 // Whether what one tensor writes is memory of another one, or of its own gradient in another place than in place
 bool outputs_overlap(const mmtrain_grad_tensor *t, int32_t n) {
-    struct Range { uintptr_t a, b; };
+    struct Range { uintptr_t a, b; bool written; };
     auto width = [](int32_t dtype) { return dtype == MMTRAIN_F32 ? 4 : 2; };
     std::vector<Range> r;
     r.reserve(2 * (size_t)n);
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].n == 0) continue;
         const uintptr_t g = (uintptr_t)t[i].grad, o = (uintptr_t)t[i].out;
-        r.push_back({g, g + (uintptr_t)t[i].n * width(t[i].dtype)});
-        if (o && o != g) r.push_back({o, o + (uintptr_t)t[i].n * width(t[i].out_dtype)});
+        const bool in_place = !o || o == g;
+        r.push_back({g, g + (uintptr_t)t[i].n * width(t[i].dtype), in_place});
+        if (!in_place) r.push_back({o, o + (uintptr_t)t[i].n * width(t[i].out_dtype), true});
     }
     auto before = [](const Range &x, const Range &y) { return x.a < y.a; };
     if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
-    for (size_t i = 1; i < r.size(); ++i)
-        if (r[i].a < r[i - 1].b) return true;
+    uintptr_t end = 0, end_written = 0;                     // of the ranges that begin before
+    for (const Range &x : r) {
+        if (x.a < (x.written ? end : end_written)) return true;
+        end = std::max(end, x.b);
+        if (x.written) end_written = std::max(end_written, x.b);
+    }
     return false;
 }
 

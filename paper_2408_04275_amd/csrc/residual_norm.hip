@@ -26,7 +26,7 @@ __device__ __forceinline__ int find_segment_wave(const int *cu, int S, int t) {
     int lo = 0, hi = S;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, at = lo + (int)(threadIdx.x & 63) * step;
-        lo += (__popcll(__ballot(at < hi && cu[min(at, S)] <= t)) - 1) * step;         // (cu[lo] <= t always)
+        lo += max(__popcll(__ballot(at < hi && cu[min(at, S)] <= t)) - 1, 0) * step;    // (cu[lo] <= t always)
         hi = min(hi, lo + step);
     }
     return lo;
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
         if constexpr (GATE) {
             if (by_segment) {
                 seg = find_segment_wave(a.cu, a.S, start);
-                end = min(r1, a.cu[seg + 1]);
+                end = min(r1, max(a.cu[seg + 1], start + 1));  // (goes on whatever the boundaries in memory are)
                 if (start + grp >= end) forget();           // a row of the next segment: requested again in its turn
 #pragma unroll
                 for (int i = 0; i < MC; ++i)
@@ -555,7 +555,7 @@ __global__ __launch_bounds__(256) void join_sums_kernel(ReduceJobSet set, GateSu
         const int s = find_segment(g.cu, g.S, r1 - 1), b0 = g.cu[s], b1 = g.cu[s + 1];
         goes_on = b0 >= r0 && b1 > r1;
         const int q = g.T / g.blocks, longer = g.T % g.blocks, t = b1 - 1;      // the workgroup of row t
-        mine = make_int4(s, 2 * tid + (b0 > r0), tid + 1, t < longer * (q + 1) ? t / (q + 1) : longer + (t - longer * (q + 1)) / q);
+        mine = make_int4(s, 2 * tid + (b0 > r0), tid + 1, min(t < longer * (q + 1) ? t / (q + 1) : longer + (t - longer * (q + 1)) / q, g.blocks - 1));
     }
     const unsigned long long set_lanes = __ballot(goes_on);
     if ((tid & 63) == 0) waves[tid >> 6] = __popcll(set_lanes);

@@ -379,6 +379,16 @@ def test_grad_clip_writes_nothing_past_its_tensors():
     assert torch.all(flat[~touched] == 2.0) and torch.all(flat[touched] < 1.0)
 
 
+def test_grad_clip_one_gradient_into_two_places():
+    g = grads_of([1000], (mm.F32,), seed=5)[0]
+    outs = [torch.empty(1000, device="cuda"), torch.empty(500, device="cuda", dtype=torch.bfloat16)]
+    result, *_ , factor = norm_of(mm.make_grad_tensors([g]), 1, 1.0)
+    check(mm.mmtrain_grad_clip(mm.make_grad_tensors([g, g[:500]], outs), result), "clip")
+    ref = host(g) * factor
+    close("fp32", outs[0], ref, np.abs(ref), 3, mm.F32)
+    close("bf16", outs[1], ref[:500], np.abs(ref[:500]), 3, mm.BF16)
+
+
 def test_grad_tensor_past_32_bits():
     n = (1 << 31) + 21
     g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
