@@ -135,10 +135,10 @@ bool outputs_overlap(const mmtrain_grad_tensor *t, int32_t n) {
     return false;
 }
 
-// The tensors in batches of GRAD_BATCH, each handed to launch(); empty tensors are left out
-template <typename F>
-int for_batches(const mmtrain_grad_tensor *t, int32_t n, F launch) {
-    GradBatch b;
+// The tensors in batches of N, each handed to launch(); empty tensors are left out
+template <int N, typename F>
+int for_batches_of(const mmtrain_grad_tensor *t, int32_t n, F launch) {
+    GradBatch<N> b;
     b.count = 0;
     for (int32_t k = 0; k < n; ++k) {
         const mmtrain_grad_tensor &g = t[k];
@@ -148,7 +148,7 @@ int for_batches(const mmtrain_grad_tensor *t, int32_t n, F launch) {
         b.n[i] = g.n;
         b.in_f32[i] = g.dtype == MMTRAIN_F32;
         b.out_f32[i] = (g.out ? g.out_dtype : g.dtype) == MMTRAIN_F32;
-        if (b.count < GRAD_BATCH) continue;
+        if (b.count < N) continue;
         grad_chunks(b);
         HIP_TRY(launch(b));
         b.count = 0;
@@ -158,6 +158,11 @@ int for_batches(const mmtrain_grad_tensor *t, int32_t n, F launch) {
         HIP_TRY(launch(b));
     }
     return MMTRAIN_OK;
+}
+
+template <typename F>
+int for_batches(const mmtrain_grad_tensor *t, int32_t n, F launch) {
+    return n <= GRAD_FEW ? for_batches_of<GRAD_FEW>(t, n, launch) : for_batches_of<GRAD_BATCH>(t, n, launch);
 }
 
 }  // namespace
@@ -285,7 +290,7 @@ int mmtrain_grad_norm(const mmtrain_grad_tensor *tensors, int32_t n_tensors, flo
     hipStream_t st = (hipStream_t)hip_stream;
     double *part = (double *)workspace;
     int parts = 0;
-    rc = for_batches(tensors, n_tensors, [&](const GradBatch &b) {
+    rc = for_batches(tensors, n_tensors, [&](const auto &b) {
         const hipError_t e = grad_sum_sq(b, part + parts, st);
         parts += grad_norm_blocks(b);
         return e;
@@ -306,7 +311,7 @@ int mmtrain_grad_clip(const mmtrain_grad_tensor *tensors, int32_t n_tensors, con
     }
     size_t written = 0;
     for (int32_t i = 0; i < n_tensors; ++i) written += (size_t)tensors[i].n * ((tensors[i].out ? tensors[i].out_dtype : tensors[i].dtype) == MMTRAIN_F32 ? 4 : 2);
-    return for_batches(tensors, n_tensors, [&](const GradBatch &b) {
+    return for_batches(tensors, n_tensors, [&](const auto &b) {
         return grad_clip(b, reinterpret_cast<const GradResult *>(result), grad_clip_streams(written), (hipStream_t)hip_stream);
     });
 }

@@ -14,7 +14,7 @@ namespace mmt {
 namespace {
 
 // the tensor that holds chunk k
-__device__ __forceinline__ int tensor_of(const GradBatch &b, int k) {
+template <int N> __device__ __forceinline__ int tensor_of(const GradBatch<N> &b, int k) {
     int lo = 0, hi = b.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -75,7 +75,7 @@ template <typename T> __device__ __forceinline__ void add_squares(const T *p, in
     });
 }
 
-__global__ __launch_bounds__(256) void grad_sum_sq_kernel(GradBatch b, double *part) {
+template <int N> __global__ __launch_bounds__(256) void grad_sum_sq_kernel(GradBatch<N> b, double *part) {
     __shared__ double red[4];
     double q[2] = {0.0, 0.0};
     for (int k = blockIdx.x; k < b.first[b.count]; k += gridDim.x) {
@@ -118,8 +118,8 @@ template <bool STREAM, typename T, typename O> __device__ __forceinline__ void s
     }, [&](int e) { Elem<O>::store(o + e, f * Elem<T>::load(p + e)); });
 }
 
-template <bool STREAM>
-__global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch b, const GradResult *result) {
+template <bool STREAM, int N>
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch<N> b, const GradResult *result) {
     float f = result->factor;
     const bool keep = f != f || f == 1.f;
     if (keep) f = 1.f;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch b, const GradR
 
 // Chunks of 2048 elements (one or two accesses a thread) as long as there are workgroups for them, up to 16384; longer ones only where their number
 // would leave 32 bits
-void grad_chunks(GradBatch &b) {
+template <int N> void grad_chunks(GradBatch<N> &b) {
     long total = 0;
     for (int i = 0; i < b.count; ++i) total += b.n[i];
     long chunk = std::min(std::max((total / GRAD_BLOCKS + 2047) / 2048 * 2048, 2048l), 16384l);
@@ -155,10 +155,10 @@ void grad_chunks(GradBatch &b) {
     b.first[b.count] = (int)first;
 }
 
-int grad_norm_blocks(const GradBatch &b) { return std::min(b.first[b.count], GRAD_BLOCKS); }
+template <int N> int grad_norm_blocks(const GradBatch<N> &b) { return std::min(b.first[b.count], GRAD_BLOCKS); }
 
-hipError_t grad_sum_sq(const GradBatch &b, double *part, hipStream_t st) {
-    grad_sum_sq_kernel<<<grad_norm_blocks(b), 256, 0, st>>>(b, part);
+template <int N> hipError_t grad_sum_sq(const GradBatch<N> &b, double *part, hipStream_t st) {
+    grad_sum_sq_kernel<N><<<grad_norm_blocks(b), 256, 0, st>>>(b, part);
     return hipGetLastError();
 }
 
@@ -173,10 +173,19 @@ hipError_t grad_norm_finish(const double *part, int n, float max_norm, bool add,
 // 738 -> 690.  In place there is no difference.
 bool grad_clip_streams(size_t bytes_written) { return bytes_written >= (size_t)384 << 20; }
 
-hipError_t grad_clip(const GradBatch &b, const GradResult *result, bool stream, hipStream_t st) {
-    if (stream) grad_clip_kernel<true><<<grad_norm_blocks(b), 256, 0, st>>>(b, result);
-    else grad_clip_kernel<false><<<grad_norm_blocks(b), 256, 0, st>>>(b, result);
+template <int N> hipError_t grad_clip(const GradBatch<N> &b, const GradResult *result, bool stream, hipStream_t st) {
+    if (stream) grad_clip_kernel<true, N><<<grad_norm_blocks(b), 256, 0, st>>>(b, result);
+    else grad_clip_kernel<false, N><<<grad_norm_blocks(b), 256, 0, st>>>(b, result);
     return hipGetLastError();
 }
+
+#define INSTANTIATE(N) \
+    template void grad_chunks(GradBatch<N> &); \
+    template int grad_norm_blocks(const GradBatch<N> &); \
+    template hipError_t grad_sum_sq(const GradBatch<N> &, double *, hipStream_t); \
+    template hipError_t grad_clip(const GradBatch<N> &, const GradResult *, bool, hipStream_t);
+INSTANTIATE(GRAD_BATCH)
+INSTANTIATE(GRAD_FEW)
+#undef INSTANTIATE
 
 }  // namespace mmt

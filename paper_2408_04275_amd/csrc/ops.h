@@ -45,23 +45,24 @@ int join_bwd_blocks(int T, int H);
 hipError_t join_bwd(int dtype, const JoinArgs &a, hipStream_t st);
 
 // grad_norm.hip
-constexpr int GRAD_BATCH = 128;     // tensors a launch
-struct GradBatch {
-    const void *in[GRAD_BATCH];
-    void *out[GRAD_BATCH];
-    long n[GRAD_BATCH];
-    int first[GRAD_BATCH + 1];      // first chunk of each tensor; [count] = all
-    unsigned char in_f32[GRAD_BATCH], out_f32[GRAD_BATCH];
+constexpr int GRAD_BATCH = 128, GRAD_FEW = 16;      // tensors a launch; at most so many go as a smaller argument
+template <int N> struct GradBatch {
+    const void *in[N];
+    void *out[N];
+    long n[N];
+    int first[N + 1];               // first chunk of each tensor; [count] = all
+    unsigned char in_f32[N], out_f32[N];
     int count, chunk;               // elements a chunk, a multiple of 8
+    static constexpr int size = N;
 };
 constexpr int GRAD_BLOCKS = 2048;   // workgroups, and partial sums, of a launch at most: eight of 256 threads on each compute unit
 struct GradResult { double sum_sq; float norm, factor; };
-// Cuts a batch whose in, out, n, types and count are set into chunks (first, chunk)
-void grad_chunks(GradBatch &b);
-int grad_norm_blocks(const GradBatch &b);
-hipError_t grad_sum_sq(const GradBatch &b, double *part, hipStream_t st);
+// For GRAD_BATCH and GRAD_FEW.  grad_chunks cuts a batch whose in, out, n, types and count are set into chunks (first, chunk).
+template <int N> void grad_chunks(GradBatch<N> &b);
+template <int N> int grad_norm_blocks(const GradBatch<N> &b);
+template <int N> hipError_t grad_sum_sq(const GradBatch<N> &b, double *part, hipStream_t st);
 hipError_t grad_norm_finish(const double *part, int n, float max_norm, bool add, GradResult *result, hipStream_t st);
 bool grad_clip_streams(size_t bytes_written);       // by a whole call
-hipError_t grad_clip(const GradBatch &b, const GradResult *result, bool stream, hipStream_t st);
+template <int N> hipError_t grad_clip(const GradBatch<N> &b, const GradResult *result, bool stream, hipStream_t st);
 
 }  // namespace mmt
