@@ -128,11 +128,6 @@ template <int G, int MC, int NT> struct RowSum {
     }
 };
 
-// A parameter's chunk as loaded: keeps the compiler from holding it widened to fp32 over the whole loop, twice the registers in bf16.  For the
-// kernels that would spill otherwise (9000 x 8192, two LayerNorms and a gate, 295 -> 243 us); the others are slower for it (two RMSNorms 192 -> 214).
-__device__ __forceinline__ void as_loaded(Raw8<bf16_t> &r) { asm("" : "+v"(r.a.x), "+v"(r.a.y), "+v"(r.a.z), "+v"(r.a.w)); }
-__device__ __forceinline__ void as_loaded(Raw8<float> &) {}
-
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 __device__ __forceinline__ f32x4 load4(const bf16_t *p) {
     const u32x2 r = *reinterpret_cast<const u32x2 *>(p);
@@ -147,7 +142,7 @@ template <typename T> __device__ __forceinline__ void zero8(Raw8<T> &r) { __buil
 template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd_kernel(JoinArgs a) {
     constexpr int R = NT / G;
-    constexpr bool IN_LDS = LN && MC > 1 && G > 256 && sizeof(T) == 2, TIGHT = LN && MC > 1 && !IN_LDS;
+    constexpr bool IN_LDS = LN && MC > 1 && G > 256 && sizeof(T) == 2;
     __shared__ float2 red[2][NT / 64];
     // a wavefront has one row's columns: rows are scalars, and addresses a scalar and a column
     const int lane = threadIdx.x % G, grp = __builtin_amdgcn_readfirstlane(threadIdx.x / G), H = a.H;
@@ -171,8 +166,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
     };
     auto kept = [&](Raw8<T> *held, int slot, int i) {
         if constexpr (IN_LDS) return *reinterpret_cast<const Raw8<T> *>(&parked[slot][col(i)]);
-        if constexpr (TIGHT) as_loaded(held[i]);
-        return held[i];
+        else return held[i];
     };
 #pragma unroll
     for (int i = 0; i < MC; ++i) { zero8(nx[i]); zero8(nb[i]); }
@@ -238,10 +232,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
                 float g[8];
-                if constexpr (GATE) {
-                    if constexpr (TIGHT) as_loaded(gt[i]);
-                    unpack8(gt[i], g);
-                }
+                if constexpr (GATE) unpack8(gt[i], g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[i][j] = a.alpha * v[i][j] + a.beta * (GATE ? g[j] * n[i][j] : n[i][j]);
                 if (valid && inside(i)) store8((T *)a.y + (size_t)row * H + col(i), v[i]);
@@ -271,8 +262,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && MC > 1 ? 4 : 1) void join_fwd
 template <typename T, int G, int MC, int NT, bool LN, bool GATE, bool POST>
 __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     constexpr int R = NT / G, W = G * MC * 8;
-    constexpr bool SUM_A = POST || GATE, SUM_B = LN && POST, HEAVY = LN && GATE && POST;
-    constexpr bool IN_LDS = LN && POST && MC > 1 && (GATE || sizeof(T) == 4), TIGHT = HEAVY && NT > 512;
+    constexpr bool SUM_A = POST || GATE, SUM_B = LN && POST;
+    constexpr bool IN_LDS = LN && POST && MC > 1 && (GATE || sizeof(T) == 4);
     __shared__ float2 red[2][NT / 64];
     __shared__ __attribute__((aligned(16))) float comb[LN ? 2 : 1][R > 1 ? R : 1][R > 1 ? W : 4];
     __shared__ __attribute__((aligned(16))) float total_w[GATE && POST ? W : 4], total_b[GATE && SUM_B ? W : 4];
@@ -284,8 +275,8 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     auto col = [&](int i) { return (lane + i * G) * 8; };
     auto inside = [&](int i) { return col(i) < H; };
     const float alpha = a.b ? a.alpha : 1.f;
-    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill more otherwise (9000 rows of 8192 in fp32, two LayerNorms and
-    // a gate: 485 -> 394 us)
+    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill otherwise (9000 rows of 8192 in fp32, two LayerNorms and
+    // a gate: 645 -> 420 us)
     __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 2 : 1][IN_LDS ? W : 8];
     constexpr int HELD = IN_LDS ? 1 : MC;
     Raw8<T> pdy[MC], pdh[MC], py[MC], pb[MC], w1[HELD], w2[POST ? HELD : 1], gt[GATE ? MC : 1];
@@ -299,8 +290,7 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     };
     auto kept = [&](Raw8<T> *held, int slot, int i) {
         if constexpr (IN_LDS) return *reinterpret_cast<const Raw8<T> *>(&parked[slot][col(i)]);
-        if constexpr (TIGHT) as_loaded(held[i]);
-        return held[i];
+        else return held[i];
     };
     float s_pre_w[MC][8] = {}, s_pre_b[LN ? MC : 1][8] = {}, sum_a[MC][8] = {}, sum_b[LN ? MC : 1][8] = {};
     float pr = 0.f, pmu = 0.f, pr2 = 0.f, pmu2 = 0.f;
@@ -429,10 +419,7 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
 #pragma unroll
             for (int i = 0; i < MC; ++i) {
                 float g[8], w[8], dx[8];
-                if constexpr (GATE) {
-                    if constexpr (HEAVY && (MC > 1 || NT > 512)) as_loaded(gt[i]);
-                    unpack8(gt[i], g);
-                }
+                if constexpr (GATE) unpack8(gt[i], g);
                 if constexpr (POST) unpack8(kept(w2, 1, i), w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -640,9 +627,9 @@ hipError_t fwd_by_width(const JoinArgs &a, hipStream_t st) {
     return ln ? launch_fwd<T, 512, 2, 512, true>(a, st) : launch_fwd<T, 1024, 1, 1024, false>(a, st);
 #undef L
 }
-// Backward, where a workgroup has the compute unit to itself: as many threads as have the registers.  Two RMSNorms / two LayerNorms and a gate, bf16: 1024 (128, 1)
-// 27.7 / 43.5, (64, 2) 27.1 / 49.5 (fp32 / 68, / 100: it spills); 1280 768 threads 31.5 / 50.6, 576 threads 42.7 / 54.4; 4096 (512, 1) 97.6 / 133, (256, 2) 96.8 / 151;
-// 8192 (512, 2) 192 / 295, (1024, 1) 192 / 494.
+// Backward, where a workgroup has the compute unit to itself: as many threads as have the registers.  9000 bf16 rows, two RMSNorms / two LayerNorms and a gate
+// per segment, us: 1024 (128, 1) 26.8 / 34.0, (64, 2) 27.2 / 35.3 (in fp32 55 / 62, 55 / 79: it spills); 1280 768 threads a workgroup 31.5 / 39.2, 576 31.8 / 40.9; 4096
+// (512, 1) 98.1 / 110, (256, 2) 97.0 / 110 (fp32 186 / 198, 188 / 214); 5120 (640, 1) 118 / 130, (384, 2) 119 / 134; 8192 (512, 2) 192 / 211, (1024, 1) 192 / 622.
 template <typename T>
 hipError_t bwd_by_width(const JoinArgs &a, hipStream_t st) {
     if (a.H <= 64 * 8) return launch_bwd<T, 64, 1, 512>(a, st);
