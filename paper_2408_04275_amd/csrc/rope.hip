@@ -53,7 +53,9 @@ struct RopeShape {
 template <typename T, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_heads_kernel(RopeArgs a, RopeShape s) {
     extern __shared__ float2 turned[];                       // [tile][half]: cosine, sine
-    const int t0 = blockIdx.x * s.tile, tokens = min(s.tile, a.T - t0);
+    const long first = (blockIdx.y * (long)gridDim.x + blockIdx.x) * s.tile;
+    if (first >= a.T) return;
+    const int t0 = (int)first, tokens = min(s.tile, a.T - t0);
     const int u = threadIdx.x % s.units, g = threadIdx.x / s.units;
     const bool rotates = u < s.rot_units;
     constexpr bool SINGLE = INTERLEAVED && V == 1;
@@ -128,9 +130,11 @@ hipError_t launch(const RopeArgs &a, hipStream_t st) {
     const int by_units = (511 + a.heads * s.units) / (a.heads * s.units), by_angles = 1024 / a.half, by_tokens = a.T / 512;
     s.tile = std::max(1, std::min({by_units, by_angles, by_tokens}));
     const size_t lds = (size_t)s.tile * a.half * sizeof(float2);
+    // a grid's first dimension ends at 2^32 threads
     const int blocks = ceil_div(a.T, s.tile);
-    if (a.interleaved) rope_heads_kernel<T, V, true><<<blocks, 256, lds, st>>>(a, s);
-    else rope_heads_kernel<T, V, false><<<blocks, 256, lds, st>>>(a, s);
+    const dim3 grid(std::min(blocks, 1 << 20), ceil_div(blocks, 1 << 20));
+    if (a.interleaved) rope_heads_kernel<T, V, true><<<grid, 256, lds, st>>>(a, s);
+    else rope_heads_kernel<T, V, false><<<grid, 256, lds, st>>>(a, s);
     return hipGetLastError();
 }
 

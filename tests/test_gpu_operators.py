@@ -133,6 +133,23 @@ def test_rope_rows_past_32_bits():
     assert all(torch.equal(x[t * ld:t * ld + 256], out[t]) for t in range(T))
 
 
+@pytest.mark.parametrize("T", [(1 << 20) + 5, (1 << 24) + 5])
+def test_rope_of_more_tokens_than_a_grid_has_workgroups(T):
+    # a token a workgroup, and more than 2^32 threads
+    x = torch.zeros((T, 1024), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, T // 2, T - 2, T - 1], device="cuda")
+    rows = torch.randn((7, 1024), device="cuda").bfloat16()
+    x[at] = rows
+    desc = mm.make_rope_desc(mm.BF16, 512, 2)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    check(mm.mmtrain_rope(desc, T, None, pos, x, 1024, x, 1024), "mmtrain_rope")
+    out = torch.empty_like(rows)
+    check(mm.mmtrain_rope(desc, 7, None, at.int(), rows, 1024, out, 1024), "mmtrain_rope")
+    assert torch.equal(x[at], out)
+    x[at] = 0
+    assert not any(bool(p.any()) for p in x.split(1 << 20))
+
+
 def test_rope_special_values_stay_in_their_pair():
     x = torch.zeros((1, 16), dtype=torch.float32, device="cuda")
     x[0, 3], x[0, 6] = float("inf"), float("nan")
