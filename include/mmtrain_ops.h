@@ -74,7 +74,8 @@ MMTRAIN_API int mmtrain_rope(const mmtrain_rope_desc *desc, int32_t n_tokens, co
  * Without a branch (branch and y NULL, post_norm and gate NONE) h = norm_pre(x): the norm in front of the first block.
  * h is computed from y before y is rounded to the storage type.  Means and reciprocal deviations ([n_tokens] fp32 each) are
  * kept for the backward pass, which reads y, branch and them.
- * Supported: hidden a multiple of 8, at most 8192, and at most 2^20 segments with a SEGMENT gate; anything else: MMTRAIN_ERR_UNSUPPORTED.
+ * Supported: hidden a multiple of 8, at most 8192, at most 2^30 tokens, and at most 2^20 segments with a SEGMENT gate; anything else:
+ * MMTRAIN_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------ */
 typedef enum { MMTRAIN_NORM_NONE = 0, MMTRAIN_NORM_RMS = 1, MMTRAIN_NORM_LAYER = 2 } mmtrain_norm_kind;
 typedef enum { MMTRAIN_GATE_NONE = 0, MMTRAIN_GATE_CHANNEL = 1, MMTRAIN_GATE_SEGMENT = 2 } mmtrain_gate_kind;

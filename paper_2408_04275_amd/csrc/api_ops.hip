@@ -57,6 +57,7 @@ int join_common(const mmtrain_residual_norm_desc *d, int32_t T, const mmtrain_ba
     int rc = check_join(d);
     if (rc) return rc;
     if (T < 0 || !w) return MMTRAIN_ERR_INVALID_ARG;
+    if (T > JOIN_MAX_ROWS) return MMTRAIN_ERR_UNSUPPORTED;
     a = JoinArgs{};
     a.T = T; a.H = d->hidden; a.post = d->post_norm; a.pre = d->pre_norm; a.gate = d->gate;
     a.post_eps = d->post_eps; a.pre_eps = d->pre_eps; a.alpha = d->residual_scale; a.beta = d->branch_scale;

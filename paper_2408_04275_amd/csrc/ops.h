@@ -38,6 +38,7 @@ struct JoinArgs {
     void *d_post_w, *d_post_b, *d_gate, *d_pre_w, *d_pre_b;     // the gradients, null where not wanted
     int grad_f32, accumulate;       // their type, and whether they are added to
 };
+constexpr int JOIN_MAX_ROWS = 1 << 30;          // a row and the next ones' numbers fit an int
 constexpr int JOIN_MAX_SEGMENTS = 1 << 20;      // with a segment gate: [segments][H] are the gates alone
 hipError_t join_fwd(int dtype, const JoinArgs &a, hipStream_t st);
 // workgroups of the backward kernel: never fewer for more rows

@@ -246,6 +246,12 @@ def test_join_backward_refuses(kw, status):
     assert join_bwd(**kw) == status
 
 
+def test_join_refuses_more_rows_than_it_counts():
+    for T in ((1 << 30) + 1, (1 << 31) - 1):
+        assert join_fwd(T=T) == mm.ERR_UNSUPPORTED
+        assert join_bwd(T=T) == mm.ERR_UNSUPPORTED
+
+
 def test_join_refuses_more_segments_than_it_has_gates_for():
     n = (1 << 20) + 1
     cu = np.zeros(n + 1, dtype=np.int32)
