@@ -30,7 +30,7 @@ extern "C" {
  *                 their frequency, pairs that turn less than `low` times are stretched
  *     RAMP        the same with w_i = 1 - clamp((i - i_high) / (i_low - i_high), 0, 1), linear in the pair's index: i_high and i_low
  *                 are the (real) indices at which a pair would turn `high` and `low` times, rounded down and up and limited to
- *                 0 .. rot_dim - 1
+ *                 0 .. rot_dim - 1 (a difference below 0.001 counts as 0.001)
  * Angles are formed in fp64 and reduced to one turn before they are rounded; products in fp32, one rounding at the end.
  * ------------------------------------------------------------------------ */
 typedef enum { MMTRAIN_ROPE_HALF = 0, MMTRAIN_ROPE_INTERLEAVED = 1 } mmtrain_rope_layout;
@@ -122,7 +122,7 @@ MMTRAIN_API int mmtrain_residual_norm_bwd(const mmtrain_residual_norm_desc *desc
  * Global gradient norm over many tensors, and clipping.  The norm and the factor stay on the device: nothing waits for the
  * host, and the calls may be captured.
  *     sum_sq = sum over all tensors of g^2 (fp64),   norm = sqrt(sum_sq),   factor = norm > max_norm ? max_norm / norm : 1
- * A norm that is not finite gives the factor NaN, which stands for "leave everything as it is": mmtrain_grad_clip then writes
+ * A norm that is not finite as fp32 gives the factor NaN, which stands for "leave everything as it is": mmtrain_grad_clip then writes
  * the gradients unscaled, mmtrain_adam_step_clipped skips the step.
  * ------------------------------------------------------------------------ */
 typedef struct {

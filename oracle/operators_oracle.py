@@ -142,6 +142,6 @@ def grad_norm(grads, max_norm, start=0.0):
     """(sum of squares, norm, factor) of a list of arrays; start: a sum of squares to add to."""
     q = start + sum(float(np.sum(np.asarray(g, F64) ** 2)) for g in grads)
     norm = float(np.sqrt(q))
-    if not np.isfinite(norm):
+    if not norm <= np.finfo(np.float32).max:              # the norm is handed out in fp32
         return q, norm, float("nan")
     return q, norm, max_norm / norm if norm > max_norm else 1.0

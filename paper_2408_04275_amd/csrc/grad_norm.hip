@@ -99,7 +99,7 @@ __global__ __launch_bounds__(1024) void grad_norm_finish_kernel(const double *pa
     const double norm = sqrt(q);
     result->sum_sq = q;
     result->norm = (float)norm;
-    result->factor = !(norm < INFINITY) ? NAN : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+    result->factor = !((float)norm < INFINITY) ? NAN : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
 }
 
 // A wavefront's stores cover whole lines: 16 bytes per lane of the wider type

@@ -433,6 +433,16 @@ def test_grad_norm_extremes():
     assert norm_of(mm.make_grad_tensors([one]), 1, 4.0)[3] == 1.0 and norm_of(mm.make_grad_tensors([one]), 1, 0.0)[3] == 0.0
 
 
+def test_grad_norm_past_fp32_leaves_everything_alone():
+    # what the norm says and what is done agree: 1000 x 3e38^2 is a finite sum, its root no fp32 number
+    g = torch.full((1000,), 3e38, device="cuda")
+    result, q, norm, factor = norm_of(mm.make_grad_tensors([g]), 1, 1.0)
+    assert np.isfinite(q) and norm == np.inf and np.isnan(factor)
+    before = g.clone()
+    check(mm.mmtrain_grad_clip(mm.make_grad_tensors([g]), result), "clip")
+    assert torch.equal(g, before)
+
+
 def test_grad_norm_adds_up_calls_and_ranks():
     a, b = grads_of([5000], (mm.F32,), seed=1)[0], grads_of([3001], (mm.BF16,), seed=2)[0]
     q, norm, factor = oo.grad_norm([host(a), host(b)], 1.0)
