@@ -4,7 +4,6 @@
 #include "api_checks.h"
 #include <algorithm>
 #include <cmath>
-#include <vector>
 
 using namespace mmt;
 
@@ -112,26 +111,105 @@ int check_tensors(const mmtrain_grad_tensor *t, int32_t n, bool clip) {
     return MMTRAIN_OK;
 }
 
-// Whether what one tensor writes is memory of another one, or of its own gradient in another place than in place
-bool outputs_overlap(const mmtrain_grad_tensor *t, int32_t n) {
-    struct Range { uintptr_t a, b; bool written; };
-    auto width = [](int32_t dtype) { return dtype == MMTRAIN_F32 ? 4 : 2; };
-    std::vector<Range> r;
-    r.reserve(2 * (size_t)n);
-    for (int32_t i = 0; i < n; ++i) {
-        if (t[i].n == 0) continue;
-        const uintptr_t g = (uintptr_t)t[i].grad, o = (uintptr_t)t[i].out;
-        const bool in_place = !o || o == g;
-        r.push_back({g, g + (uintptr_t)t[i].n * width(t[i].dtype), in_place});
-        if (!in_place) r.push_back({o, o + (uintptr_t)t[i].n * width(t[i].out_dtype), true});
-    }
-    auto before = [](const Range &x, const Range &y) { return x.a < y.a; };
-    if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
-    uintptr_t end = 0, end_written = 0;                     // of the ranges that begin before
-    for (const Range &x : r) {
-        if (x.a < (x.written ? end : end_written)) return true;
+// ---- whether what one tensor writes is memory of another one, or of its own gradient in another place than in place ----
+struct Range { uintptr_t a, b; bool written; };
+
+// A tensor's gradient, and behind it what is written in another place
+int ranges_of(const mmtrain_grad_tensor &t, Range *r) {
+    if (t.n == 0) return 0;
+    auto end = [&](uintptr_t p, int32_t dtype) { return p + (uintptr_t)t.n * (dtype == MMTRAIN_F32 ? 4 : 2); };
+    const uintptr_t g = (uintptr_t)t.grad, o = (uintptr_t)t.out;
+    const bool in_place = !o || o == g;
+    r[0] = {g, end(g, t.dtype), in_place};
+    if (in_place) return 1;
+    r[1] = {o, end(o, t.out_dtype), true};
+    return 2;
+}
+
+// Ranges in the order of their beginnings: whether one meets a range before it, one of the two written
+struct Sweep {
+    uintptr_t end = 0, end_written = 0;                     // of the ranges so far
+    bool meets(const Range &x) {
+        const bool hit = x.a < (x.written ? end : end_written);
         end = std::max(end, x.b);
         if (x.written) end_written = std::max(end_written, x.b);
+        return hit;
+    }
+};
+
+// Nothing is allocated.  Lists whose gradients stand in address order, and whose outputs do (parts of flat buffers), are merged as they are.  Others are
+// sorted on the stack: in one piece where their ranges fit, else two parts of half as many at a time, every part beside every other.  us on the host, in order /
+// shuffled: 288 tensors 3.4 / 10.8 (a list of the ranges on the heap: 10.6 / 13.4), 2000 25 / 258 (94 / 288), 10000 194 / 4160 (1166 / 1507).
+constexpr int OVERLAP_RANGES = 8192;        // 128 KB
+
+bool in_address_order(const mmtrain_grad_tensor *t, int32_t n) {
+    uintptr_t last[2] = {0, 0};
+    for (int32_t i = 0; i < n; ++i) {
+        Range r[2];
+        for (int k = 0, m = ranges_of(t[i], r); k < m; ++k) {
+            if (r[k].a < last[k]) return false;
+            last[k] = r[k].a;
+        }
+    }
+    return true;
+}
+
+bool ordered_overlap(const mmtrain_grad_tensor *t, int32_t n) {
+    Sweep sweep;
+    int32_t i = 0, j = 0;                                   // next gradient, next output in another place
+    for (;;) {
+        Range g[2], o[2];
+        while (i < n && ranges_of(t[i], g) == 0) ++i;
+        while (j < n && ranges_of(t[j], o) < 2) ++j;
+        if (i >= n && j >= n) return false;
+        const bool gradient = j >= n || (i < n && g[0].a <= o[1].a);
+        if (sweep.meets(gradient ? g[0] : o[1])) return true;
+        ++(gradient ? i : j);
+    }
+}
+
+// The ranges of tensors [first, last) in the order of their beginnings: 2 (tensor - first), and 1 more for an output
+struct Begin { uintptr_t a; uint32_t which; };
+
+int sorted_ranges(const mmtrain_grad_tensor *t, int64_t first, int64_t last, Begin *order) {
+    int count = 0;
+    for (int64_t i = first; i < last; ++i) {
+        Range r[2];
+        for (int k = 0, m = ranges_of(t[i], r); k < m; ++k) order[count++] = {r[k].a, (uint32_t)(2 * (i - first) + k)};
+    }
+    std::sort(order, order + count, [](const Begin &x, const Begin &y) { return x.a < y.a; });
+    return count;
+}
+
+Range range(const mmtrain_grad_tensor *t, int64_t first, const Begin &x) {
+    Range r[2];
+    ranges_of(t[first + x.which / 2], r);
+    return r[x.which & 1];
+}
+
+bool outputs_overlap(const mmtrain_grad_tensor *t, int32_t n) {
+    if (in_address_order(t, n)) return ordered_overlap(t, n);
+    Begin order[OVERLAP_RANGES];
+    if (n <= OVERLAP_RANGES / 2) {
+        const int count = sorted_ranges(t, 0, n, order);
+        Sweep sweep;
+        for (int i = 0; i < count; ++i)
+            if (sweep.meets(range(t, 0, order[i]))) return true;
+        return false;
+    }
+    constexpr int PART = OVERLAP_RANGES / 4;                // tensors
+    Begin *other = order + OVERLAP_RANGES / 2;
+    for (int64_t p = 0; p + PART < n; p += PART) {
+        const int mine = sorted_ranges(t, p, p + PART, order);
+        for (int64_t q = p + PART; q < n; q += PART) {      // (a part's own ranges meet beside any other part)
+            const int theirs = sorted_ranges(t, q, std::min<int64_t>(q + PART, n), other);
+            Sweep sweep;
+            for (int i = 0, j = 0; i < mine || j < theirs;) {
+                const bool first = j >= theirs || (i < mine && order[i].a <= other[j].a);
+                if (sweep.meets(first ? range(t, p, order[i]) : range(t, q, other[j]))) return true;
+                ++(first ? i : j);
+            }
+        }
     }
     return false;
 }
@@ -305,11 +383,7 @@ int mmtrain_grad_clip(const mmtrain_grad_tensor *tensors, int32_t n_tensors, con
     int rc = check_tensors(tensors, n_tensors, true);
     if (rc) return rc;
     if (!result || misaligned({result})) return MMTRAIN_ERR_INVALID_ARG;
-    try {
-        if (outputs_overlap(tensors, n_tensors)) return MMTRAIN_ERR_INVALID_ARG;
-    } catch (...) {                             // no host memory for the list of ranges
-        return MMTRAIN_ERR_HIP;
-    }
+    if (outputs_overlap(tensors, n_tensors)) return MMTRAIN_ERR_INVALID_ARG;
     size_t written = 0;
     for (int32_t i = 0; i < n_tensors; ++i) written += (size_t)tensors[i].n * ((tensors[i].out ? tensors[i].out_dtype : tensors[i].dtype) == MMTRAIN_F32 ? 4 : 2);
     return for_batches(tensors, n_tensors, [&](const auto &b) {

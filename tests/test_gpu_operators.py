@@ -507,3 +507,22 @@ def test_grad_clip_of_more_than_the_caches_hold(from_dtype, to_dtype):
     got = g if out is None else out[:n]
     want = (before.float() * result.view(torch.float32)[3]).to(got.dtype)      # one fp32 product, one rounding
     assert torch.equal(got, want) and (out is None or torch.all(out[n:] == 7.0))
+
+
+@pytest.mark.parametrize("n", [300, 9000])
+def test_grad_clip_takes_lists_in_any_order(n):
+    # parts of two flat buffers that share nothing, neighbours without a gap, shuffled: more than are sorted at a time, and fewer
+    rng = np.random.default_rng(n)
+    sizes = 8 * rng.integers(0, 6, size=n)
+    at = np.concatenate([[0], np.cumsum(sizes)])
+    flat = dev(rng.standard_normal(at[-1]), mm.F32)
+    before, out = flat.clone(), torch.zeros_like(flat)
+    order = rng.permutation(n)
+    parts = [slice(int(at[i]), int(at[i + 1])) for i in order]
+    elsewhere = [bool(i % 2) for i in order]
+    tensors = mm.make_grad_tensors([flat[p] for p in parts], [out[p] if e else None for p, e in zip(parts, elsewhere)])
+    result, *_, factor = norm_of(tensors, n, 1.0)
+    check(mm.mmtrain_grad_clip(tensors, result), "clip")
+    want = before * result.view(torch.float32)[3]
+    for p, e in zip(parts, elsewhere):
+        assert torch.equal((out if e else flat)[p], want[p]) and (not e or torch.equal(flat[p], before[p]))

@@ -2,6 +2,8 @@
 (all argument checks run before any HIP call)."""
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -312,6 +314,58 @@ def test_grad_clip_refuses_what_two_tensors_share():
     assert clip((A[0], A[0], 100, f, mm.BF16)) == mm.ERR_INVALID_ARG                           # in place in another type
     assert clip((A[0], A[2] + 2, 100, f, f)) == clip((A[0], A[2], 100, f, 9)) == mm.ERR_INVALID_ARG
     assert mm.mmtrain_grad_clip(None, A[3], stream=0) == mm.OK and clip((None, None, 0, f, f)) == mm.OK
+
+
+def test_grad_clip_finds_one_overlap_in_lists_of_any_order():
+    # lists below and above what is sorted at a time, in address order and shuffled; the pair that overlaps stands anywhere
+    rng = np.random.default_rng(4)
+    for n in (2, 3, 500, 4096, 4097, 9000):
+        for shuffled in (False, True):
+            for kind in range(4):
+                at = FAKE + 4096 * np.arange(3 * n)
+                if shuffled:
+                    rng.shuffle(at)
+                grads, outs = [int(a) for a in at[:n]], [int(a) if i % 2 else None for i, a in enumerate(at[n:2 * n])]
+                p, q = (int(i) for i in rng.choice(n, 2, replace=False))
+                if kind == 0:                   # a gradient that another tensor clips in place
+                    grads[p], outs[p] = grads[q] + 4080, None
+                elif kind == 1:                 # an output in another's gradient, from its last 16 bytes
+                    outs[p] = grads[q] + 4080
+                elif kind == 2:                 # two outputs
+                    outs[p] = int(at[2 * n])
+                    outs[q] = outs[p] + 16
+                else:                           # a range that holds another one, which is written
+                    outs[p], outs[q] = int(at[2 * n]) + 1024, None
+                    grads[q] = int(at[2 * n])
+                e = [(g, o, 1024, mm.F32, mm.F32) for g, o in zip(grads, outs)]
+                if kind == 3:
+                    e[p] = (grads[p], outs[p], 8, mm.F32, mm.F32)
+                assert mm.mmtrain_grad_clip(tensors(*e), A[3], stream=0) == mm.ERR_INVALID_ARG, (n, shuffled, kind)
+
+
+NO_MEMORY = """
+import resource
+import numpy as np
+from paper_2408_04275_amd import binding as mm
+n = 1 << 21
+t = np.zeros(n, dtype=[("grad", "u8"), ("out", "u8"), ("n", "i8"), ("dtype", "i4"), ("out_dtype", "i4")])
+t["grad"] = 0x100000 + 16 * np.arange(n)
+t["n"] = 4
+lib = mm.load_library()
+t["grad"][-1] = t["grad"][-2]
+shuffled = t.copy()
+shuffled["grad"][:-1] = shuffled["grad"][:-1][::-1]
+shuffled["grad"][1] = shuffled["grad"][0]
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (used + (8 << 20), resource.getrlimit(resource.RLIMIT_AS)[1]))
+print([lib.mmtrain_grad_clip(a.ctypes.data, n, 0x100000, None) for a in (t, shuffled)])
+"""
+
+
+def test_grad_clip_allocates_no_host_memory():
+    # a list of two million tensors with 8 MB left to the process: less than a list of their ranges would take
+    r = subprocess.run([sys.executable, "-c", NO_MEMORY], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert r.stdout.strip() == str([mm.ERR_INVALID_ARG] * 2), r.stdout + r.stderr
 
 
 def test_clipped_adam_refuses():
