@@ -208,8 +208,9 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        # the handle alone: building the Stream object around it takes 2.5 us, as long as a launch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the handle alone, where this torch hands it out: building the Stream object around it takes 2.5 us, as long as a launch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     return stream
 
 

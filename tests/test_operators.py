@@ -383,3 +383,9 @@ def test_binding_refuses_lists_that_do_not_fit():
             bad()
     t = mm.make_grad_tensors([g, g.bfloat16()], [None, torch.zeros(8)])
     assert (t[0].out, t[0].out_dtype, t[1].dtype, t[1].out_dtype, t[1].n) == (None, mm.F32, mm.BF16, mm.F32, 8)
+
+
+def test_binding_finds_the_current_stream_with_public_calls_alone(monkeypatch):
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: type("Stream", (), {"cuda_stream": 77}))
+    assert mm._stream(None) == 77 and mm._stream(5) == 5
