@@ -1,7 +1,7 @@
 """Plain fp64 definitions of the operators around a block's products: rotary positions, the join of a block's branch with the
 residual stream, gradient norm and clipping.
 
-The functions that end in `_mag` return, beside a result's shape, the sum of the absolute values of the terms that make it up: what
+Rotary positions and the join return, beside each result, the sum of the absolute values of the terms that make it up (`mag`): what
 an fp32 evaluation's rounding errors are proportional to, however much the terms cancel.
 """
 import numpy as np

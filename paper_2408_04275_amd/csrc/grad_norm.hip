@@ -7,7 +7,6 @@
 // Squares are added up in fp64: those of fp32 gradients leave the range of fp32 (a gradient of 1e20, or of 1e-23), and the conversions and fused
 // multiply-adds, a quarter of what the vector ALUs can do while 5 TB/s arrive, cost nothing.  Every sum has a fixed order.
 #include "ops.h"
-#include "vec8.h"
 #include <algorithm>
 
 namespace mmt {

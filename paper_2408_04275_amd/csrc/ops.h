@@ -54,7 +54,6 @@ template <int N> struct GradBatch {
     int first[N + 1];               // first chunk of each tensor; [count] = all
     unsigned char in_f32[N], out_f32[N];
     int count, chunk;               // elements a chunk, a multiple of 8
-    static constexpr int size = N;
 };
 constexpr int GRAD_BLOCKS = 2048;   // workgroups, and partial sums, of a launch at most: eight of 256 threads on each compute unit
 struct GradResult { double sum_sq; float norm, factor; };

@@ -5,6 +5,10 @@
 // registers from its first use to its last.  A row is worked on by a group of G threads with MC chunks of 8 columns each, and a
 // workgroup of NT threads walks over a contiguous range of rows, NT / G at a time, the next ones requested before the present ones are
 // reduced.  Gains, biases and gates stay in registers; so do backward's sums over tokens, which leave the workgroup as one partial row.
+// Not every instance keeps these requests on their way while it works.  Backward does in bf16; in fp32 the compiler waits inside each turn for the statistics and
+// rows just requested (4111 x 1280, two LayerNorms and segment gates 42 to 45 us for 25 us of bytes; where rows are wide it costs little, 9000 x 5120, two
+// RMSNorms 230 for 221).  Forward with one chunk a thread does without a gate; with one, per channel too, it waits for the next row where the branch that loads a
+// segment's gate joins (9000 bf16 rows of 1280, two LayerNorms: no gate 19.7 us, channel 22.7, segment 23.3; bytes 18.4).
 // 8192 rows of 4096 in bf16, two RMSNorms: forward 55 us (4.9 TB/s), backward 81 us (4.9 TB/s) and 5 us for the sums of the partial rows; a copy
 // of as many bytes runs at 5.0 to 5.4 TB/s.  Below about 2000 rows the launches and the first row's way through the chip bound both.
 #include "ops.h"
@@ -275,8 +279,9 @@ __global__ __launch_bounds__(NT) void join_bwd_kernel(JoinArgs a) {
     auto col = [&](int i) { return (lane + i * G) * 8; };
     auto inside = [&](int i) { return col(i) < H; };
     const float alpha = a.b ? a.alpha : 1.f;
-    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill otherwise (9000 rows of 8192 in fp32, two LayerNorms and
-    // a gate: 645 -> 420 us)
+    // IN_LDS: the gains wait in LDS, each thread's own, where the kernel would spill most (9000 rows of 8192 in fp32, two LayerNorms and
+    // a gate: 645 -> 420 us).  Registers that still spill, with a gate and a post norm: two LayerNorms in fp32 2, 2, 6 and 16 at 128, 192, 256 and 640 threads a row, 57
+    // at 512 with two chunks (8 without the post norm), in bf16 2 at 640; two RMSNorms in fp32 14 at 512 with two chunks.
     __shared__ __attribute__((aligned(16))) T parked[IN_LDS ? 2 : 1][IN_LDS ? W : 8];
     constexpr int HELD = IN_LDS ? 1 : MC;
     Raw8<T> pdy[MC], pdh[MC], py[MC], pb[MC], w1[HELD], w2[POST ? HELD : 1], gt[GATE ? MC : 1];
@@ -610,7 +615,8 @@ hipError_t launch_bwd(const JoinArgs &a, hipStream_t st) {
 // By width: threads a row, chunks a thread, threads a workgroup.  Few idle lanes in a row, and few enough registers for two workgroups per compute unit or
 // more, so that one's sums go on beside another's loads.  9000 bf16 rows forward, two RMSNorms / two LayerNorms and a gate, us, the row's class against the
 // next best: 1024 (128, 1) 15.0 / 18.3, (64, 2) 15.1 / 21.7; 1280 192 threads a workgroup 21.2 / 23.0, 384 17.7 / 30.8, so the latter where there is no mean;
-// 4096 (512, 1) 60.3 / 63.6, (256, 2) 61.6 / 66.3; 5120 (640, 1) 79.4 / 96.4, (384, 2) 78.9 / 89.7 (fp32 151 / 154, 155 / 165); 8192 (512, 2) 129 / 147, (1024, 1) 122 / 155, so the latter where there is no mean.
+// 4096 (512, 1) 60.3 / 63.6, (256, 2) 61.6 / 66.3; the same class at 2560 and 3584, where 192 and 64 of its threads have no columns, 37.7 / 45.9 and 52.9 / 56.0
+// (bytes at 5 TB/s: 36.9 and 51.6; no class between was tried); 5120 (640, 1) 79.4 / 96.4, (384, 2) 78.9 / 89.7 (fp32 151 / 154, 155 / 165); 8192 (512, 2) 129 / 147, (1024, 1) 122 / 155, so the latter where there is no mean.
 template <typename T>
 hipError_t fwd_by_width(const JoinArgs &a, hipStream_t st) {
     const bool ln = a.post == NORM_LAYER || a.pre == NORM_LAYER;
@@ -629,7 +635,8 @@ hipError_t fwd_by_width(const JoinArgs &a, hipStream_t st) {
 }
 // Backward, where a workgroup has the compute unit to itself: as many threads as have the registers.  9000 bf16 rows, two RMSNorms / two LayerNorms and a gate
 // per segment, us: 1024 (128, 1) 26.8 / 34.0, (64, 2) 27.2 / 35.3 (in fp32 55 / 62, 55 / 79: it spills); 1280 768 threads a workgroup 31.5 / 39.2, 576 31.8 / 40.9; 4096
-// (512, 1) 98.1 / 110, (256, 2) 97.0 / 110 (fp32 186 / 198, 188 / 214); 5120 (640, 1) 118 / 130, (384, 2) 119 / 134; 8192 (512, 2) 192 / 211, (1024, 1) 192 / 622.
+// (512, 1) 98.1 / 110, (256, 2) 97.0 / 110 (fp32 186 / 198, 188 / 214); the same class at 2560 and 3584 63.5 / 72.6 and 84.6 / 93.9 (bytes 55.3 and 77.4; no class
+// between was tried); 5120 (640, 1) 118 / 130, (384, 2) 119 / 134; 8192 (512, 2) 192 / 211, (1024, 1) 192 / 622.
 template <typename T>
 hipError_t bwd_by_width(const JoinArgs &a, hipStream_t st) {
     if (a.H <= 64 * 8) return launch_bwd<T, 64, 1, 512>(a, st);

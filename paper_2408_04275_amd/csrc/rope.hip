@@ -142,7 +142,9 @@ hipError_t launch(const RopeArgs &a, hipStream_t st) {
 
 hipError_t rope(int dtype, const RopeArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    // elements that every chunk's place is a multiple of: the widest chunk that all accesses are aligned for
+    // elements that every chunk's place is a multiple of: the widest chunk that all accesses are aligned for.  12000 bf16 tokens of 40 heads of 80, us, of which
+    // 20 / 40 / 80 features rotate (chunks of 4 / 8 / 16 bytes): in place 33.7 / 37.2 / 36.6: the heads' whole lines are read
+    // whatever rotates, so narrow chunks cost nothing; out of place 50.5 / 38.4 / 36.1, where the features that pass through go by the narrow chunks too
     const long places = a.half | a.d | a.ldx | a.ldy;
     const int v = dtype == DT_F32 ? (places % 4 == 0 ? 4 : places % 2 == 0 ? 2 : 1)
                                   : (places % 8 == 0 ? 8 : places % 4 == 0 ? 4 : places % 2 == 0 ? 2 : 1);
