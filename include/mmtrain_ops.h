@@ -1,6 +1,7 @@
 /*
  * mmtrain operators around a block's products: rotary positions, the join of a block's branch with the residual stream,
- * and the end of a training step (global gradient norm, clipping, the optimizer step that clips as it reads).
+ * the end of a training step (global gradient norm, clipping, the optimizer step that clips as it reads), the embedding that a
+ * pack starts with, per-head norms of queries and keys with their rotation, and attention to encoder states of another length.
  *
  * With mmtrain_gemm, mmtrain_attn_fwd / _bwd and mmtrain_adam_step these make up the attention half of a block that differs from
  * the two layers of mmtrain_layer_fwd / _bwd -- another norm placement, gates, other positions -- and the norms and gates around
@@ -163,6 +164,142 @@ MMTRAIN_API int mmtrain_grad_clip(const mmtrain_grad_tensor *tensors, int32_t n_
 MMTRAIN_API int mmtrain_adam_step_clipped(const mmtrain_adam_desc *desc, int64_t n, float *master, float *grad, float *exp_avg,
                                           float *exp_avg_sq, void *param_out, int32_t param_dtype,
                                           const mmtrain_grad_norm_result *result, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Embedding of a multimodal pack.  ids_dev (device int32 [n_tokens]) names the row that each token of the pack starts from:
+ *     0 <= id < vocab:            y_t = scale table[id]             (text)
+ *     -n_features <= id < 0:      y_t = features[-1 - id]           (an encoder's output row, at its place in the pack)
+ *     anything else:              y_t = 0, and no gradient          (padding; vocab itself, say)
+ * Backward: d_table[v] = scale times the sum of dy_t over the tokens with id v, d_features[f] the sum over those with id -1 - f.
+ * The tokens are sorted by id; a row's sum has a fixed order.
+ * Supported: hidden a multiple of 8 up to 65536, vocab >= 1, vocab + n_features <= 2^30, at most 2^30 tokens; anything else:
+ * MMTRAIN_ERR_UNSUPPORTED.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    uint32_t struct_size;           /* sizeof(mmtrain_embed_desc) */
+    int32_t dtype;                  /* mmtrain_dtype of table, features, activations and (by default) the table's gradient */
+    int32_t hidden;
+    int32_t vocab;                  /* rows of the table */
+    int32_t n_features;             /* rows of features; 0: none */
+    float scale;                    /* of the table's rows (features keep theirs); finite */
+} mmtrain_embed_desc;
+
+/* y [n_tokens, hidden] from table [vocab, hidden] and features [n_features, hidden] (NULL where n_features is 0).  y may share
+ * memory with nothing. */
+MMTRAIN_API int mmtrain_embed_fwd(const mmtrain_embed_desc *desc, int32_t n_tokens, const int32_t *ids_dev, const void *table,
+                                  const void *features, void *y, void *hip_stream);
+
+/* Bytes of `workspace` for mmtrain_embed_bwd.  0 on an invalid description.  Never falls as n_tokens grows. */
+MMTRAIN_API size_t mmtrain_embed_workspace_bytes(const mmtrain_embed_desc *desc, int32_t n_tokens);
+
+/* From dy [n_tokens, hidden] writes d_table and d_features (either may be NULL: not computed).  flags concern d_table:
+ * MMTRAIN_BWD_WGRAD_F32: it is fp32; MMTRAIN_BWD_ACCUMULATE_WGRAD: the sums are added to it, and rows that no token names are not
+ * touched; without that flag every row is written, zeros where no token names it.  d_features (the type of `dtype`) is always
+ * written as a whole.  Sums are fp32, of chunks of up to 16 + n_tokens / 2048 tokens and then of the chunks. */
+MMTRAIN_API int mmtrain_embed_bwd(const mmtrain_embed_desc *desc, int32_t n_tokens, const int32_t *ids_dev, const void *dy,
+                                  void *d_table, void *d_features, uint32_t flags, void *workspace, size_t workspace_bytes,
+                                  void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Norms of queries and keys for each head, and their rotation, in one pass.  A row of x holds n_q_heads query heads, then
+ * n_k_heads key heads (what stands behind them, values say, is left alone).  Each head of head_dim features is normalised by itself,
+ *     RMS: n = v rsqrt(mean(v^2) + eps) w,   LAYER: n = (v - mean(v)) rsqrt(var(v) + eps) w + b,
+ * with one gain (and bias) [head_dim] for all query heads and one for all key heads, and then rotated as mmtrain_rope does it.
+ * In front of mmtrain_attn_fwd both kinds are done by one call on the packed qkv; in front of mmtrain_cross_attn_fwd the queries
+ * by one (n_k_heads = 0) and the encoder's keys by another (n_q_heads = 0), without a rotation usually.
+ * Supported: head_dim a multiple of 8 up to 256, rot_dim a multiple of 4, strides multiples of 8 (bf16) or 4 (fp32) elements, at most
+ * 65536 heads and 2^30 tokens; anything else: MMTRAIN_ERR_UNSUPPORTED.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    uint32_t struct_size;           /* sizeof(mmtrain_qk_norm_desc) */
+    int32_t dtype;                  /* mmtrain_dtype of rows, parameters and (by default) parameter gradients */
+    int32_t n_q_heads, n_k_heads;   /* either may be 0, not both */
+    int32_t head_dim;
+    int32_t norm;                   /* MMTRAIN_NORM_RMS or MMTRAIN_NORM_LAYER */
+    float eps;                      /* > 0 */
+} mmtrain_qk_norm_desc;
+
+/* [head_dim] each, required for heads that there are (biases: LAYER), NULL elsewhere. */
+typedef struct { const void *q_w, *q_b, *k_w, *k_b; } mmtrain_qk_norm_weights;
+/* Where to write parameter gradients; NULL: not computed. */
+typedef struct { void *q_w, *q_b, *k_w, *k_b; } mmtrain_qk_norm_grads;
+
+/* y = the normalised and rotated heads of x; strides as for mmtrain_rope.  `rope` describes the rotation (its dtype and head_dim are
+ * desc's, its n_heads n_q_heads + n_k_heads); NULL: none.  Positions as for mmtrain_rope; without a rotation neither `batch` nor
+ * positions_dev is read.  y may be x (with ld_y = ld_x), for passes that have no backward pass; otherwise no element of y may be one of x. */
+MMTRAIN_API int mmtrain_qk_norm_rope_fwd(const mmtrain_qk_norm_desc *desc, const mmtrain_rope_desc *rope, int32_t n_tokens,
+                                         const mmtrain_batch *batch, const int32_t *positions_dev,
+                                         const mmtrain_qk_norm_weights *weights, const void *x, int64_t ld_x, void *y, int64_t ld_y,
+                                         void *hip_stream);
+
+/* Bytes of `workspace` for backward.  0 on an invalid description.  Never falls as n_tokens grows. */
+MMTRAIN_API size_t mmtrain_qk_norm_rope_workspace_bytes(const mmtrain_qk_norm_desc *desc, int32_t n_tokens);
+
+/* From dy (the gradient of y) and forward's x writes dx (NULL: not computed) and every non-NULL member of grads (which may be NULL);
+ * statistics are formed anew from x.  dx may be dy's buffer (with ld_dx = ld_dy); otherwise an output may share memory with nothing.
+ * flags: MMTRAIN_BWD_ACCUMULATE_WGRAD, MMTRAIN_BWD_WGRAD_F32.  workspace: needed where grads has a member. */
+MMTRAIN_API int mmtrain_qk_norm_rope_bwd(const mmtrain_qk_norm_desc *desc, const mmtrain_rope_desc *rope, int32_t n_tokens,
+                                         const mmtrain_batch *batch, const int32_t *positions_dev,
+                                         const mmtrain_qk_norm_weights *weights, const void *x, int64_t ld_x, const void *dy,
+                                         int64_t ld_dy, void *dx, int64_t ld_dx, const mmtrain_qk_norm_grads *grads, uint32_t flags,
+                                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Cross attention: queries of a pack attend to keys and values of another length (an encoder's states).  The queries are cut into
+ * runs; all tokens of run s, cu_q[s] .. cu_q[s + 1] - 1, see the keys kv_begin[s] .. kv_end[s] - 1 and no others:
+ *     o_t = sum_j softmax_j(softmax_scale q_t . k_j) v_j,    lse_t = ln sum_j exp(softmax_scale q_t . k_j)
+ * A pack whose samples have their own images: kv_begin = cu_kv, kv_end = cu_kv + 1 (the same array).  Runs may see the same keys (several
+ * continuations of one prompt) or overlapping ranges (text that sees the images so far).  kv_begin[s] = kv_end[s]: the run sees
+ * nothing, o = 0, lse = -infinity, no gradient.  What a query does not see does not reach it, not even an infinity or NaN.
+ * Grouped heads as in mmtrain_layer_desc: query head h reads key/value head h / (n_heads / n_kv_heads).
+ * One token for each of many sequences is a call with runs of one token: with few queries the keys are shared out over the chip.
+ * Supported: head_dim a multiple of 16 up to 128, n_heads % n_kv_heads = 0, at most 4096 heads, 65536 runs, 2^27 query and 2^30 key tokens, strides
+ * multiples of 8 (bf16) or 4 (fp32) elements below 2^24; anything else: MMTRAIN_ERR_UNSUPPORTED.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+    uint32_t struct_size;           /* sizeof(mmtrain_cross_attn_desc) */
+    int32_t dtype;                  /* mmtrain_dtype */
+    int32_t n_heads, n_kv_heads, head_dim;
+    float softmax_scale;            /* > 0; 0 => 1/sqrt(head_dim) */
+} mmtrain_cross_attn_desc;
+
+/* The host arrays hold the same values as the device arrays: validation and launch sizing.  A captured call is replayed for the ranges
+ * that it was captured with. */
+typedef struct {
+    int32_t q_tokens, kv_tokens;    /* rows of q, and of k and v */
+    int32_t n_segments;             /* runs of queries, S */
+    const int32_t *cu_q_dev, *cu_q_host;            /* [S + 1]: 0, non-decreasing, q_tokens */
+    const int32_t *kv_begin_dev, *kv_begin_host;    /* [S] */
+    const int32_t *kv_end_dev, *kv_end_host;        /* [S]: kv_begin <= kv_end <= kv_tokens */
+} mmtrain_cross_batch;
+
+/* Rows of q and o: n_heads heads, of k and v: n_kv_heads heads; strides in elements (k and v may be columns of one tensor). */
+typedef struct {
+    const void *q; int64_t ld_q;
+    const void *k; int64_t ld_k;
+    const void *v; int64_t ld_v;
+    void *o; int64_t ld_o;          /* written by fwd, read by bwd */
+    float *lse;                     /* [n_heads, q_tokens]; fwd: may be NULL; bwd: required */
+} mmtrain_cross_attn_tensors;
+typedef struct {
+    const void *d_o; int64_t ld_do;
+    void *d_q; int64_t ld_dq;       /* NULL: not computed */
+    void *d_k; int64_t ld_dk;       /* d_k and d_v: both, or neither (a frozen encoder) */
+    void *d_v; int64_t ld_dv;
+} mmtrain_cross_attn_grads;
+
+/* Bytes of `workspace` for fwd (is_bwd = 0) or bwd (is_bwd = 1); the host arrays of `batch` are read.  0 where the call would be refused. */
+MMTRAIN_API size_t mmtrain_cross_attn_workspace_bytes(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, int is_bwd);
+
+MMTRAIN_API int mmtrain_cross_attn_fwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch,
+                                       const mmtrain_cross_attn_tensors *tensors, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Every row of d_q, d_k and d_v is written, zeros for queries that see nothing and keys that nobody sees.  Where d_k and d_v are computed, kv_begin and
+ * kv_end have to be non-decreasing over the runs that see something (MMTRAIN_ERR_BAD_SEGMENTS), so that the runs which see a key
+ * follow one another.  Outputs may share memory with nothing. */
+MMTRAIN_API int mmtrain_cross_attn_bwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch,
+                                       const mmtrain_cross_attn_tensors *tensors, const mmtrain_cross_attn_grads *grads,
+                                       void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -34,7 +34,10 @@ EXPORTS = ("mmtrain_layer_ctx_bytes", "mmtrain_layer_workspace_bytes", "mmtrain_
            "mmtrain_profile_gemm_clock", "mmtrain_attn_bwd_noalloc")
 # declared in include/mmtrain_ops.h
 OPS_EXPORTS = ("mmtrain_rope", "mmtrain_residual_norm_workspace_bytes", "mmtrain_residual_norm_fwd", "mmtrain_residual_norm_bwd",
-               "mmtrain_grad_norm_workspace_bytes", "mmtrain_grad_norm", "mmtrain_grad_clip", "mmtrain_adam_step_clipped")
+               "mmtrain_grad_norm_workspace_bytes", "mmtrain_grad_norm", "mmtrain_grad_clip", "mmtrain_adam_step_clipped",
+               "mmtrain_embed_fwd", "mmtrain_embed_workspace_bytes", "mmtrain_embed_bwd",
+               "mmtrain_qk_norm_rope_fwd", "mmtrain_qk_norm_rope_workspace_bytes", "mmtrain_qk_norm_rope_bwd",
+               "mmtrain_cross_attn_workspace_bytes", "mmtrain_cross_attn_fwd", "mmtrain_cross_attn_bwd")
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_WAVELENGTH, ROPE_RAMP = range(4)
 ROPE_GRADIENT = 1
@@ -105,6 +108,47 @@ class ResidualNormGrads(C.Structure):
 
 class ResidualNormStats(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in RESIDUAL_NORM_STATS]
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("hidden", C.c_int32), ("vocab", C.c_int32),
+                ("n_features", C.c_int32), ("scale", C.c_float)]
+
+
+QK_NORM_FIELDS = ("q_w", "q_b", "k_w", "k_b")
+
+
+class QkNormDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_k_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float)]
+
+
+class QkNormWeights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in QK_NORM_FIELDS]
+
+
+class QkNormGrads(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in QK_NORM_FIELDS]
+
+
+class CrossAttnDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("softmax_scale", C.c_float)]
+
+
+class CrossBatchStruct(C.Structure):
+    _fields_ = [("q_tokens", C.c_int32), ("kv_tokens", C.c_int32), ("n_segments", C.c_int32),
+                *[(n, C.c_void_p) for n in ("cu_q_dev", "cu_q_host", "kv_begin_dev", "kv_begin_host", "kv_end_dev", "kv_end_host")]]
+
+
+class CrossAttnTensors(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld_q", C.c_int64), ("k", C.c_void_p), ("ld_k", C.c_int64), ("v", C.c_void_p), ("ld_v", C.c_int64),
+                ("o", C.c_void_p), ("ld_o", C.c_int64), ("lse", C.c_void_p)]
+
+
+class CrossAttnGrads(C.Structure):
+    _fields_ = [("d_o", C.c_void_p), ("ld_do", C.c_int64), ("d_q", C.c_void_p), ("ld_dq", C.c_int64), ("d_k", C.c_void_p),
+                ("ld_dk", C.c_int64), ("d_v", C.c_void_p), ("ld_dv", C.c_int64)]
 
 
 class GradTensor(C.Structure):
@@ -187,6 +231,24 @@ def load_library() -> C.CDLL:
     lib.mmtrain_grad_clip.argtypes = [P, I, P, P]
     lib.mmtrain_adam_step_clipped.restype = C.c_int
     lib.mmtrain_adam_step_clipped.argtypes = [P, L, P, P, P, P, P, I, P, P]
+    lib.mmtrain_embed_fwd.restype = C.c_int
+    lib.mmtrain_embed_fwd.argtypes = [P, I, P, P, P, P, P]
+    lib.mmtrain_embed_workspace_bytes.restype = S
+    lib.mmtrain_embed_workspace_bytes.argtypes = [P, I]
+    lib.mmtrain_embed_bwd.restype = C.c_int
+    lib.mmtrain_embed_bwd.argtypes = [P, I, P, P, P, P, U, P, S, P]
+    lib.mmtrain_qk_norm_rope_fwd.restype = C.c_int
+    lib.mmtrain_qk_norm_rope_fwd.argtypes = [P, P, I, P, P, P, P, L, P, L, P]
+    lib.mmtrain_qk_norm_rope_workspace_bytes.restype = S
+    lib.mmtrain_qk_norm_rope_workspace_bytes.argtypes = [P, I]
+    lib.mmtrain_qk_norm_rope_bwd.restype = C.c_int
+    lib.mmtrain_qk_norm_rope_bwd.argtypes = [P, P, I, P, P, P, P, L, P, L, P, L, P, U, P, S, P]
+    lib.mmtrain_cross_attn_workspace_bytes.restype = S
+    lib.mmtrain_cross_attn_workspace_bytes.argtypes = [P, P, C.c_int]
+    lib.mmtrain_cross_attn_fwd.restype = C.c_int
+    lib.mmtrain_cross_attn_fwd.argtypes = [P, P, P, P, S, P]
+    lib.mmtrain_cross_attn_bwd.restype = C.c_int
+    lib.mmtrain_cross_attn_bwd.argtypes = [P, P, P, P, P, S, P]
     _lib = lib
     return lib
 
@@ -533,3 +595,117 @@ def mmtrain_grad_clip(tensors, result, stream=None) -> int:
 def mmtrain_adam_step_clipped(desc, n, master, grad, exp_avg, exp_avg_sq, param_out, param_dtype, result, stream=None) -> int:
     return load_library().mmtrain_adam_step_clipped(_ref(desc), n, _ptr(master), _ptr(grad), _ptr(exp_avg), _ptr(exp_avg_sq),
                                                     _ptr(param_out), param_dtype, _ptr(result), _stream(stream))
+
+
+# ----------------------------------------------------------------------------
+# embedding, norms of queries and keys with rotation, cross attention
+# ----------------------------------------------------------------------------
+def make_embed_desc(dtype, hidden, vocab, n_features=0, scale=1.0) -> EmbedDesc:
+    return EmbedDesc(C.sizeof(EmbedDesc), dtype, hidden, vocab, n_features, scale)
+
+
+def mmtrain_embed_fwd(desc, n_tokens, ids, table, features, y, stream=None) -> int:
+    return load_library().mmtrain_embed_fwd(_ref(desc), n_tokens, _ptr(ids), _ptr(table), _ptr(features), _ptr(y), _stream(stream))
+
+
+def mmtrain_embed_workspace_bytes(desc, n_tokens: int) -> int:
+    return load_library().mmtrain_embed_workspace_bytes(_ref(desc), n_tokens)
+
+
+def mmtrain_embed_bwd(desc, n_tokens, ids, dy, d_table, d_features, flags, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmtrain_embed_bwd(_ref(desc), n_tokens, _ptr(ids), _ptr(dy), _ptr(d_table), _ptr(d_features), flags,
+                                            _ptr(workspace), workspace_bytes, _stream(stream))
+
+
+def make_qk_norm_desc(dtype, n_q_heads, n_k_heads, head_dim, norm=NORM_RMS, eps=1e-6) -> QkNormDesc:
+    return QkNormDesc(C.sizeof(QkNormDesc), dtype, n_q_heads, n_k_heads, head_dim, norm, eps)
+
+
+def make_qk_norm_weights(tensors: Dict[str, object]) -> QkNormWeights:
+    return QkNormWeights(*[_ptr(tensors.get(n)) for n in QK_NORM_FIELDS])
+
+
+def make_qk_norm_grads(tensors: Dict[str, object]) -> QkNormGrads:
+    return QkNormGrads(*[_ptr(tensors.get(n)) for n in QK_NORM_FIELDS])
+
+
+def mmtrain_qk_norm_rope_fwd(desc, rope, n_tokens, batch, positions, weights, x, ld_x, y, ld_y, stream=None) -> int:
+    b = batch.struct if isinstance(batch, PackedBatch) else batch
+    return load_library().mmtrain_qk_norm_rope_fwd(_ref(desc), _ref(rope), n_tokens, _ref(b), _ptr(positions), _ref(weights), _ptr(x),
+                                                   ld_x, _ptr(y), ld_y, _stream(stream))
+
+
+def mmtrain_qk_norm_rope_workspace_bytes(desc, n_tokens: int) -> int:
+    return load_library().mmtrain_qk_norm_rope_workspace_bytes(_ref(desc), n_tokens)
+
+
+def mmtrain_qk_norm_rope_bwd(desc, rope, n_tokens, batch, positions, weights, x, ld_x, dy, ld_dy, dx, ld_dx, grads, flags, workspace,
+                             workspace_bytes, stream=None) -> int:
+    b = batch.struct if isinstance(batch, PackedBatch) else batch
+    return load_library().mmtrain_qk_norm_rope_bwd(_ref(desc), _ref(rope), n_tokens, _ref(b), _ptr(positions), _ref(weights), _ptr(x),
+                                                   ld_x, _ptr(dy), ld_dy, _ptr(dx), ld_dx, _ref(grads), flags, _ptr(workspace),
+                                                   workspace_bytes, _stream(stream))
+
+
+def make_cross_attn_desc(dtype, n_heads, n_kv_heads, head_dim, softmax_scale=0.0) -> CrossAttnDesc:
+    return CrossAttnDesc(C.sizeof(CrossAttnDesc), dtype, n_heads, n_kv_heads, head_dim, softmax_scale)
+
+
+class CrossBatch:
+    """Runs of queries and the range of keys that each sees: host and device copies, and the C struct that points at them."""
+
+    def __init__(self, cu_q_host, kv_begin_host, kv_end_host, kv_tokens, cu_q_dev=None, kv_begin_dev=None, kv_end_dev=None,
+                 q_tokens: Optional[int] = None):
+        host = [np.ascontiguousarray(a, dtype=np.int32) for a in (cu_q_host, kv_begin_host, kv_end_host)]
+        self.cu_q_host, self.kv_begin_host, self.kv_end_host = host
+        self.device = (cu_q_dev, kv_begin_dev, kv_end_dev)
+        if len(host[1]) != len(host[0]) - 1 or len(host[2]) != len(host[1]):
+            raise ValueError("one range of keys for each run of queries")
+        T = int(host[0][-1]) if q_tokens is None else q_tokens
+        self.struct = CrossBatchStruct(T, kv_tokens, len(host[1]), _ptr(cu_q_dev), _ptr(host[0]), _ptr(kv_begin_dev), _ptr(host[1]),
+                                       _ptr(kv_end_dev), _ptr(host[2]))
+
+    @classmethod
+    def on_device(cls, cu_q_host, kv_begin_host, kv_end_host, kv_tokens, device="cuda"):
+        import torch
+        dev = []
+        for a in (cu_q_host, kv_begin_host, kv_end_host):
+            a = np.ascontiguousarray(a, dtype=np.int32)
+            dev.append(torch.from_numpy(a.copy()).to(device) if len(a) else torch.empty(1, dtype=torch.int32, device=device))
+        return cls(cu_q_host, kv_begin_host, kv_end_host, kv_tokens, *dev)
+
+
+def _rows(t):
+    """Address and row stride of a 2-d tensor of rows whose elements are neighbours."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("rows of neighbouring elements")
+    return _ptr(t), t.stride(0)
+
+
+def make_cross_attn_tensors(q, k, v, o, lse=None) -> CrossAttnTensors:
+    """From torch tensors [tokens, heads * head_dim], which may be columns of wider ones.  The struct holds addresses: keep the tensors alive."""
+    return CrossAttnTensors(*_rows(q), *_rows(k), *_rows(v), *_rows(o), _ptr(lse))
+
+
+def make_cross_attn_grads(d_o, d_q=None, d_k=None, d_v=None) -> CrossAttnGrads:
+    return CrossAttnGrads(*_rows(d_o), *_rows(d_q), *_rows(d_k), *_rows(d_v))
+
+
+def _cross(batch):
+    return batch.struct if isinstance(batch, CrossBatch) else batch
+
+
+def mmtrain_cross_attn_workspace_bytes(desc, batch, is_bwd) -> int:
+    return load_library().mmtrain_cross_attn_workspace_bytes(_ref(desc), _ref(_cross(batch)), 1 if is_bwd else 0)
+
+
+def mmtrain_cross_attn_fwd(desc, batch, tensors, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmtrain_cross_attn_fwd(_ref(desc), _ref(_cross(batch)), _ref(tensors), _ptr(workspace), workspace_bytes,
+                                                 _stream(stream))
+
+
+def mmtrain_cross_attn_bwd(desc, batch, tensors, grads, workspace, workspace_bytes, stream=None) -> int:
+    return load_library().mmtrain_cross_attn_bwd(_ref(desc), _ref(_cross(batch)), _ref(tensors), _ref(grads), _ptr(workspace),
+                                                 workspace_bytes, _stream(stream))

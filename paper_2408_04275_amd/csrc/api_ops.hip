@@ -38,6 +38,90 @@ int rope_turns(const mmtrain_rope_desc &d, RopeArgs &a) {
     return MMTRAIN_OK;
 }
 
+// What the calls that rotate have in common: the description, and where the positions come from
+int rope_common(const mmtrain_rope_desc *desc, int32_t n_tokens, const mmtrain_batch *batch, const int32_t *positions_dev, uint32_t flags, RopeArgs &a) {
+    if (!desc || desc->struct_size != sizeof(mmtrain_rope_desc) || !is_dtype(desc->dtype)) return MMTRAIN_ERR_INVALID_ARG;
+    if (desc->layout != MMTRAIN_ROPE_HALF && desc->layout != MMTRAIN_ROPE_INTERLEAVED) return MMTRAIN_ERR_INVALID_ARG;
+    if (desc->scaling < MMTRAIN_ROPE_PLAIN || desc->scaling > MMTRAIN_ROPE_RAMP) return MMTRAIN_ERR_INVALID_ARG;
+    if (desc->n_heads <= 0 || desc->head_dim <= 0 || desc->rot_dim <= 0 || desc->rot_dim > desc->head_dim) return MMTRAIN_ERR_INVALID_ARG;
+    if (!(desc->base > 1.f && std::isfinite(desc->base)) || !(desc->magnitude >= 0.f && std::isfinite(desc->magnitude))) return MMTRAIN_ERR_INVALID_ARG;
+    if (desc->rot_dim % 2 || desc->head_dim > 2 * ROPE_MAX_HALF || desc->n_heads > ROPE_MAX_HEADS) return MMTRAIN_ERR_UNSUPPORTED;
+    a.half = desc->rot_dim / 2;
+    int rc = rope_turns(*desc, a);
+    if (rc) return rc;
+    if (n_tokens < 0 || (flags & ~MMTRAIN_ROPE_GRADIENT) || (batch && positions_dev)) return MMTRAIN_ERR_INVALID_ARG;
+    if (batch) {
+        if ((rc = check_batch(batch))) return rc;
+        if (batch->total_tokens != n_tokens) return MMTRAIN_ERR_BAD_SEGMENTS;
+        a.cu = batch->cu_seqlens_dev; a.S = batch->n_segments;
+    }
+    a.T = n_tokens; a.heads = desc->n_heads; a.d = desc->head_dim;
+    a.interleaved = desc->layout == MMTRAIN_ROPE_INTERLEAVED;
+    a.positions = positions_dev;
+    double m = desc->magnitude;
+    if (m == 0.0) m = desc->scaling == MMTRAIN_ROPE_RAMP ? 0.1 * std::log((double)desc->factor) + 1.0 : 1.0;
+    a.cos_scale = (float)m;
+    a.sin_scale = (flags & MMTRAIN_ROPE_GRADIENT) ? -(float)m : (float)m;
+    return MMTRAIN_OK;
+}
+
+// ---- norms of queries and keys ---------------------------------------------------------------
+int check_qk_norm(const mmtrain_qk_norm_desc *d) {
+    if (!d || d->struct_size != sizeof(mmtrain_qk_norm_desc) || !is_dtype(d->dtype)) return MMTRAIN_ERR_INVALID_ARG;
+    if (d->norm != MMTRAIN_NORM_RMS && d->norm != MMTRAIN_NORM_LAYER) return MMTRAIN_ERR_INVALID_ARG;
+    if (d->n_q_heads < 0 || d->n_k_heads < 0 || (!d->n_q_heads && !d->n_k_heads) || d->head_dim <= 0 || !(d->eps > 0.f)) return MMTRAIN_ERR_INVALID_ARG;
+    if (d->head_dim % 8 || d->head_dim > 2 * ROPE_MAX_HALF || d->n_q_heads > ROPE_MAX_HEADS || d->n_k_heads > ROPE_MAX_HEADS - d->n_q_heads)
+        return MMTRAIN_ERR_UNSUPPORTED;
+    return MMTRAIN_OK;
+}
+
+int qk_norm_stride(const mmtrain_qk_norm_desc &d, int64_t ld) {
+    if (ld < ((int64_t)d.n_q_heads + d.n_k_heads) * d.head_dim) return MMTRAIN_ERR_INVALID_ARG;
+    return ld % (d.dtype == MMTRAIN_F32 ? 4 : 8) ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
+}
+
+int qk_norm_common(const mmtrain_qk_norm_desc *d, const mmtrain_rope_desc *rope, int32_t n_tokens, const mmtrain_batch *batch, const int32_t *positions_dev,
+                   const mmtrain_qk_norm_weights *w, uint32_t flags, QkNormArgs &a) {
+    int rc = check_qk_norm(d);
+    if (rc) return rc;
+    if (n_tokens < 0 || !w) return MMTRAIN_ERR_INVALID_ARG;
+    if (n_tokens > QK_MAX_ROWS) return MMTRAIN_ERR_UNSUPPORTED;
+    if (rope) {
+        if ((rc = rope_common(rope, n_tokens, batch, positions_dev, flags, a.r))) return rc;
+        if (rope->dtype != d->dtype || rope->head_dim != d->head_dim || rope->n_heads != d->n_q_heads + d->n_k_heads) return MMTRAIN_ERR_INVALID_ARG;
+        if (rope->rot_dim % 4) return MMTRAIN_ERR_UNSUPPORTED;
+        if (n_tokens > 0 && ((!batch && !positions_dev) || ((uintptr_t)positions_dev & 3))) return MMTRAIN_ERR_INVALID_ARG;
+    } else {
+        a.r.T = n_tokens; a.r.heads = d->n_q_heads + d->n_k_heads; a.r.d = d->head_dim;
+    }
+    const bool layer = d->norm == MMTRAIN_NORM_LAYER;
+    if (!w->q_w != !d->n_q_heads || !w->k_w != !d->n_k_heads || !w->q_b != !(layer && d->n_q_heads) || !w->k_b != !(layer && d->n_k_heads) ||
+        misaligned({w->q_w, w->q_b, w->k_w, w->k_b}))
+        return MMTRAIN_ERR_INVALID_ARG;
+    a.nq = d->n_q_heads; a.norm = d->norm; a.eps = d->eps;
+    a.q_w = w->q_w; a.q_b = w->q_b; a.k_w = w->k_w; a.k_b = w->k_b;
+    return MMTRAIN_OK;
+}
+
+size_t qk_norm_part_bytes(const mmtrain_qk_norm_desc &d, int32_t T) { return ((size_t)qk_norm_bwd_blocks(T) * d.head_dim * sizeof(float) + 255) & ~size_t(255); }
+
+// ---- embedding ---------------------------------------------------------------------------------
+int check_embed(const mmtrain_embed_desc *d) {
+    if (!d || d->struct_size != sizeof(mmtrain_embed_desc) || !is_dtype(d->dtype)) return MMTRAIN_ERR_INVALID_ARG;
+    if (d->hidden <= 0 || d->vocab <= 0 || d->n_features < 0 || !std::isfinite(d->scale)) return MMTRAIN_ERR_INVALID_ARG;
+    if (d->hidden % 8 || d->hidden > 65536 || (int64_t)d->vocab + d->n_features > EMBED_MAX_ROWS) return MMTRAIN_ERR_UNSUPPORTED;
+    return MMTRAIN_OK;
+}
+
+int embed_common(const mmtrain_embed_desc *d, int32_t n_tokens, const int32_t *ids, EmbedArgs &a) {
+    int rc = check_embed(d);
+    if (rc) return rc;
+    if (n_tokens < 0 || (n_tokens > 0 && !ids) || ((uintptr_t)ids & 3)) return MMTRAIN_ERR_INVALID_ARG;
+    if (n_tokens > EMBED_MAX_ROWS) return MMTRAIN_ERR_UNSUPPORTED;
+    a.T = n_tokens; a.H = d->hidden; a.vocab = d->vocab; a.features = d->n_features; a.scale = d->scale; a.ids = ids;
+    return MMTRAIN_OK;
+}
+
 // ---- the join of branch and residual stream ----------------------------------------------
 int check_join(const mmtrain_residual_norm_desc *d) {
     if (!d || d->struct_size != sizeof(mmtrain_residual_norm_desc) || !is_dtype(d->dtype)) return MMTRAIN_ERR_INVALID_ARG;
@@ -251,35 +335,103 @@ extern "C" {
 
 int mmtrain_rope(const mmtrain_rope_desc *desc, int32_t n_tokens, const mmtrain_batch *batch, const int32_t *positions_dev,
                  const void *x, int64_t ld_x, void *y, int64_t ld_y, uint32_t flags, void *hip_stream) {
-    if (!desc || desc->struct_size != sizeof(mmtrain_rope_desc) || !is_dtype(desc->dtype)) return MMTRAIN_ERR_INVALID_ARG;
-    if (desc->layout != MMTRAIN_ROPE_HALF && desc->layout != MMTRAIN_ROPE_INTERLEAVED) return MMTRAIN_ERR_INVALID_ARG;
-    if (desc->scaling < MMTRAIN_ROPE_PLAIN || desc->scaling > MMTRAIN_ROPE_RAMP) return MMTRAIN_ERR_INVALID_ARG;
-    if (desc->n_heads <= 0 || desc->head_dim <= 0 || desc->rot_dim <= 0 || desc->rot_dim > desc->head_dim) return MMTRAIN_ERR_INVALID_ARG;
-    if (!(desc->base > 1.f && std::isfinite(desc->base)) || !(desc->magnitude >= 0.f && std::isfinite(desc->magnitude))) return MMTRAIN_ERR_INVALID_ARG;
-    if (desc->rot_dim % 2 || desc->head_dim > 2 * ROPE_MAX_HALF || desc->n_heads > ROPE_MAX_HEADS) return MMTRAIN_ERR_UNSUPPORTED;
     RopeArgs a = {};
-    a.half = desc->rot_dim / 2;
-    int rc = rope_turns(*desc, a);
+    int rc = rope_common(desc, n_tokens, batch, positions_dev, flags, a);
     if (rc) return rc;
-    if (n_tokens < 0 || (flags & ~MMTRAIN_ROPE_GRADIENT) || (batch && positions_dev)) return MMTRAIN_ERR_INVALID_ARG;
-    if (batch) {
-        if ((rc = check_batch(batch))) return rc;
-        if (batch->total_tokens != n_tokens) return MMTRAIN_ERR_BAD_SEGMENTS;
-        a.cu = batch->cu_seqlens_dev; a.S = batch->n_segments;
-    }
     const int64_t row = (int64_t)desc->n_heads * desc->head_dim;
     if (ld_x < row || ld_y < row) return MMTRAIN_ERR_INVALID_ARG;
     if (n_tokens == 0) return MMTRAIN_OK;
     if ((!batch && !positions_dev) || !x || !y || misaligned({x, y}) || ((uintptr_t)positions_dev & 3)) return MMTRAIN_ERR_INVALID_ARG;
     if (x == y && ld_x != ld_y) return MMTRAIN_ERR_INVALID_ARG;
-    a.T = n_tokens; a.heads = desc->n_heads; a.d = desc->head_dim;
-    a.interleaved = desc->layout == MMTRAIN_ROPE_INTERLEAVED;
-    a.positions = positions_dev; a.x = x; a.ldx = ld_x; a.y = y; a.ldy = ld_y;
-    double m = desc->magnitude;
-    if (m == 0.0) m = desc->scaling == MMTRAIN_ROPE_RAMP ? 0.1 * std::log((double)desc->factor) + 1.0 : 1.0;
-    a.cos_scale = (float)m;
-    a.sin_scale = (flags & MMTRAIN_ROPE_GRADIENT) ? -(float)m : (float)m;
+    a.x = x; a.ldx = ld_x; a.y = y; a.ldy = ld_y;
     HIP_TRY(rope(desc->dtype, a, (hipStream_t)hip_stream));
+    return MMTRAIN_OK;
+}
+
+int mmtrain_qk_norm_rope_fwd(const mmtrain_qk_norm_desc *desc, const mmtrain_rope_desc *rope, int32_t n_tokens, const mmtrain_batch *batch,
+                             const int32_t *positions_dev, const mmtrain_qk_norm_weights *weights, const void *x, int64_t ld_x,
+                             void *y, int64_t ld_y, void *hip_stream) {
+    QkNormArgs a = {};
+    int rc = qk_norm_common(desc, rope, n_tokens, batch, positions_dev, weights, 0, a);
+    if (rc) return rc;
+    if ((rc = qk_norm_stride(*desc, ld_x)) || (rc = qk_norm_stride(*desc, ld_y))) return rc;
+    if (n_tokens == 0) return MMTRAIN_OK;
+    if (!x || !y || misaligned({x, y}) || (x == y && ld_x != ld_y)) return MMTRAIN_ERR_INVALID_ARG;
+    a.r.x = x; a.r.ldx = ld_x; a.r.y = y; a.r.ldy = ld_y;
+    HIP_TRY(qk_norm_fwd(desc->dtype, a, (hipStream_t)hip_stream));
+    return MMTRAIN_OK;
+}
+
+size_t mmtrain_qk_norm_rope_workspace_bytes(const mmtrain_qk_norm_desc *desc, int32_t n_tokens) {
+    if (check_qk_norm(desc) != MMTRAIN_OK || n_tokens < 0) return 0;
+    return 4 * qk_norm_part_bytes(*desc, n_tokens) + 256;
+}
+
+int mmtrain_qk_norm_rope_bwd(const mmtrain_qk_norm_desc *desc, const mmtrain_rope_desc *rope, int32_t n_tokens, const mmtrain_batch *batch,
+                             const int32_t *positions_dev, const mmtrain_qk_norm_weights *weights, const void *x, int64_t ld_x,
+                             const void *dy, int64_t ld_dy, void *dx, int64_t ld_dx, const mmtrain_qk_norm_grads *grads, uint32_t flags,
+                             void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (flags & ~(MMTRAIN_BWD_ACCUMULATE_WGRAD | MMTRAIN_BWD_WGRAD_F32)) return MMTRAIN_ERR_INVALID_ARG;
+    QkNormArgs a = {};
+    int rc = qk_norm_common(desc, rope, n_tokens, batch, positions_dev, weights, MMTRAIN_ROPE_GRADIENT, a);
+    if (rc) return rc;
+    if ((rc = qk_norm_stride(*desc, ld_x)) || (rc = qk_norm_stride(*desc, ld_dy)) || (dx && (rc = qk_norm_stride(*desc, ld_dx)))) return rc;
+    const mmtrain_qk_norm_grads none = {};
+    const mmtrain_qk_norm_grads &g = grads ? *grads : none;
+    const bool layer = desc->norm == MMTRAIN_NORM_LAYER;
+    if ((g.q_w && !desc->n_q_heads) || (g.q_b && !(layer && desc->n_q_heads)) || (g.k_w && !desc->n_k_heads) || (g.k_b && !(layer && desc->n_k_heads)))
+        return MMTRAIN_ERR_INVALID_ARG;
+    if (misaligned({g.q_w, g.q_b, g.k_w, g.k_b})) return MMTRAIN_ERR_INVALID_ARG;
+    const bool any = g.q_w || g.q_b || g.k_w || g.k_b;
+    if (n_tokens > 0) {
+        if (!x || !dy || misaligned({x, dy, dx}) || dx == x || (dx == dy && ld_dx != ld_dy)) return MMTRAIN_ERR_INVALID_ARG;
+    }
+    if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
+    if (any && (!workspace || workspace_bytes < mmtrain_qk_norm_rope_workspace_bytes(desc, n_tokens))) return MMTRAIN_ERR_WORKSPACE;
+    if (!any && (!dx || n_tokens == 0)) return MMTRAIN_OK;
+    void *const out[4] = {g.q_w, g.q_b, g.k_w, g.k_b};
+    for (int i = 0; i < 4; ++i) {
+        a.grad[i] = out[i];
+        a.part[i] = out[i] ? reinterpret_cast<float *>((uint8_t *)workspace + i * qk_norm_part_bytes(*desc, n_tokens)) : nullptr;
+    }
+    a.grad_f32 = desc->dtype == MMTRAIN_F32 || (flags & MMTRAIN_BWD_WGRAD_F32);
+    a.accumulate = (flags & MMTRAIN_BWD_ACCUMULATE_WGRAD) != 0;
+    a.r.x = x; a.r.ldx = ld_x; a.dy = dy; a.lddy = ld_dy; a.r.y = dx; a.r.ldy = ld_dx;
+    HIP_TRY(qk_norm_bwd(desc->dtype, a, (hipStream_t)hip_stream));
+    return MMTRAIN_OK;
+}
+
+int mmtrain_embed_fwd(const mmtrain_embed_desc *desc, int32_t n_tokens, const int32_t *ids_dev, const void *table, const void *features,
+                      void *y, void *hip_stream) {
+    EmbedArgs a = {};
+    int rc = embed_common(desc, n_tokens, ids_dev, a);
+    if (rc || n_tokens == 0) return rc;
+    if (!table || !features != (desc->n_features == 0) || !y || misaligned({table, features, y}) || y == table || y == features) return MMTRAIN_ERR_INVALID_ARG;
+    a.table = table; a.rows = features; a.y = y;
+    HIP_TRY(embed_fwd(desc->dtype, a, (hipStream_t)hip_stream));
+    return MMTRAIN_OK;
+}
+
+size_t mmtrain_embed_workspace_bytes(const mmtrain_embed_desc *desc, int32_t n_tokens) {
+    if (check_embed(desc) != MMTRAIN_OK || n_tokens < 0 || n_tokens > EMBED_MAX_ROWS) return 0;
+    return embed_bwd_bytes(n_tokens, desc->hidden);
+}
+
+int mmtrain_embed_bwd(const mmtrain_embed_desc *desc, int32_t n_tokens, const int32_t *ids_dev, const void *dy, void *d_table,
+                      void *d_features, uint32_t flags, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    EmbedArgs a = {};
+    int rc = embed_common(desc, n_tokens, ids_dev, a);
+    if (rc) return rc;
+    if (flags & ~(MMTRAIN_BWD_ACCUMULATE_WGRAD | MMTRAIN_BWD_WGRAD_F32)) return MMTRAIN_ERR_INVALID_ARG;
+    if ((n_tokens > 0 && !dy) || (d_features && !desc->n_features) || misaligned({dy, d_table, d_features})) return MMTRAIN_ERR_INVALID_ARG;
+    if ((d_table && (d_table == dy || d_table == d_features)) || (d_features && d_features == dy)) return MMTRAIN_ERR_INVALID_ARG;
+    if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < embed_bwd_bytes(n_tokens, desc->hidden)) return MMTRAIN_ERR_WORKSPACE;
+    if (!d_table && !d_features) return MMTRAIN_OK;
+    a.dy = dy; a.d_table = d_table; a.d_rows = d_features; a.ws = workspace;
+    a.table_f32 = desc->dtype == MMTRAIN_F32 || (flags & MMTRAIN_BWD_WGRAD_F32);
+    a.accumulate = (flags & MMTRAIN_BWD_ACCUMULATE_WGRAD) != 0;
+    HIP_TRY(embed_bwd(desc->dtype, a, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 

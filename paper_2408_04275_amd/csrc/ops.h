@@ -65,4 +65,57 @@ hipError_t grad_norm_finish(const double *part, int n, float max_norm, bool add,
 bool grad_clip_streams(size_t bytes_written);       // by a whole call
 template <int N> hipError_t grad_clip(const GradBatch<N> &b, const GradResult *result, bool stream, hipStream_t st);
 
+// qk_norm.hip: per-head norms and rotation
+struct QkNormArgs {
+    RopeArgs r;                     // rows, heads (queries first), rotation (half = 0: none)
+    int nq, norm;                   // query heads; NORM_RMS or NORM_LAYER
+    float eps;
+    const void *q_w, *q_b, *k_w, *k_b;
+    const void *dy; long lddy;      // backward: r.y is dx (may be null)
+    float *part[4];                 // partial sums of q_w, q_b, k_w, k_b [qk_norm_bwd_blocks][d], null where not wanted
+    void *grad[4];
+    int grad_f32, accumulate;
+};
+constexpr int QK_MAX_ROWS = 1 << 30;
+hipError_t qk_norm_fwd(int dtype, const QkNormArgs &a, hipStream_t st);
+int qk_norm_bwd_blocks(int T);      // never fewer for more rows
+hipError_t qk_norm_bwd(int dtype, const QkNormArgs &a, hipStream_t st);
+
+// embed.hip
+constexpr int EMBED_MAX_ROWS = 1 << 30;
+struct EmbedArgs {
+    int T, H, vocab, features;
+    float scale;
+    const int *ids;
+    const void *table, *rows;       // forward
+    void *y;
+    const void *dy;                 // backward
+    void *d_table, *d_rows;         // null where not wanted
+    int table_f32, accumulate;
+    void *ws;
+};
+hipError_t embed_fwd(int dtype, const EmbedArgs &a, hipStream_t st);
+size_t embed_bwd_bytes(int T, int H);
+hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st);
+
+// cross_attn.hip
+constexpr int CROSS_MAX_SEGMENTS = 1 << 16;
+struct CrossArgs {
+    int Tq, Tk, S, nh, nkv, d;
+    float scale;
+    const int *cu, *begin, *end;    // device
+    const void *q; long ldq;
+    const void *k; long ldk;
+    const void *v; long ldv;
+    void *o; long ldo;
+    float *lse;                     // [nh, Tq]; forward: may be null
+    const void *d_o; long lddo;     // backward
+    void *dq; long lddq;            // null where not wanted
+    void *dk; long lddk;
+    void *dv; long lddv;
+    float *D;                       // backward scratch [nh, Tq]: rowsum(dO * O)
+};
+hipError_t cross_fwd(int dtype, const CrossArgs &a, hipStream_t st);
+hipError_t cross_bwd(int dtype, const CrossArgs &a, hipStream_t st);
+
 }  // namespace mmt
