@@ -36,6 +36,12 @@ int check_cross_batch(const mmtrain_cross_batch *b, bool ordered) {
     return MMTRAIN_OK;
 }
 
+// rows of a run and key/value head, log-sum-exps of a group: 32-bit numbers and byte offsets
+int check_sizes(const mmtrain_cross_attn_desc &d, const mmtrain_cross_batch &b) {
+    return (int64_t)b.q_tokens * (d.n_heads / d.n_kv_heads) > 1 << 28 || ((int64_t)b.q_tokens + b.n_segments) * d.n_heads > INT32_MAX ||
+           ((int64_t)b.kv_tokens / 16 + b.n_segments) * d.n_kv_heads > INT32_MAX ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
+}
+
 int check_rows(const mmtrain_cross_attn_desc &d, int heads, const void *p, int64_t ld) {
     if (!p || misaligned({p}) || ld < (int64_t)heads * d.head_dim) return MMTRAIN_ERR_INVALID_ARG;
     return ld % (d.dtype == MMTRAIN_F32 ? 4 : 8) || ld >= MAX_STRIDE ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
@@ -47,6 +53,10 @@ void fill(const mmtrain_cross_attn_desc &d, const mmtrain_cross_batch &b, CrossA
     a.nh = d.n_heads; a.nkv = d.n_kv_heads; a.d = d.head_dim;
     a.scale = d.softmax_scale > 0.f ? d.softmax_scale : 1.f / std::sqrt((float)d.head_dim);
     a.cu = b.cu_q_dev; a.begin = b.kv_begin_dev; a.end = b.kv_end_dev;
+}
+
+CrossShape shape_of(const mmtrain_cross_attn_desc &d, const mmtrain_cross_batch &b) {
+    return {b.q_tokens, b.kv_tokens, b.n_segments, d.n_heads, d.n_kv_heads, d.head_dim, b.cu_q_host, b.kv_begin_host, b.kv_end_host};
 }
 
 // q, k, v and o as the calls have them in common (k and v: only where there are keys)
@@ -65,22 +75,28 @@ int tensors_of(const mmtrain_cross_attn_desc &d, const mmtrain_cross_attn_tensor
 extern "C" {
 
 size_t mmtrain_cross_attn_workspace_bytes(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, int is_bwd) {
-    if (check_cross(desc) || check_cross_batch(batch, false)) return 0;
-    return (is_bwd ? (size_t)batch->q_tokens * desc->n_heads * sizeof(float) : 0) + 256;
+    if (check_cross(desc) || check_cross_batch(batch, false) || check_sizes(*desc, *batch)) return 0;
+    if (is_bwd) return (size_t)batch->q_tokens * desc->n_heads * sizeof(float) + 256;
+    const CrossShape c = shape_of(*desc, *batch);
+    return (desc->dtype == MMTRAIN_BF16 ? cross_mfma_fwd_bytes(c, cross_mfma_fwd_plan(c)) : 0) + 256;
 }
 
 int mmtrain_cross_attn_fwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, const mmtrain_cross_attn_tensors *tensors,
                            void *workspace, size_t workspace_bytes, void *hip_stream) {
     int rc = check_cross(desc);
-    if (rc || (rc = check_cross_batch(batch, false))) return rc;
+    if (rc || (rc = check_cross_batch(batch, false)) || (rc = check_sizes(*desc, *batch))) return rc;
     CrossArgs a;
     fill(*desc, *batch, a);
     if ((rc = tensors_of(*desc, tensors, a))) return rc;
     if (a.Tq == 0) return MMTRAIN_OK;
     if (a.o == a.q || a.o == a.k || a.o == a.v) return MMTRAIN_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < mmtrain_cross_attn_workspace_bytes(desc, batch, 0)) return MMTRAIN_ERR_WORKSPACE;
-    HIP_TRY(cross_fwd(desc->dtype, a, (hipStream_t)hip_stream));
+    hipStream_t st = (hipStream_t)hip_stream;
+    const CrossShape c = shape_of(*desc, *batch);
+    const bool bf16 = desc->dtype == MMTRAIN_BF16;
+    const CrossPlan plan = bf16 ? cross_mfma_fwd_plan(c) : CrossPlan{};
+    if (!workspace || workspace_bytes < (bf16 ? cross_mfma_fwd_bytes(c, plan) : 0) + 256) return MMTRAIN_ERR_WORKSPACE;
+    HIP_TRY(bf16 ? cross_mfma_fwd(a, plan, workspace, st) : cross_fwd(desc->dtype, a, st));
     return MMTRAIN_OK;
 }
 
@@ -89,7 +105,7 @@ int mmtrain_cross_attn_bwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
     int rc = check_cross(desc);
     if (rc) return rc;
     if (!grads || !grads->d_k != !grads->d_v) return MMTRAIN_ERR_INVALID_ARG;
-    if ((rc = check_cross_batch(batch, grads->d_k != nullptr))) return rc;
+    if ((rc = check_cross_batch(batch, grads->d_k != nullptr)) || (rc = check_sizes(*desc, *batch))) return rc;
     CrossArgs a;
     fill(*desc, *batch, a);
     if ((rc = tensors_of(*desc, tensors, a))) return rc;

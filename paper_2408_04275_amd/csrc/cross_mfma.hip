@@ -1,0 +1,628 @@
+// Attention of runs of queries to ranges of keys on the gfx950 matrix cores (bf16 in, fp32 accumulate).
+//
+// All tokens of a run see the same keys, and the query heads of a group share them.  So the rows of a tile are (token, head of the group)
+// pairs of ONE run and key/value head -- row r is token r / group, head r % group -- and what a workgroup walks is the run's keys and
+// nothing else: no row has a mask of its own, only the last block of keys ends early.  Rows and keys that do not exist are read as
+// zeros (the bounds of the buffer descriptor), so nothing that belongs to others, an infinity or NaN in the next run's keys, can enter a product.
+//
+// Scores are computed transposed, as in attn_mfma.hip: a lane holds 16 keys of ONE row per block of 32 keys.
+#include "ops.h"
+#include "attn_tiles.h"
+#include <algorithm>
+#include <atomic>
+
+namespace mmt {
+
+namespace {
+
+constexpr int KEYS = 64;                                // a step of the tile kernel
+template <int D> constexpr int ROWS32 = 32 * D * 2;     // bytes of 32 rows in LDS
+template <int D> constexpr int STAGE = 32 * (2 * D + 16);
+
+// all but the N youngest LDS reads that are written as assembly have landed, x's among them
+template <int N, typename V>
+__device__ __forceinline__ void lds_wait(V &x) { asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(x) : "n"(N)); }
+
+// ---- which rows and keys a workgroup has ----------------------------------------------------------------------------
+__host__ __device__ inline int items_of(int tokens, int keys, int group, int tile_rows, int chunk) {
+    const int tiles = (tokens * group + tile_rows - 1) / tile_rows, parts = chunk ? (keys + chunk - 1) / chunk : 1;
+    return tiles * (parts > 0 ? parts : 1);
+}
+
+struct Item {
+    int q0, rows, lo, hi;       // run: first token, rows of a key/value head, keys
+    int index, first;           // the item's number within its run; of the run's first item among all
+};
+
+// Item y of all runs' items.  Up to 64 runs: one per lane, their items added up across the wavefront; more: from the table that
+// cross_prefix_kernel left.
+__device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_rows, int chunk) {
+    const int group = a.nh / a.nkv, lane = threadIdx.x & 63;
+    Item it;
+    if (a.S <= 64) {
+        int c0 = 0, c1 = 0, lo = 0, hi = 0;
+        if (lane < a.S) { c0 = a.cu[lane]; c1 = a.cu[lane + 1]; lo = a.begin[lane]; hi = a.end[lane]; }
+        const int n = lane < a.S ? items_of(c1 - c0, hi - lo, group, tile_rows, chunk) : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += v;
+        }
+        const int s = min(__popcll(__builtin_amdgcn_ballot_w64(sum <= y)), 63);
+        it.q0 = __builtin_amdgcn_readlane(c0, s);
+        it.rows = (__builtin_amdgcn_readlane(c1, s) - it.q0) * group;
+        it.lo = __builtin_amdgcn_readlane(lo, s);
+        it.hi = __builtin_amdgcn_readlane(hi, s);
+        it.first = __builtin_amdgcn_readlane(sum - n, s);
+    } else {
+        const int s = __builtin_amdgcn_readfirstlane(find_segment(a.prefix, a.S, y));
+        it.q0 = __builtin_amdgcn_readfirstlane(a.cu[s]);
+        it.rows = (__builtin_amdgcn_readfirstlane(a.cu[s + 1]) - it.q0) * group;
+        it.lo = __builtin_amdgcn_readfirstlane(a.begin[s]);
+        it.hi = __builtin_amdgcn_readfirstlane(a.end[s]);
+        it.first = __builtin_amdgcn_readfirstlane(a.prefix[s]);
+    }
+    it.index = y - it.first;
+    return it;
+}
+
+// exclusive sums of the runs' items, [S + 1]: one workgroup
+__global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int tile_rows, int chunk, int *out) {
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 1024) {
+        const int s = s0 + threadIdx.x;
+        const int n = s < a.S ? items_of(a.cu[s + 1] - a.cu[s], a.end[s] - a.begin[s], a.nh / a.nkv, tile_rows, chunk) : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += v;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        int before = base, all = base;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) before += sums[w];
+            all += sums[w];
+        }
+        if (s < a.S) out[s] = before + sum - n;
+        base = all;
+    }
+    if (threadIdx.x == 0) out[a.S] = base;
+}
+
+// Division of a small number (below group + 128) by the group: a product's high half (exact while number * group < 2^32)
+struct Group {
+    int n;
+    uint32_t magic;
+    __device__ __forceinline__ Group(const CrossArgs &a) : n(a.nh / a.nkv), magic(0xffffffffu / (uint32_t)n + 1u) {}
+    __device__ __forceinline__ int token(int r) const { return n == 1 ? r : (int)__umulhi((uint32_t)r, magic); }
+};
+
+// 32 rows of a run from row0 on: row i is token t + token(j + i), head of the group (j + i) % group
+struct Rows {
+    int t, j, left;             // first token, its first head, rows that exist
+    __device__ __forceinline__ Rows(const Item &it, const Group &g, int row0) {
+        const int tok = row0 / g.n;
+        t = it.q0 + tok;
+        j = row0 - tok * g.n;
+        left = it.rows - row0;
+    }
+    // elements from the first token's row of the group (stride ld, heads d wide)
+    __device__ __forceinline__ uint32_t offset(const Group &g, int i, long ld, int d) const {
+        const int tok = g.token(j + i);
+        return (uint32_t)(tok * (int)ld + (j + i - tok * g.n) * d);
+    }
+};
+
+// n rows of dh features: what stands behind them reads as zero
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const bf16_t *p, long row, long ld, int n, int dh) {
+    const uint32_t bytes = n > 0 ? (uint32_t)((min(n, 64) - 1) * (int)ld + dh) * 2u : 0u;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p + row * ld), 0, (int)bytes, 0x00020000);
+}
+
+// Copies 32 rows (`at`, of a tensor with stride ld whose group of heads starts at p) into LDS, row-major and swizzled
+template <int D>
+__device__ __forceinline__ void copy_rows(const bf16_t *p, long ld, int dh, const Rows &at, const Group &g, uint8_t *to) {
+    constexpr int UPR = D / 8, PER = 1024 / (2 * D), N = ROWS32<D> / 1024;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p + at.t * ld), 0, 0x7fff0000, 0x00020000);
+    const int lane = threadIdx.x & 63, lrow = lane / UPR, pos = lane % UPR;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = i * PER + lrow, unit = pos ^ swz_unit<D>(row);
+        const uint32_t off = row < at.left && unit * 8 < dh ? (at.offset(g, row, ld, dh) + unit * 8) * 2u : 0x80000000u;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(to + i * PER * 2 * D), 16, (int)off, 0, 0, 0);
+    }
+}
+
+// 32 x D results of a wavefront (a lane holds a row) as bf16 rows, through LDS so that neighbouring lanes store neighbouring pieces
+template <int D, int CB>
+__device__ __forceinline__ void store_rows_at(uint8_t *stage, const f32x16 (&acc)[CB], float scale, bf16_t *p, long ld, int dh, const Rows &at, const Group &g) {
+    constexpr int RS = 2 * D + 16, LPR = D / 8, RPI = 64 / LPR;
+    const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq) {
+            uint2 w;
+            w.x = pack_bf16x2(acc[c][4 * gq] * scale, acc[c][4 * gq + 1] * scale);
+            w.y = pack_bf16x2(acc[c][4 * gq + 2] * scale, acc[c][4 * gq + 3] * scale);
+            *reinterpret_cast<uint2 *>(stage + l32 * RS + (32 * c + 8 * gq + 4 * half) * 2) = w;
+        }
+    const int r0 = lane / LPR, cb = (lane % LPR) * 8;
+    bf16_t *const first = p + at.t * ld;
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+        const int r = i * RPI + r0;
+        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * RS + cb * 2);
+        if (r < at.left && cb < dh) *reinterpret_cast<uint4 *>(first + at.offset(g, r, ld, dh) + cb) = v;
+    }
+}
+
+__device__ __forceinline__ float natural_lse(float m, float l, float sl2) { return (m * sl2 + __builtin_amdgcn_logf(l)) * LN2; }
+
+// ---- forward, many rows ------------------------------------------------------------------------------------------------
+// WAVES wavefronts x 32 rows, keys 64 at a time through two LDS slots.  Each wavefront works one block of 32 keys ahead, as
+// attn_mfma.hip's forward kernel does: the next block's scores are multiplied between the exponentials of the current one, and a
+// step's K tile stands one block further on than its V tile.
+template <int D, int WAVES> constexpr int FWD_LDS = 2 * 2 * KEYS * D * 2 + (WAVES == 8 ? 9 : 1) * ROWS32<D>;
+
+template <int D, int KS, int CB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
+    constexpr int TILE = KEYS * D * 2, SLOT = 2 * TILE, COPIES = TILE / 1024 / 4;
+    constexpr int Q_AT = WAVES == 8 ? 2 * SLOT : SLOT, K_FIRST = WAVES == 8 ? 2 * SLOT + 8 * ROWS32<D> : 2 * SLOT;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    const int head = blockIdx.x % a.nkv, dh = a.d;
+    const Item it = find_item(a, blockIdx.x / a.nkv, WAVES * 32, 0);
+    const Group g(a);
+    const Rows mine(it, g, it.index * WAVES * 32 + wave * 32);
+    const int kbeg = it.lo, kend = it.hi;
+    const bf16_t *const K = (const bf16_t *)a.k + (long)head * dh, *const V = (const bf16_t *)a.v + (long)head * dh;
+
+    bf16x8 qf[KS];
+    f32x16 oacc[CB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) oacc[c] = zero16();
+    float m_run = -INFINITY, msc = 0.f, l_run = 0.f;    // reference of the exponentials (raw score), in the exponent's units, row sum
+    const float sl2 = a.scale * LOG2E;
+
+    RowCopier<D, COPIES> cpk, cpv;
+    cpk.init((wave & 3) * COPIES, a.ldk, dh);
+    cpv.init((wave & 3) * COPIES, a.ldv, dh);
+    auto copy_kv = [&](uint8_t *slot, int kt) {
+        if (WAVES == 4 || wave >= 4) cpk.issue(rows_rsrc(K, kt + 32, a.ldk, kend - kt - 32, dh), slot, 0, 0, 0);
+        if (WAVES == 4 || wave < 4) cpv.issue(rows_rsrc(V, kt, a.ldv, kend - kt, dh), slot + TILE, 0, 0, 0);
+    };
+    uint8_t *const st_q = smem + Q_AT + wave * ROWS32<D>;
+    copy_rows<D>((const bf16_t *)a.q + (long)head * g.n * dh, a.ldq, dh, mine, g, st_q);
+    if (wave >= WAVES - 4 && wave < WAVES - 2) cpk.issue(rows_rsrc(K, kbeg, a.ldk, kend - kbeg, dh), smem + K_FIRST, 0, 0, 0);
+    copy_kv(smem, kbeg);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = frag_k<D>(st_q, l32, ks, half);
+
+    TrReader<D> tr;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    tr.init(lds0);
+    uint32_t kadr[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kadr[ks] = lds0 + (l32 * (D / 8) + ((2 * ks + half) ^ swz_unit<D>(l32))) * 16;
+    f32x16 s[2];                                         // scores of the blocks of either parity
+    uint32_t pp[8];
+    // element i of a block: its exponential, the row sum, packed in pairs.  Register i  <->  key kb + 8 (i >> 2) + 4 half + (i & 3)
+    auto element = [&](auto I_, const f32x16 &cur, float &keep) {
+        constexpr int i = decltype(I_)::value;
+        const float p = __builtin_amdgcn_exp2f(fmaf(cur[i], sl2, -msc));
+        l_run += p;
+        asm volatile("" : "+v"(l_run));
+        if constexpr (i & 1) pp[i >> 1] = pack_bf16x2(keep, p);
+        else keep = p;
+    };
+    auto p_frag = [&](auto M_) {
+        constexpr int m = decltype(M_)::value;
+        const rawx4 w = {pp[4 * m], pp[4 * m + 1], pp[4 * m + 2], pp[4 * m + 3]};
+        return *reinterpret_cast<const bf16x8 *>(&w);
+    };
+    auto mask = [&](f32x16 &x, int kb) {
+        const int left = kend - kb - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 8 * (i >> 2) + (i & 3) < left ? x[i] : -INFINITY;
+    };
+    auto max16 = [&](const f32x16 &x) {
+        float mx = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+        return mx;
+    };
+    float m_limit = -INFINITY;                           // the maximum that moves the reference
+    const float lazy = LAZY_LOG2 / sl2;
+    auto follow = [&](float mx, auto STRICT_) {
+        if (__builtin_amdgcn_ballot_w64(mx > m_limit) == 0) return;
+        mx = max_across_halves(mx);
+        const bool need = mx > m_limit;
+        const float corr = need ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
+        m_run = need ? mx : m_run;
+        m_limit = decltype(STRICT_)::value ? m_run : m_run + lazy;
+        msc = m_run == -INFINITY ? 0.f : m_run * sl2;
+        l_run *= corr;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[c][i] *= corr;
+    };
+    // block b of a step, whose scores are in s[b]: its exponentials and products with V, and the scores of the block behind it (keys nb ..)
+    auto block = [&](auto SLOT_, auto B_, int nb) {
+        constexpr int b = decltype(B_)::value, NI = KS + 2 * CB, AHEAD = 4, AT = decltype(SLOT_)::value * SLOT;
+        const f32x16 &cur = s[b];
+        f32x16 &nxt = s[b ^ 1];
+        bf16x8 fr[KS];
+        shortx4 v0[2 * CB], v1[2 * CB];
+        auto issue = [&](auto X_) {
+            constexpr int x = decltype(X_)::value;
+            if constexpr (x < KS) lds_read16<AT + b * 64 * D>(fr[x], kadr[x]);
+            else if constexpr (x < NI) {
+                constexpr int m = (x - KS) / CB, c = (x - KS) % CB;
+                v0[x - KS] = TrReader<D>::template read_at<b, m, c, 0, AT + TILE>(tr.off);
+                v1[x - KS] = TrReader<D>::template read_at<b, m, c, 1, AT + TILE>(tr.off);
+            }
+        };
+        float keep = 0.f, mx = -INFINITY;
+        static_for<0, AHEAD>([&](auto X_) { issue(X_); });
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int E0 = 2, SPAN = KS + CB;
+        static_for<0, E0>([&](auto I_) { element(I_, cur, keep); });
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<0, NI>([&](auto X_) {
+            constexpr int x = decltype(X_)::value;
+            constexpr int behind = lds_ops<KS, NI>(x + 1, x + AHEAD);       // reads issued behind item x's
+            if constexpr (x < KS) {
+                asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(fr[x]) : "n"(behind));
+                if constexpr (x == 0) nxt = MFMA(fr[x], qf[x], zero16());
+                else nxt = MFMA(fr[x], qf[x], nxt);
+            } else {
+                constexpr int m = (x - KS) / CB, c = (x - KS) % CB;
+                asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(v0[x - KS]), "+v"(v1[x - KS]) : "n"(behind));
+                oacc[c] = MFMA(join(v0[x - KS], v1[x - KS]), p_frag(std::integral_constant<int, m>{}), oacc[c]);
+            }
+            issue(std::integral_constant<int, x + AHEAD>{});
+            constexpr int lo = x < SPAN ? E0 + (16 - E0) * x / SPAN : 16, hi = x + 1 < SPAN ? E0 + (16 - E0) * (x + 1) / SPAN : 16;
+            static_for<lo, hi>([&](auto I_) { element(I_, cur, keep); });
+            if constexpr (x > KS) {
+                constexpr int d0 = 16 * (x - KS - 1) / (2 * CB - 1), d1 = 16 * (x - KS) / (2 * CB - 1);
+                static_for<d0, d1>([&](auto I_) { mx = fmaxf(mx, nxt[decltype(I_)::value]); });
+                asm volatile("" : "+v"(mx));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (nb + 32 > kend) {
+            mask(nxt, nb);
+            mx = max16(nxt);
+        }
+        follow(mx, std::false_type{});
+    };
+    auto step = [&](auto SLOT_, int kt) {
+        constexpr int slot = decltype(SLOT_)::value;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this step's tiles have landed
+        lds_barrier();                                               // ... and everyone is done with the other slot
+        if (kt == kbeg) {
+            f32x16 x = zero16();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) x = MFMA(lds_load<bf16x8>(kadr[ks] + K_FIRST), qf[ks], x);
+            if (kbeg + 32 > kend) mask(x, kbeg);
+            s[0] = x;
+            follow(max16(x), std::true_type{});
+        }
+        block(SLOT_, std::integral_constant<int, 0>{}, kt + 32);
+        // (behind the first block: right behind the barrier all wavefronts would wait for each other at the copies)
+        if (kt + KEYS < kend) copy_kv(smem + (slot ^ 1) * SLOT, kt + KEYS);
+        if (kt + 32 < kend) block(SLOT_, std::integral_constant<int, 1>{}, kt + KEYS);
+    };
+    for (int kt = kbeg; kt < kend; kt += 2 * KEYS) {
+        step(std::integral_constant<int, 0>{}, kt);
+        if (kt + KEYS >= kend) break;
+        step(std::integral_constant<int, 1>{}, kt + KEYS);
+    }
+
+    lds_barrier();                                       // the tiles are done with: LDS now stages the output rows
+    const float l_tot = sum_across_halves(l_run);
+    store_rows_at<D, CB>(smem + wave * STAGE<D>, oacc, l_tot > 0.f ? 1.f / l_tot : 0.f, (bf16_t *)a.o + (long)head * g.n * dh, a.ldo, dh, mine, g);
+    if (a.lse && half == 0 && l32 < mine.left) {
+        const int tok = g.token(mine.j + l32), h = head * g.n + mine.j + l32 - tok * g.n;
+        a.lse[(long)h * a.Tq + mine.t + tok] = natural_lse(m_run, l_tot, sl2);
+    }
+}
+
+// ---- forward, few rows ----------------------------------------------------------------------------------------------------
+// Up to 32 rows per workgroup, whose four wavefronts share out the blocks of 32 keys, each with two LDS slots of its own and no barrier on
+// the way: the next block is in flight while this one is multiplied.  Where that leaves the chip empty or one workgroup with a long walk, the keys
+// are cut into chunks, one per workgroup, whose partial results (32 rows of fp32, maximum and sum) cross_combine_kernel joins.
+constexpr int FEW_ROWS = 32;
+template <int D> constexpr int FEW_LDS = 4 * 4 * ROWS32<D>;
+
+template <int D, int KS, int CB>
+__global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
+    constexpr int N = ROWS32<D> / 1024, SLOT = 2 * ROWS32<D>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem_all[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
+    uint8_t *const smem = smem_all + wave * 2 * SLOT;
+    const int head = blockIdx.x % a.nkv, dh = a.d;
+    const Item it = find_item(a, blockIdx.x / a.nkv, FEW_ROWS, a.chunk);
+    const int parts = a.chunk ? max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1) : 1;
+    const Group g(a);
+    const Rows mine(it, g, it.index / parts * FEW_ROWS);
+    const int kbeg = it.lo + it.index % parts * a.chunk, kend = parts > 1 ? min(kbeg + a.chunk, it.hi) : it.hi;
+    const bf16_t *const K = (const bf16_t *)a.k + (long)head * dh, *const V = (const bf16_t *)a.v + (long)head * dh;
+    const float sl2 = a.scale * LOG2E;
+
+    RowCopier<D, N> cpk, cpv;
+    cpk.init(0, a.ldk, dh);
+    cpv.init(0, a.ldv, dh);
+    auto copy_kv = [&](uint8_t *slot, int kb) {
+        cpk.issue(rows_rsrc(K, kb, a.ldk, min(kend - kb, 32), dh), slot, 0, 0, 0);
+        cpv.issue(rows_rsrc(V, kb, a.ldv, min(kend - kb, 32), dh), slot + ROWS32<D>, 0, 0, 0);
+    };
+    int kb = kbeg + 32 * wave;
+    copy_rows<D>((const bf16_t *)a.q + (long)head * g.n * dh, a.ldq, dh, mine, g, smem + SLOT);
+    if (kb < kend) {
+        copy_kv(smem, kb);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N) : "memory");
+    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
+    uint32_t kadr[KS];
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kadr[ks] = lds0 + (l32 * (D / 8) + ((2 * ks + half) ^ swz_unit<D>(l32))) * 16;
+    static_for<0, KS>([&](auto K_) { lds_read16<SLOT>(qf[decltype(K_)::value], kadr[decltype(K_)::value]); });
+    static_for<0, KS>([&](auto K_) { lds_wait<0>(qf[decltype(K_)::value]); });
+    TrReader<D> tr;
+    tr.init(lds0);
+    f32x16 oacc[CB];
+#pragma unroll
+    for (int c = 0; c < CB; ++c) oacc[c] = zero16();
+    float m_run = -INFINITY, l_run = 0.f;
+    auto block = [&](auto SLOT_, int kb) {
+        constexpr int AT = decltype(SLOT_)::value * SLOT;
+        bf16x8 fr[KS];
+        shortx4 v0[2 * CB], v1[2 * CB];
+        static_for<0, KS>([&](auto K_) { lds_read16<AT>(fr[decltype(K_)::value], kadr[decltype(K_)::value]); });
+        f32x16 s = zero16();
+        static_for<0, KS>([&](auto K_) {
+            constexpr int ks = decltype(K_)::value;
+            lds_wait<KS - 1 - ks>(fr[ks]);
+            s = MFMA(fr[ks], qf[ks], s);
+        });
+        static_for<0, 2 * CB>([&](auto X_) {
+            constexpr int x = decltype(X_)::value;
+            v0[x] = TrReader<D>::template read_at<0, x / CB, x % CB, 0, AT + ROWS32<D>>(tr.off);
+            v1[x] = TrReader<D>::template read_at<0, x / CB, x % CB, 1, AT + ROWS32<D>>(tr.off);
+        });
+        if (kb + 32 > kend) {
+            const int left = kend - kb - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < left ? s[i] : -INFINITY;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        mx = max_across_halves(mx);
+        const bool need = (mx - m_run) * sl2 > LAZY_LOG2;
+        if (__builtin_amdgcn_ballot_w64(need) != 0) {
+            const float corr = need ? __builtin_amdgcn_exp2f((m_run - mx) * sl2) : 1.f;
+            m_run = need ? mx : m_run;
+            l_run *= corr;
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) oacc[c][i] *= corr;
+        }
+        const float msc = m_run == -INFINITY ? 0.f : m_run * sl2;
+        float p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sl2, -msc));
+            l_run += p[i];
+        }
+        const bf16x8 pf[2] = {pack8(p), pack8(p + 8)};
+        static_for<0, 2 * CB>([&](auto X_) {
+            lds_wait<0>(v0[decltype(X_)::value]);
+            lds_wait<0>(v1[decltype(X_)::value]);
+        });
+        static_for<0, 2 * CB>([&](auto X_) {
+            constexpr int x = decltype(X_)::value;
+            oacc[x % CB] = MFMA(join(v0[x], v1[x]), pf[x / CB], oacc[x % CB]);
+        });
+    };
+    auto step = [&](auto SLOT_) {
+        constexpr int slot = decltype(SLOT_)::value;
+        asm volatile("" ::: "memory");
+        if (kb + 128 < kend) {                           // (the other slot has been read: its reads have been waited for)
+            copy_kv(smem + (slot ^ 1) * SLOT, kb + 128);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N) : "memory");
+        } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        block(SLOT_, kb);
+        kb += 128;
+    };
+    while (kb < kend) {
+        step(std::integral_constant<int, 0>{});
+        if (kb >= kend) break;
+        step(std::integral_constant<int, 1>{});
+    }
+
+    asm volatile("" ::: "memory");
+    // four partial softmaxes over disjoint keys become one: each wavefront joins one block of 32 features
+    put_acc(smem, oacc);
+    const float l_own = sum_across_halves(l_run);
+    float2 *const ml = reinterpret_cast<float2 *>(smem + SLOT);
+    if (half == 0) ml[l32] = make_float2(m_run, l_own);
+    lds_barrier();
+    float m = -INFINITY, l = 0.f, mw[4], f[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float2 v = reinterpret_cast<const float2 *>(smem_all + w * 2 * SLOT + SLOT)[l32];
+        mw[w] = v.x; f[w] = v.y;
+        m = fmaxf(m, v.x);
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float e = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw[w] - m) * sl2);
+        l += f[w] * e;
+        f[w] = e;
+    }
+    const int tok = g.token(mine.j + l32), h = mine.j + l32 - tok * g.n;
+    const bool live = l32 < mine.left;
+    if (wave < CB) {
+        f32x4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[i] += reinterpret_cast<const f32x4 *>(smem_all + w * 2 * SLOT)[(4 * wave + i) * 64 + lane] * f[w];
+        }
+        const int c0 = 32 * wave + 4 * half;
+        if (parts > 1) {
+            float *out = a.part + ((size_t)blockIdx.x * FEW_ROWS + l32) * dh + c0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (live && c0 + 8 * i < dh) *reinterpret_cast<f32x4 *>(out + 8 * i) = x[i];
+        } else {
+            const float r = l > 0.f ? 1.f / l : 0.f;
+            bf16_t *out = (bf16_t *)a.o + (mine.t + tok) * a.ldo + (long)(head * g.n + h) * dh + c0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (live && c0 + 8 * i < dh)
+                    *reinterpret_cast<uint2 *>(out + 8 * i) = make_uint2(pack_bf16x2(x[i][0] * r, x[i][1] * r), pack_bf16x2(x[i][2] * r, x[i][3] * r));
+        }
+    }
+    if (wave == 3 && half == 0 && live) {
+        if (parts > 1) a.part_ml[(size_t)blockIdx.x * FEW_ROWS + l32] = make_float2(m, l);
+        else if (a.lse) a.lse[(long)(head * g.n + h) * a.Tq + mine.t + tok] = natural_lse(m, l, sl2);
+    }
+}
+
+// The chunks' results of up to 32 rows; a workgroup for each of the kernel's above, of which the one of a chunk 0 does it
+__global__ __launch_bounds__(256) void cross_combine_kernel(CrossArgs a) {
+    const int head = blockIdx.x % a.nkv, dh = a.d;
+    const Item it = find_item(a, blockIdx.x / a.nkv, FEW_ROWS, a.chunk);
+    const int parts = max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1);
+    if (parts == 1 || it.index % parts) return;
+    const Group g(a);
+    const Rows mine(it, g, it.index / parts * FEW_ROWS);
+    const float sl2 = a.scale * LOG2E;
+    const int quads = dh / 4, rows = min(mine.left, FEW_ROWS);
+    const size_t stride = (size_t)a.nkv * FEW_ROWS;
+    for (int e = threadIdx.x; e < rows * quads; e += 256) {
+        const int r = e / quads, c = e % quads * 4;
+        const float2 *ml = a.part_ml + (size_t)blockIdx.x * FEW_ROWS + r;
+        const float *part = a.part + ((size_t)blockIdx.x * FEW_ROWS + r) * dh + c;
+        float m = -INFINITY, l = 0.f;
+        for (int j = 0; j < parts; ++j) m = fmaxf(m, ml[j * stride].x);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < parts; ++j) {
+            const float2 v = ml[j * stride];
+            const float w = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - m) * sl2);
+            l += v.y * w;
+            x += *reinterpret_cast<const f32x4 *>(part + j * stride * dh) * w;
+        }
+        const int tok = g.token(mine.j + r), h = head * g.n + mine.j + r - tok * g.n;
+        const float f = l > 0.f ? 1.f / l : 0.f;
+        *reinterpret_cast<uint2 *>((bf16_t *)a.o + (mine.t + tok) * a.ldo + (long)h * dh + c) =
+            make_uint2(pack_bf16x2(x[0] * f, x[1] * f), pack_bf16x2(x[2] * f, x[3] * f));
+        if (a.lse && c == 0) a.lse[(long)h * a.Tq + mine.t + tok] = natural_lse(m, l, sl2);
+    }
+}
+
+template <typename K>
+hipError_t set_smem(std::atomic<bool> &done, K kern, int bytes) {
+    if (done.load(std::memory_order_acquire)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.store(true, std::memory_order_release);
+    return e;
+}
+
+template <int D, int KS, int CB, int WAVES>
+hipError_t launch_tiles(const CrossArgs &a, int items, hipStream_t st) {
+    static std::atomic<bool> done{false};
+    constexpr int LDS = std::max(FWD_LDS<D, WAVES>, WAVES * STAGE<D>);
+    const hipError_t e = set_smem(done, cross_fwd_kernel<D, KS, CB, WAVES>, LDS);
+    if (e != hipSuccess) return e;
+    cross_fwd_kernel<D, KS, CB, WAVES><<<items * a.nkv, WAVES * 64, LDS, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int D, int KS, int CB>
+hipError_t launch_few(const CrossArgs &a, int items, hipStream_t st) {
+    static std::atomic<bool> done{false};
+    const hipError_t e = set_smem(done, cross_fwd_few_kernel<D, KS, CB>, FEW_LDS<D>);
+    if (e != hipSuccess) return e;
+    cross_fwd_few_kernel<D, KS, CB><<<items * a.nkv, 256, FEW_LDS<D>, st>>>(a);
+    if (a.chunk) cross_combine_kernel<<<items * a.nkv, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int D, int KS, int CB>
+hipError_t launch_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st) {
+    return p.rows == FEW_ROWS ? launch_few<D, KS, CB>(a, p.items, st)
+                              : p.rows == 256 ? launch_tiles<D, KS, CB, 8>(a, p.items, st) : launch_tiles<D, KS, CB, 4>(a, p.items, st);
+}
+
+}  // namespace
+
+// How a forward pass is cut: by the rows of the runs and the keys they see
+CrossPlan cross_mfma_fwd_plan(const CrossShape &c) {
+    const int group = c.nh / c.nkv;
+    auto count = [&](int rows, int chunk) {
+        long n = 0;
+        for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], group, rows, chunk);
+        return n;
+    };
+    // steps of 32 rows and 32 keys
+    long few = 0, many = 0, longest = 0;
+    for (int s = 0; s < c.S; ++s) {
+        const long keys = (c.end[s] - c.begin[s] + 31) / 32, rows = (long)(c.cu[s + 1] - c.cu[s]) * group;
+        few += (rows + 31) / 32 * keys;
+        many += (rows + 127) / 128 * 4 * keys;
+        longest = std::max(longest, keys);
+    }
+    CrossPlan p = {};
+    if (many > 2 * few || count(128, 0) * c.nkv < 128) {
+        p.rows = FEW_ROWS;
+        const long whole = count(FEW_ROWS, 0) * c.nkv;
+        if (whole < 512 && longest > 32) {
+            const long want = std::max(few * c.nkv / 1024, 8l);      // blocks a workgroup
+            p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
+            if (p.chunk >= longest * 32) p.chunk = 0;
+        }
+    } else p.rows = c.d > 64 ? 256 : 128;
+    p.items = (int)count(p.rows, p.chunk);
+    p.table = c.S > 64;
+    return p;
+}
+
+size_t cross_mfma_fwd_bytes(const CrossShape &c, const CrossPlan &p) {
+    return (p.table ? (((size_t)(c.S + 1) * sizeof(int) + 255) & ~size_t(255)) : 0) +
+           (p.chunk ? (size_t)p.items * c.nkv * FEW_ROWS * (c.d * sizeof(float) + sizeof(float2)) : 0);
+}
+
+hipError_t cross_mfma_fwd(const CrossArgs &args, const CrossPlan &p, void *ws, hipStream_t st) {
+    CrossArgs a = args;
+    uint8_t *at = (uint8_t *)ws;
+    if (p.table) {
+        a.prefix = (int *)at;
+        cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, p.chunk, (int *)at);
+        at += ((size_t)(a.S + 1) * sizeof(int) + 255) & ~size_t(255);
+    }
+    a.chunk = p.chunk;
+    if (p.chunk) {
+        a.part = (float *)at;
+        a.part_ml = (float2 *)(a.part + (size_t)p.items * a.nkv * FEW_ROWS * a.d);
+    }
+    return a.d <= 64 ? launch_fwd<64, 4, 2>(a, p, st) : a.d <= 80 ? launch_fwd<128, 5, 3>(a, p, st) : a.d <= 96 ? launch_fwd<128, 6, 3>(a, p, st)
+                                                                                                          : launch_fwd<128, 8, 4>(a, p, st);
+}
+
+}  // namespace mmt

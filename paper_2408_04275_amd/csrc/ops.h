@@ -114,7 +114,21 @@ struct CrossArgs {
     void *dk; long lddk;
     void *dv; long lddv;
     float *D;                       // backward scratch [nh, Tq]: rowsum(dO * O)
+    // cross_mfma.hip
+    const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
+    int chunk;                      // keys of a workgroup with few rows; 0: all of its run's
+    float *part; float2 *part_ml;   // partial results of the chunks
 };
+// What a call is planned from: sizes, and the runs' host arrays
+struct CrossShape { int Tq, Tk, S, nh, nkv, d; const int *cu, *begin, *end; };
+struct CrossPlan {
+    int rows, chunk, items;         // rows of a workgroup, keys of a chunk (0: not cut), workgroups per key/value head
+    bool table;                     // items are found in a table
+};
+// bf16 forward.  The workspace is 256-byte aligned.
+CrossPlan cross_mfma_fwd_plan(const CrossShape &c);
+size_t cross_mfma_fwd_bytes(const CrossShape &c, const CrossPlan &p);
+hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, void *ws, hipStream_t st);
 hipError_t cross_fwd(int dtype, const CrossArgs &a, hipStream_t st);
 hipError_t cross_bwd(int dtype, const CrossArgs &a, hipStream_t st);
 
