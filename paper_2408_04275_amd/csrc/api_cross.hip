@@ -76,8 +76,11 @@ extern "C" {
 
 size_t mmtrain_cross_attn_workspace_bytes(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, int is_bwd) {
     if (check_cross(desc) || check_cross_batch(batch, false) || check_sizes(*desc, *batch)) return 0;
-    if (is_bwd) return (size_t)batch->q_tokens * desc->n_heads * sizeof(float) + 256;
     const CrossShape c = shape_of(*desc, *batch);
+    if (is_bwd) {
+        if (desc->dtype == MMTRAIN_F32) return (size_t)batch->q_tokens * desc->n_heads * sizeof(float) + 256;
+        return cross_mfma_bwd_bytes(c, cross_mfma_bwd_plan(c, check_cross_batch(batch, true) == MMTRAIN_OK)) + 256;
+    }
     return (desc->dtype == MMTRAIN_BF16 ? cross_mfma_fwd_bytes(c, cross_mfma_fwd_plan(c)) : 0) + 256;
 }
 
@@ -120,11 +123,15 @@ int mmtrain_cross_attn_bwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
         if (out[i] && out[i] == out[(i + 1) % 3]) return MMTRAIN_ERR_INVALID_ARG;
     }
     if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < mmtrain_cross_attn_workspace_bytes(desc, batch, 1)) return MMTRAIN_ERR_WORKSPACE;
+    const CrossShape c = shape_of(*desc, *batch);
+    const bool bf16 = desc->dtype == MMTRAIN_BF16;
+    const CrossBwdPlan plan = bf16 ? cross_mfma_bwd_plan(c, g.d_k != nullptr) : CrossBwdPlan{};
+    if (!workspace || workspace_bytes < (bf16 ? cross_mfma_bwd_bytes(c, plan) : (size_t)a.Tq * a.nh * sizeof(float)) + 256) return MMTRAIN_ERR_WORKSPACE;
     a.d_o = g.d_o; a.lddo = g.ld_do;
     a.dq = g.d_q; a.lddq = g.ld_dq; a.dk = g.d_k; a.lddk = g.ld_dk; a.dv = g.d_v; a.lddv = g.ld_dv;
     a.D = (float *)workspace;
-    HIP_TRY(cross_bwd(desc->dtype, a, (hipStream_t)hip_stream));
+    hipStream_t st = (hipStream_t)hip_stream;
+    HIP_TRY(bf16 ? cross_mfma_bwd(a, plan, workspace, st) : cross_bwd(desc->dtype, a, st));
     return MMTRAIN_OK;
 }
 

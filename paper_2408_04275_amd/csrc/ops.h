@@ -118,6 +118,11 @@ struct CrossArgs {
     const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
     int chunk;                      // keys of a workgroup with few rows; 0: all of its run's
     float *part; float2 *part_ml;   // partial results of the chunks
+    // cross_mfma_bwd.hip, dK and dV: see cross_plan_kernel
+    const int *nb, *ne, *first_step, *cuts, *first_tile;
+    const int4 *steps;
+    int parts;                      // workgroups that share the rows which see a tile of keys
+    float *dkv_part;                // [parts][Tk][2 nkv d], where there are several
 };
 // What a call is planned from: sizes, and the runs' host arrays
 struct CrossShape { int Tq, Tk, S, nh, nkv, d; const int *cu, *begin, *end; };
@@ -129,6 +134,16 @@ struct CrossPlan {
 CrossPlan cross_mfma_fwd_plan(const CrossShape &c);
 size_t cross_mfma_fwd_bytes(const CrossShape &c, const CrossPlan &p);
 hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, void *ws, hipStream_t st);
+// exclusive sums of the runs' items (tiles of rows times chunks of keys), [S + 1]
+void cross_item_table(const CrossArgs &a, int tile_rows, int chunk, int *out, hipStream_t st);
+struct CrossBwdPlan {
+    int rows, items;                // dQ: rows of a workgroup, workgroups per key/value head
+    bool table, dkv;
+    int tiles, steps, parts;        // dK and dV: tiles of keys, tiles of rows of all runs, workgroups per tile of keys
+};
+CrossBwdPlan cross_mfma_bwd_plan(const CrossShape &c, bool dkv);
+size_t cross_mfma_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p);
+hipError_t cross_mfma_bwd(const CrossArgs &a, const CrossBwdPlan &p, void *ws, hipStream_t st);
 hipError_t cross_fwd(int dtype, const CrossArgs &a, hipStream_t st);
 hipError_t cross_bwd(int dtype, const CrossArgs &a, hipStream_t st);
 

@@ -29,10 +29,16 @@ HALF = {mm.BF16: 2.0 ** -8, mm.F32: 2.0 ** -24}
 NORMS = {"rms": mm.NORM_RMS, "layer": mm.NORM_LAYER}
 
 
+# A probability below fp32's (and bf16's) smallest normal number, 2^-126, may come out as zero.  It is then off by less than 2^-126, and a result by
+# that times what it multiplies: in the cases here |dP - D| < 2^9 (64 to 128 terms of at most 4 x 4, twice) times softmax_scale |q| or |k| < 2^7 at
+# most, for each of the result's fewer than k terms.
+UNDERFLOW = 2.0 ** -126 * 2.0 ** 16
+
+
 def near(name, got, ref, mag, k, stored, dtype, out_dtype=None):
     """Every element by its own bound, and the whole by its norm."""
     bf16 = dtype == mm.BF16
-    close(name, got, ref, mag, k, dtype if out_dtype is None else out_dtype, (HALF[mm.BF16] * 1.01 * stored if bf16 else 0.0))
+    close(name, got, ref, mag, k, dtype if out_dtype is None else out_dtype, (HALF[mm.BF16] * 1.01 * stored if bf16 else 0.0) + k * UNDERFLOW)
     got = host(got).reshape(np.shape(ref))
     norm = np.linalg.norm(ref)
     if bf16 and norm > 0:

@@ -2,12 +2,15 @@
 import os
 import subprocess
 
+import pytest
+
 from paper_2408_04275_amd.build import CSRC, FLAGS, HIPCC
 from test_lds_waits import early_uses, functions
 
 
-def test_no_register_is_touched_while_a_read_fills_it():
-    r = subprocess.run([HIPCC, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, "cross_mfma.hip"), "-o", "-"], capture_output=True, text=True)
+@pytest.mark.parametrize("source", ["cross_mfma.hip", "cross_mfma_bwd.hip"])
+def test_no_register_is_touched_while_a_read_fills_it(source):
+    r = subprocess.run([HIPCC, *FLAGS, "-S", "--cuda-device-only", os.path.join(CSRC, source), "-o", "-"], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     reads = 0
     for name, body in functions(r.stdout):
