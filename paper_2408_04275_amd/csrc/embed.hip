@@ -1,14 +1,19 @@
 // Embedding of a pack, and its gradient by sorted tokens.
+//
+// Forward moves each row once.  Backward sorts the tokens by the row that they name, equal ones in their order in the pack, and adds up
+// neighbours: a workgroup has a chunk of the order, writes the rows whose tokens it has all of, and leaves partial sums of the (at most two) that
+// reach into other chunks for the next launch.  Rows that nobody names are cleared beside it, found absent by a search in the order.
 #include "ops.h"
 #include "vec8.h"
+#include <algorithm>
 
 namespace mmt {
 namespace {
 
-// where a token's row comes from: row of the table, vocab + row of features, or -1
+// where a token's row comes from: row of the table, vocab + row of features, or vocab + features for none
 __device__ __forceinline__ int source_of(const EmbedArgs &a, int id) {
-    if (id >= 0) return id < a.vocab ? id : -1;
-    return id >= -a.features ? a.vocab - 1 - id : -1;
+    if (id >= 0) return id < a.vocab ? id : a.vocab + a.features;
+    return id >= -a.features ? a.vocab - 1 - id : a.vocab + a.features;
 }
 
 template <typename T>
@@ -18,7 +23,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
     if (i >= (long)a.T * chunks) return;
     const int t = (int)(i / chunks), c = (int)(i % chunks), src = source_of(a, a.ids[t]);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (src >= 0) {
+    if (src < a.vocab + a.features) {
         const bool text = src < a.vocab;
         load8((text ? (const T *)a.table + (long)src * a.H : (const T *)a.rows + (long)(src - a.vocab) * a.H) + 8 * c, v);
         if (text) {
@@ -29,43 +34,330 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
     store8((T *)a.y + (long)t * a.H + 8 * c, v);
 }
 
-// place of each token in the order by (row, token), by counting the tokens in front of it
+// ---- the order --------------------------------------------------------------------------------------------------------------
+// Short packs: each token's place is the number of tokens in front of it, counted: 32 tokens a workgroup, whose wavefronts compare 64 others at a
+// time and count the answers with one scalar instruction.  One launch, T^2 / 64 comparisons.
+constexpr int RANK_TOKENS = 32;
 __global__ __launch_bounds__(256) void embed_rank_kernel(EmbedArgs a, int *order, int *key) {
-    const int t = blockIdx.x * 256 + threadIdx.x;
-    const int mine = t < a.T ? source_of(a, a.ids[t]) : 0;
-    int rank = 0;
-    for (int u = 0; u < a.T; ++u) {
-        const int other = source_of(a, a.ids[u]);
-        rank += other < mine || (other == mine && u < t);
+    __shared__ int counts[4][RANK_TOKENS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = blockIdx.x * RANK_TOKENS, none = a.vocab + a.features;
+    const int mine = t0 + (lane & 31) < a.T ? source_of(a, a.ids[t0 + (lane & 31)]) : none;
+    int key_of[RANK_TOKENS], count[RANK_TOKENS];
+#pragma unroll
+    for (int i = 0; i < RANK_TOKENS; ++i) {
+        key_of[i] = __builtin_amdgcn_readlane(mine, i);
+        count[i] = 0;
     }
-    if (t < a.T) { order[rank] = t; key[rank] = mine; }
+    for (int u0 = 64 * wave; u0 < a.T; u0 += 256) {
+        const int u = u0 + lane;
+        const int other = u < a.T ? source_of(a, a.ids[u]) : none + 1;       // behind all
+        if (u0 + 64 <= t0) {
+#pragma unroll
+            for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(other <= key_of[i]));
+        } else if (u0 >= t0 + RANK_TOKENS) {
+#pragma unroll
+            for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(other < key_of[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < RANK_TOKENS; ++i)
+                count[i] += __popcll(__builtin_amdgcn_ballot_w64(other < key_of[i] || (other == key_of[i] && u < t0 + i)));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RANK_TOKENS; ++i)
+        if (lane == 0) counts[wave][i] = count[i];
+    __syncthreads();
+    const int t = t0 + threadIdx.x;
+    if (threadIdx.x < RANK_TOKENS && t < a.T) {
+        const int at = counts[0][threadIdx.x] + counts[1][threadIdx.x] + counts[2][threadIdx.x] + counts[3][threadIdx.x];
+        order[at] = t;
+        key[at] = mine;
+    }
 }
 
-// a workgroup per place in the order: the first of its row's sums up the row
-template <typename T, typename G>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, const int *order, const int *key) {
-    const int i = blockIdx.x, row = key[i];
-    if (row < 0 || (i > 0 && key[i - 1] == row)) return;
-    const bool text = row < a.vocab;
-    if (text ? !a.d_table : !a.d_rows) return;
-    for (int c = threadIdx.x; c < a.H / 8; c += 256) {
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, v[8];
-        for (int j = i; j < a.T && key[j] == row; ++j) {
-            load8((const T *)a.dy + (long)order[j] * a.H + 8 * c, v);
+// Long packs: a radix sort from the lowest eight bits up.  A workgroup has 4096 entries, a wavefront 1024 of them in a row.
+constexpr int RADIX_BLOCK = 4096, RADIX_ROUNDS = 16;
+struct RadixPass {
+    const int *key_in, *order_in;   // null: the ids themselves
+    int *key_out, *order_out;
+    int *hist;                      // [256][blocks]
+    int blocks, shift;
+};
+__device__ __forceinline__ int radix_key(const EmbedArgs &a, const RadixPass &p, int i) { return p.key_in ? p.key_in[i] : source_of(a, a.ids[i]); }
+// lanes of the wavefront whose digit is this lane's (of those that have one)
+__device__ __forceinline__ unsigned long long same_digit(int digit, bool live) {
+    unsigned long long m = __builtin_amdgcn_ballot_w64(live);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += v[e];
-        }
-        if (!text) { store8((T *)a.d_rows + (long)(row - a.vocab) * a.H + 8 * c, s); continue; }
-        G *out = (G *)a.d_table + (long)row * a.H + 8 * c;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] *= a.scale;
-        if (a.accumulate) {
-            load8(out, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += v[e];
-        }
-        store8(out, s);
+    for (int b = 0; b < 8; ++b) {
+        const bool bit = (digit >> b) & 1;
+        const unsigned long long on = __builtin_amdgcn_ballot_w64(bit);
+        m &= bit ? on : ~on;
     }
+    return m;
+}
+__global__ __launch_bounds__(256) void embed_radix_count_kernel(EmbedArgs a, RadixPass p) {
+    __shared__ int n[256];
+    n[threadIdx.x] = 0;
+    __syncthreads();
+    const long first = (long)blockIdx.x * RADIX_BLOCK;
+    for (int r = 0; r < RADIX_ROUNDS; ++r) {
+        const long i = first + r * 256 + threadIdx.x;
+        if (i < a.T) atomicAdd(&n[radix_key(a, p, (int)i) >> p.shift & 255], 1);
+    }
+    __syncthreads();
+    p.hist[(size_t)threadIdx.x * p.blocks + blockIdx.x] = n[threadIdx.x];
+}
+// exclusive sums of hist, in place: one workgroup
+__global__ __launch_bounds__(1024) void embed_radix_scan_kernel(RadixPass p) {
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long all = 256l * p.blocks;
+    int base = 0;
+    for (long i0 = 0; i0 < all; i0 += 4096) {
+        const long i = i0 + threadIdx.x * 4;
+        int v[4], n = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = i + e < all ? p.hist[i + e] : 0;
+            n += v[e];
+        }
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int u = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += u;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        int at = base + sum - n;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) at += sums[w];
+            base += sums[w];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e < all) p.hist[i + e] = at;
+            at += v[e];
+        }
+    }
+}
+__global__ __launch_bounds__(256) void embed_radix_move_kernel(EmbedArgs a, RadixPass p) {
+    __shared__ int place[4][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long first = (long)blockIdx.x * RADIX_BLOCK + wave * (64 * RADIX_ROUNDS);
+    volatile int *const mine = place[wave];
+    for (int d = lane; d < 256; d += 64) mine[d] = 0;
+    __builtin_amdgcn_wave_barrier();
+    int key[RADIX_ROUNDS];
+#pragma unroll
+    for (int r = 0; r < RADIX_ROUNDS; ++r) {
+        const long i = first + r * 64 + lane;
+        key[r] = i < a.T ? radix_key(a, p, (int)i) : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < RADIX_ROUNDS; ++r) {
+        const bool live = first + r * 64 + lane < a.T;
+        const int d = key[r] >> p.shift & 255;
+        const unsigned long long m = same_digit(d, live);
+        const bool leads = live && __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)) == 0;
+        if (leads) mine[d] = mine[d] + __popcll(m);
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    {
+        int at = p.hist[(size_t)threadIdx.x * p.blocks + blockIdx.x];
+        for (int w = 0; w < 4; ++w) {
+            const int n = place[w][threadIdx.x];
+            place[w][threadIdx.x] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RADIX_ROUNDS; ++r) {
+        const long i = first + r * 64 + lane;
+        const bool live = i < a.T;
+        const int d = key[r] >> p.shift & 255;
+        const unsigned long long m = same_digit(d, live);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+        const int start = mine[d];
+        __builtin_amdgcn_wave_barrier();
+        if (live && before == 0) mine[d] = start + __popcll(m);
+        __builtin_amdgcn_wave_barrier();
+        if (live) {
+            p.key_out[start + before] = key[r];
+            p.order_out[start + before] = p.order_in ? p.order_in[i] : (int)i;
+        }
+    }
+}
+
+// ---- the sums -------------------------------------------------------------------------------------------------------------------
+struct EmbedSums {
+    const int *order, *key;         // [T]
+    float *part;                    // [chunks][2][H]: sums of a chunk's first and last row, where those reach into other chunks
+    int chunk, chunks, fill_rows;   // tokens a chunk; rows that a clearing workgroup looks at
+    int columns;                    // columns a workgroup
+};
+
+template <typename T, typename G>
+__device__ __forceinline__ void add_old(const EmbedArgs &a, int row, int c, float (&old)[8]) {
+    if (row < a.vocab) load8((const G *)a.d_table + (long)row * a.H + c, old);
+}
+// a row's sum, complete; old: what the table holds, where it is added to
+template <typename T, typename G>
+__device__ __forceinline__ void put_row(const EmbedArgs &a, int row, int c, const float (&s)[8], const float (&old)[8]) {
+    float v[8];
+    if (row >= a.vocab) {
+        if (a.d_rows) store8((T *)a.d_rows + (long)(row - a.vocab) * a.H + c, s);
+        return;
+    }
+    if (!a.d_table) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = a.accumulate ? old[e] + s[e] * a.scale : s[e] * a.scale;
+    store8((G *)a.d_table + (long)row * a.H + c, v);
+}
+__device__ __forceinline__ bool is_named(const int *key, int n, int row) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (key[mid] < row) lo = mid + 1; else hi = mid;
+    }
+    return lo < n && key[lo] == row;
+}
+
+// Workgroups of the first chunks * (H / columns) have a chunk and some columns each, eight tokens' rows (and the old contents of the rows that
+// end among them) on their way at a time; the others clear rows.
+constexpr int SUM_ROWS = 8;
+template <typename T, typename G>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s) {
+    const int slabs = (a.H + s.columns - 1) / s.columns, none = a.vocab + a.features;
+    const int chunk = blockIdx.x / slabs;
+    if (chunk >= s.chunks) {
+        __shared__ int clear[64];
+        const int first = (a.accumulate || !a.d_table ? a.vocab : 0) + (blockIdx.x - s.chunks * slabs) * s.fill_rows;
+        const int rows = min(s.fill_rows, (a.d_rows ? none : a.vocab) - first);
+        if ((int)threadIdx.x < rows) clear[threadIdx.x] = !is_named(s.key, a.T, first + threadIdx.x);
+        __syncthreads();
+        const u32x4 zero = {0u, 0u, 0u, 0u};
+        for (int r = 0; r < rows; ++r) {
+            if (!clear[r]) continue;
+            const int row = first + r;
+            const bool text = row < a.vocab;
+            u32x4 *out = text ? (u32x4 *)((G *)a.d_table + (long)row * a.H) : (u32x4 *)((T *)a.d_rows + (long)(row - a.vocab) * a.H);
+            for (int i = threadIdx.x; i < a.H * (int)(text ? sizeof(G) : sizeof(T)) / 16; i += blockDim.x) __builtin_nontemporal_store(zero, out + i);
+        }
+        return;
+    }
+    const int c = (blockIdx.x % slabs) * s.columns + threadIdx.x * 8;
+    if (c >= a.H || (int)threadIdx.x * 8 >= s.columns) return;
+    const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, a.T);
+    const int before = p0 > 0 ? s.key[p0 - 1] : -1;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bool whole = s.key[p0] != before;                  // the present row's first token is in this chunk
+    for (int p = p0; p < p1; p += SUM_ROWS) {
+        int row[SUM_ROWS + 1];
+        Raw8<T> x[SUM_ROWS];
+        float old[SUM_ROWS][8];
+#pragma unroll
+        for (int i = 0; i <= SUM_ROWS; ++i) row[i] = p + i < a.T ? s.key[p + i] : -1;
+#pragma unroll
+        for (int i = 0; i < SUM_ROWS; ++i)
+            if (p + i < p1 && row[i] != none) x[i] = load_plain8((const T *)a.dy + (long)s.order[p + i] * a.H + c);
+        if (a.accumulate && a.d_table) {
+#pragma unroll
+            for (int i = 0; i < SUM_ROWS; ++i)
+                if (p + i < p1 && row[i] != row[i + 1] && row[i] != none) add_old<T, G>(a, row[i], c, old[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < SUM_ROWS; ++i) {
+            if (p + i >= p1 || row[i] == none) continue;
+            float v[8];
+            unpack8(x[i], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            const bool ends = row[i] != row[i + 1], last = p + i + 1 == p1;
+            if (ends && whole) put_row<T, G>(a, row[i], c, sum, old[i]);
+            else if (ends || last) store8(s.part + ((size_t)chunk * 2 + (whole ? 1 : 0)) * a.H + c, sum);
+            if (ends) {
+                whole = true;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+            }
+        }
+    }
+}
+
+// Rows whose tokens stand in several chunks: the workgroup of the chunk that a row begins in adds up the chunks' sums, four threads of one
+// column eight at a time
+template <typename T, typename G>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedSums s) {
+    __shared__ float red[3][64][9];
+    const int slabs = (a.H + 511) / 512, chunk = blockIdx.x / slabs;
+    const int last = min((chunk + 1) * s.chunk, a.T) - 1, row = s.key[last];
+    if (last + 1 >= a.T || row == a.vocab + a.features || s.key[last + 1] != row) return;          // ends here
+    if (chunk > 0 && s.key[chunk * s.chunk - 1] == row) return;                                     // began earlier
+    int lo = last + 1, hi = a.T;                       // the row's end in the order
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (s.key[mid] == row) lo = mid + 1; else hi = mid;
+    }
+    const int n = (lo - 1) / s.chunk - chunk;          // chunks behind this one
+    const int c = (blockIdx.x % slabs) * 512 + (threadIdx.x & 63) * 8, q = threadIdx.x >> 6;
+    const bool live = c < a.H;
+    const size_t stride = (size_t)2 * a.H;
+    const float *part = s.part + (size_t)(chunk + 1) * stride + c;       // their first rows
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, old[8];
+    if (live) {
+        if (q == 0) {
+            load8(s.part + (size_t)chunk * stride + a.H + c, sum);
+            if (a.accumulate && a.d_table) add_old<T, G>(a, row, c, old);
+        }
+        int j = q;
+        for (; j + 12 < n; j += 16) {
+            float v[4][8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load8(part + (size_t)(j + 4 * i) * stride, v[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[i][e];
+        }
+        for (; j < n; j += 4) {
+            float v[8];
+            load8(part + (size_t)j * stride, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+        }
+    }
+    if (q > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) red[q - 1][threadIdx.x & 63][e] = sum[e];
+    }
+    __syncthreads();
+    if (q > 0 || !live) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += red[w][threadIdx.x][e];
+    put_row<T, G>(a, row, c, sum, old);
+}
+
+// ---- sizes ---------------------------------------------------------------------------------------------------------------------------
+constexpr int RANK_MAX = 32768;                        // the longest pack that is ordered by counting
+// tokens a chunk: as few as keep their number within 2048
+int chunk_of(int T) { return std::max(16, (T / 2048 + 8) / 8 * 8); }
+size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
+int radix_blocks(int T) { return ceil_div(T, RADIX_BLOCK); }
+
+template <typename T, typename G>
+hipError_t sums(const EmbedArgs &a, const EmbedSums &s, hipStream_t st) {
+    const int threads = std::min(256, (a.H / 8 + 63) / 64 * 64), slabs = ceil_div(a.H, s.columns);
+    const int first = a.accumulate || !a.d_table ? a.vocab : 0, rows = (a.d_rows ? a.vocab + a.features : a.vocab) - first;
+    const int blocks = s.chunks * slabs + ceil_div(rows, s.fill_rows);
+    if (blocks) embed_sum_kernel<T, G><<<blocks, threads, 0, st>>>(a, s);
+    if (s.chunks > 1) embed_join_kernel<T, G><<<s.chunks * ceil_div(a.H, 512), 256, 0, st>>>(a, s);
+    return blocks ? hipGetLastError() : hipSuccess;
 }
 
 }  // namespace
@@ -78,20 +370,47 @@ hipError_t embed_fwd(int dtype, const EmbedArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-size_t embed_bwd_bytes(int T, int H) { return (size_t)T * 2 * sizeof(int) + 256; }
+// [key] [order] [partial sums], and for long packs [key] [order] [counts] of the sort
+size_t embed_bwd_bytes(int T, int H) {
+    size_t most = 0;
+    // (a longer pack has fewer chunks where theirs become longer: the most of any up to T)
+    auto parts = [&](int t) { return (size_t)ceil_div(t, chunk_of(t)) * 2 * H * sizeof(float); };
+    most = std::max(parts(T), T >= 2048 * 16 ? (size_t)2050 * 2 * H * sizeof(float) : 0);
+    return 2 * aligned((size_t)T * sizeof(int)) + aligned(most) +
+           (T > RANK_MAX ? 2 * aligned((size_t)T * sizeof(int)) + aligned(256ul * radix_blocks(T) * sizeof(int)) : 0) + 256;
+}
 
 hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st) {
-    hipError_t e = hipSuccess;
-    const int table_dtype = a.table_f32 ? DT_F32 : dtype;
-    if (a.d_table && !a.accumulate) e = fill_zero(a.d_table, (size_t)a.vocab * a.H, table_dtype, st);
-    if (e == hipSuccess && a.d_rows) e = fill_zero(a.d_rows, (size_t)a.features * a.H, dtype, st);
-    if (e != hipSuccess || a.T == 0) return e;
-    int *order = (int *)a.ws, *key = order + a.T;
-    embed_rank_kernel<<<ceil_div(a.T, 256), 256, 0, st>>>(a, order, key);
-    if (dtype == DT_F32) embed_sum_kernel<float, float><<<a.T, 256, 0, st>>>(a, order, key);
-    else if (a.table_f32) embed_sum_kernel<bf16_t, float><<<a.T, 256, 0, st>>>(a, order, key);
-    else embed_sum_kernel<bf16_t, bf16_t><<<a.T, 256, 0, st>>>(a, order, key);
-    return hipGetLastError();
+    EmbedSums s = {};
+    uint8_t *at = (uint8_t *)a.ws;
+    auto take = [&](size_t n) { void *p = at; at += aligned(n); return p; };
+    int *key = (int *)take((size_t)a.T * sizeof(int)), *order = (int *)take((size_t)a.T * sizeof(int));
+    if (a.T > RANK_MAX) {
+        int *key2 = (int *)take((size_t)a.T * sizeof(int)), *order2 = (int *)take((size_t)a.T * sizeof(int));
+        RadixPass p = {};
+        p.blocks = radix_blocks(a.T);
+        p.hist = (int *)take(256ul * p.blocks * sizeof(int));
+        int bits = 1;
+        while ((a.vocab + a.features) >> bits) ++bits;
+        const int passes = (bits + 7) / 8;
+        for (int i = 0; i < passes; ++i) {
+            const bool to_first = (passes - i) % 2;    // the last pass writes key and order
+            p.key_out = to_first ? key : key2; p.order_out = to_first ? order : order2;
+            p.shift = 8 * i;
+            embed_radix_count_kernel<<<p.blocks, 256, 0, st>>>(a, p);
+            embed_radix_scan_kernel<<<1, 1024, 0, st>>>(p);
+            embed_radix_move_kernel<<<p.blocks, 256, 0, st>>>(a, p);
+            p.key_in = p.key_out; p.order_in = p.order_out;
+        }
+    } else if (a.T > 0) embed_rank_kernel<<<ceil_div(a.T, RANK_TOKENS), 256, 0, st>>>(a, order, key);
+    s.key = key; s.order = order;
+    s.chunk = chunk_of(a.T);
+    s.chunks = ceil_div(a.T, s.chunk);
+    s.part = (float *)at;
+    s.fill_rows = 16;
+    s.columns = std::min(2048, (a.H / 8 + 63) / 64 * 64 * 8);
+    if (dtype == DT_F32) return sums<float, float>(a, s, st);
+    return a.table_f32 ? sums<bf16_t, float>(a, s, st) : sums<bf16_t, bf16_t>(a, s, st);
 }
 
 }  // namespace mmt
