@@ -39,7 +39,7 @@ int check_cross_batch(const mmtrain_cross_batch *b, bool ordered) {
 // rows of a run and key/value head, log-sum-exps of a group: 32-bit numbers and byte offsets
 int check_sizes(const mmtrain_cross_attn_desc &d, const mmtrain_cross_batch &b) {
     return (int64_t)b.q_tokens * (d.n_heads / d.n_kv_heads) > 1 << 28 || ((int64_t)b.q_tokens + b.n_segments) * d.n_heads > INT32_MAX ||
-           ((int64_t)b.kv_tokens / 16 + b.n_segments) * d.n_kv_heads > INT32_MAX ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
+           ((int64_t)b.kv_tokens / 16 + 16 * ((int64_t)b.n_segments + 1)) * d.n_kv_heads > INT32_MAX ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
 }
 
 int check_rows(const mmtrain_cross_attn_desc &d, int heads, const void *p, int64_t ld) {
@@ -77,11 +77,7 @@ extern "C" {
 size_t mmtrain_cross_attn_workspace_bytes(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, int is_bwd) {
     if (check_cross(desc) || check_cross_batch(batch, false) || check_sizes(*desc, *batch)) return 0;
     const CrossShape c = shape_of(*desc, *batch);
-    if (is_bwd) {
-        if (desc->dtype == MMTRAIN_F32) return (size_t)batch->q_tokens * desc->n_heads * sizeof(float) + 256;
-        return cross_mfma_bwd_bytes(c, cross_mfma_bwd_plan(c, check_cross_batch(batch, true) == MMTRAIN_OK)) + 256;
-    }
-    return (desc->dtype == MMTRAIN_BF16 ? cross_mfma_fwd_bytes(c, cross_mfma_fwd_plan(c)) : 0) + 256;
+    return (is_bwd ? cross_bwd_bytes(c, cross_bwd_plan(desc->dtype, c, check_cross_batch(batch, true) == MMTRAIN_OK)) : cross_fwd_bytes(c, cross_fwd_plan(desc->dtype, c))) + 256;
 }
 
 int mmtrain_cross_attn_fwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cross_batch *batch, const mmtrain_cross_attn_tensors *tensors,
@@ -94,12 +90,10 @@ int mmtrain_cross_attn_fwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
     if (a.Tq == 0) return MMTRAIN_OK;
     if (a.o == a.q || a.o == a.k || a.o == a.v) return MMTRAIN_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
-    hipStream_t st = (hipStream_t)hip_stream;
     const CrossShape c = shape_of(*desc, *batch);
-    const bool bf16 = desc->dtype == MMTRAIN_BF16;
-    const CrossPlan plan = bf16 ? cross_mfma_fwd_plan(c) : CrossPlan{};
-    if (!workspace || workspace_bytes < (bf16 ? cross_mfma_fwd_bytes(c, plan) : 0) + 256) return MMTRAIN_ERR_WORKSPACE;
-    HIP_TRY(bf16 ? cross_mfma_fwd(a, plan, workspace, st) : cross_fwd(desc->dtype, a, st));
+    const CrossPlan plan = cross_fwd_plan(desc->dtype, c);
+    if (!workspace || workspace_bytes < cross_fwd_bytes(c, plan) + 256) return MMTRAIN_ERR_WORKSPACE;
+    HIP_TRY(cross_fwd(desc->dtype, a, plan, workspace, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 
@@ -124,14 +118,11 @@ int mmtrain_cross_attn_bwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
     }
     if ((uintptr_t)workspace & 255) return MMTRAIN_ERR_INVALID_ARG;
     const CrossShape c = shape_of(*desc, *batch);
-    const bool bf16 = desc->dtype == MMTRAIN_BF16;
-    const CrossBwdPlan plan = bf16 ? cross_mfma_bwd_plan(c, g.d_k != nullptr) : CrossBwdPlan{};
-    if (!workspace || workspace_bytes < (bf16 ? cross_mfma_bwd_bytes(c, plan) : (size_t)a.Tq * a.nh * sizeof(float)) + 256) return MMTRAIN_ERR_WORKSPACE;
+    const CrossBwdPlan plan = cross_bwd_plan(desc->dtype, c, g.d_k != nullptr);
+    if (!workspace || workspace_bytes < cross_bwd_bytes(c, plan) + 256) return MMTRAIN_ERR_WORKSPACE;
     a.d_o = g.d_o; a.lddo = g.ld_do;
     a.dq = g.d_q; a.lddq = g.ld_dq; a.dk = g.d_k; a.lddk = g.ld_dk; a.dv = g.d_v; a.lddv = g.ld_dv;
-    a.D = (float *)workspace;
-    hipStream_t st = (hipStream_t)hip_stream;
-    HIP_TRY(bf16 ? cross_mfma_bwd(a, plan, workspace, st) : cross_bwd(desc->dtype, a, st));
+    HIP_TRY(cross_bwd(desc->dtype, a, plan, workspace, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 

@@ -13,34 +13,6 @@ namespace mmt {
 
 namespace {
 
-// exclusive sums of the runs' items, [S + 1]: one workgroup
-__global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int tile_rows, int chunk, int *out) {
-    __shared__ int sums[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int base = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 1024) {
-        const int s = s0 + threadIdx.x;
-        const int n = s < a.S ? items_of(a.cu[s + 1] - a.cu[s], a.end[s] - a.begin[s], a.nh / a.nkv, tile_rows, chunk) : 0;
-        int sum = n;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const int v = __shfl_up(sum, o, 64);
-            if (lane >= o) sum += v;
-        }
-        __syncthreads();
-        if (lane == 63) sums[wave] = sum;
-        __syncthreads();
-        int before = base, all = base;
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) before += sums[w];
-            all += sums[w];
-        }
-        if (s < a.S) out[s] = before + sum - n;
-        base = all;
-    }
-    if (threadIdx.x == 0) out[a.S] = base;
-}
-
 // ---- forward, many rows ------------------------------------------------------------------------------------------------
 // WAVES wavefronts x 32 rows, keys 64 at a time through two LDS slots.  Each wavefront works one block of 32 keys ahead, as
 // attn_mfma.hip's forward kernel does: the next block's scores are multiplied between the exponentials of the current one, and a
@@ -217,7 +189,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
 // Up to 32 rows per workgroup, whose four wavefronts share out the blocks of 32 keys, each with two LDS slots of its own and no barrier on
 // the way: the next block is in flight while this one is multiplied.  Where that leaves the chip empty or one workgroup with a long walk, the keys
 // are cut into chunks, one per workgroup, whose partial results (32 rows of fp32, maximum and sum) cross_combine_kernel joins.
-constexpr int FEW_ROWS = 32;
 template <int D> constexpr int FEW_LDS = 4 * 4 * ROWS32<D>;
 
 template <int D, int KS, int CB>
@@ -440,57 +411,7 @@ hipError_t launch_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st) {
 
 }  // namespace
 
-void cross_item_table(const CrossArgs &a, int tile_rows, int chunk, int *out, hipStream_t st) { cross_prefix_kernel<<<1, 1024, 0, st>>>(a, tile_rows, chunk, out); }
-
-// How a forward pass is cut: by the rows of the runs and the keys they see
-CrossPlan cross_mfma_fwd_plan(const CrossShape &c) {
-    const int group = c.nh / c.nkv;
-    auto count = [&](int rows, int chunk) {
-        long n = 0;
-        for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], group, rows, chunk);
-        return n;
-    };
-    // steps of 32 rows and 32 keys
-    long few = 0, many = 0, longest = 0;
-    for (int s = 0; s < c.S; ++s) {
-        const long keys = (c.end[s] - c.begin[s] + 31) / 32, rows = (long)(c.cu[s + 1] - c.cu[s]) * group;
-        few += (rows + 31) / 32 * keys;
-        many += (rows + 127) / 128 * 4 * keys;
-        longest = std::max(longest, keys);
-    }
-    CrossPlan p = {};
-    if (many > 2 * few || count(128, 0) * c.nkv < 128) {
-        p.rows = FEW_ROWS;
-        const long whole = count(FEW_ROWS, 0) * c.nkv;
-        if (whole < 512 && longest > 32) {
-            const long want = std::max(few * c.nkv / 1024, 8l);      // blocks a workgroup
-            p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
-            if (p.chunk >= longest * 32) p.chunk = 0;
-        }
-    } else p.rows = c.d > 64 ? 256 : 128;
-    p.items = (int)count(p.rows, p.chunk);
-    p.table = c.S > 64;
-    return p;
-}
-
-size_t cross_mfma_fwd_bytes(const CrossShape &c, const CrossPlan &p) {
-    return (p.table ? table_bytes(c.S) : 0) +
-           (p.chunk ? (size_t)p.items * c.nkv * FEW_ROWS * (c.d * sizeof(float) + sizeof(float2)) : 0);
-}
-
-hipError_t cross_mfma_fwd(const CrossArgs &args, const CrossPlan &p, void *ws, hipStream_t st) {
-    CrossArgs a = args;
-    uint8_t *at = (uint8_t *)ws;
-    if (p.table) {
-        a.prefix = (int *)at;
-        cross_item_table(a, p.rows, p.chunk, (int *)at, st);
-        at += table_bytes(a.S);
-    }
-    a.chunk = p.chunk;
-    if (p.chunk) {
-        a.part = (float *)at;
-        a.part_ml = (float2 *)(a.part + (size_t)p.items * a.nkv * FEW_ROWS * a.d);
-    }
+hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st) {
     return a.d <= 64 ? launch_fwd<64, 4, 2>(a, p, st) : a.d <= 80 ? launch_fwd<128, 5, 3>(a, p, st) : a.d <= 96 ? launch_fwd<128, 6, 3>(a, p, st)
                                                                                                           : launch_fwd<128, 8, 4>(a, p, st);
 }

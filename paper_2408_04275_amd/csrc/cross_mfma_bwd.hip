@@ -10,8 +10,6 @@ namespace mmt {
 
 namespace {
 
-constexpr int STEP_ROWS = 64, TILE_KEYS = 128;
-
 // A wavefront's share of 64 rows on their way into LDS: copies first .. first + N - 1 of 1 KiB each
 template <int D, int N>
 __device__ __forceinline__ void copy_rows_part(const bf16_t *p, long ld, int dh, const Rows &at, const Group &g, uint8_t *tile, int first) {
@@ -156,106 +154,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_dq_kernel(CrossArgs a) {
     store_rows_at<D, CB>(smem + wave * STAGE<D>, dq, a.scale, (bf16_t *)a.dq + col, a.lddq, dh, mine, g);
 }
 
-// ---- dK, dV: what is walked ---------------------------------------------------------------------------------------------------
-// One workgroup.  Where the runs that see something begin and end, non-decreasing, is completed over the others (nb, ne: a run that sees nothing gets
-// the last one's); all those places together, sorted, cut the keys into pieces (cuts, [2 S + 2]); first_tile [2 S + 2]: tiles of
-// 128 keys in front of each piece; first_step [S + 1]: steps of 64 rows in front of each run; steps: {token, head of the group, rows} of each.
-__device__ __forceinline__ int block_scan(int v, bool max, int *sums) {      // inclusive, of 1024 threads
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int u = __shfl_up(v, o, 64);
-        if (lane >= o) v = max ? ::max(v, u) : v + u;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = v;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) v = max ? ::max(v, sums[w]) : v + sums[w];
-    return v;
-}
-__device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool upper) {     // entries below v, or up to it
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (x[mid] < v || (upper && x[mid] == v)) lo = mid + 1; else hi = mid;
-    }
-    return lo;
-}
-__global__ __launch_bounds__(1024) void cross_plan_kernel(CrossArgs a, int *nb, int *ne, int *first_step, int *cuts, int *first_tile, int4 *steps) {
-    __shared__ int sums[16], carry[3];
-    const int group = a.nh / a.nkv, S = a.S;
-    if (threadIdx.x < 3) carry[threadIdx.x] = 0;
-    __syncthreads();
-    for (int s0 = 0; s0 < S; s0 += 1024) {
-        const int s = s0 + threadIdx.x;
-        int b = 0, e = 0, n = 0;
-        if (s < S && a.begin[s] < a.end[s]) {
-            b = a.begin[s]; e = a.end[s];
-            n = ((a.cu[s + 1] - a.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
-        }
-        b = max(block_scan(b, true, sums), carry[0]);
-        e = max(block_scan(e, true, sums), carry[1]);
-        const int sum = block_scan(n, false, sums) + carry[2];
-        if (s < S) { nb[s] = b; ne[s] = e; first_step[s] = sum - n; }
-        __syncthreads();
-        if (threadIdx.x == 1023) { carry[0] = b; carry[1] = e; carry[2] = sum; }
-        __syncthreads();
-    }
-    const int all = carry[2];
-    if (threadIdx.x == 0) { first_step[S] = all; cuts[0] = 0; cuts[2 * S + 1] = a.Tk; carry[0] = 0; }
-    __threadfence_block();
-    __syncthreads();
-    for (int s = threadIdx.x; s < S; s += 1024) {
-        cuts[1 + s + lower_bound(ne, S, nb[s], false)] = nb[s];
-        cuts[1 + s + lower_bound(nb, S, ne[s], true)] = ne[s];
-    }
-    __threadfence_block();
-    __syncthreads();
-    for (int p0 = 0; p0 < 2 * S + 1; p0 += 1024) {
-        const int p = p0 + threadIdx.x, n = p < 2 * S + 1 ? (cuts[p + 1] - cuts[p] + TILE_KEYS - 1) / TILE_KEYS : 0;
-        const int sum = block_scan(n, false, sums) + carry[0];
-        if (p < 2 * S + 1) first_tile[p] = sum - n;
-        if (p == 2 * S) first_tile[2 * S + 1] = sum;
-        __syncthreads();
-        if (threadIdx.x == 1023) carry[0] = sum;
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < all; i += 1024) {
-        const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group;
-        steps[i] = make_int4(a.cu[s] + tok, row - tok * group, min((a.cu[s + 1] - a.cu[s]) * group - row, STEP_ROWS), 0);
-    }
-}
-
-struct KeyTile {
-    int key, end;               // keys
-    int step, steps;            // first step, how many
-};
-__device__ __forceinline__ KeyTile find_tile(const CrossArgs &a, int y) {
-    KeyTile k;
-    const int p = find_segment(a.first_tile, 2 * a.S + 1, y), first = a.cuts[p];
-    k.key = first + (y - a.first_tile[p]) * TILE_KEYS;
-    k.end = a.cuts[p + 1];
-    int begin = 0, end = 0;                            // the runs that see the piece: behind the last that ends in front of it
-    if (a.S > 0) {
-        begin = a.first_step[lower_bound(a.ne, a.S, first, true)];
-        end = a.first_step[lower_bound(a.nb, a.S, first, true)];
-    }
-    const long n = max(end - begin, 0);
-    k.step = begin + (int)(n * blockIdx.y / a.parts);
-    k.steps = begin + (int)(n * (blockIdx.y + 1) / a.parts) - k.step;
-    k.key = __builtin_amdgcn_readfirstlane(k.key);
-    k.end = __builtin_amdgcn_readfirstlane(k.end);
-    k.step = __builtin_amdgcn_readfirstlane(k.step);
-    k.steps = __builtin_amdgcn_readfirstlane(k.steps);
-    return k;
-}
-__device__ __forceinline__ Rows rows_of(const int4 &e) {
-    Rows r;
-    r.t = __builtin_amdgcn_readfirstlane(e.x);
-    r.j = __builtin_amdgcn_readfirstlane(e.y);
-    r.left = __builtin_amdgcn_readfirstlane(e.z);
-    return r;
-}
 // 64 values of a [heads, Tq] array, those of a step's rows, into LDS
 __device__ __forceinline__ void copy_stats(const float *x, const CrossArgs &a, int head, const Rows &at, const Group &g, uint8_t *to) {
     const int lane = threadIdx.x & 63, tok = g.token(at.j + lane), h = at.j + lane - tok * g.n;
@@ -643,70 +541,9 @@ hipError_t launch_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st)
     return hipGetLastError();
 }
 
-size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
-size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
-
 }  // namespace
 
-CrossBwdPlan cross_mfma_bwd_plan(const CrossShape &c, bool dkv) {
-    const int group = c.nh / c.nkv;
-    CrossBwdPlan p = {};
-    p.rows = c.d > 64 ? 256 : 128;
-    for (int s = 0; s < c.S; ++s) p.items += items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
-    p.table = c.S > 64;
-    p.dkv = dkv;
-    p.parts = 1;
-    if (!dkv) return p;
-    // the pieces of the keys: beginnings and ends of the runs that see something, merged
-    long tiles = 0, steps = 0;
-    int at = 0;
-    auto cut = [&](int place) {
-        tiles += (place - at + TILE_KEYS - 1) / TILE_KEYS;
-        at = place;
-    };
-    int b = 0, e = 0;
-    auto next = [&](int s) { while (s < c.S && c.begin[s] == c.end[s]) ++s; return s; };
-    for (b = next(0), e = b; e < c.S;) {
-        if (b < c.S && c.begin[b] <= c.end[e]) { cut(c.begin[b]); b = next(b + 1); }
-        else { cut(c.end[e]); e = next(e + 1); }
-    }
-    cut(c.Tk);
-    for (int s = 0; s < c.S; ++s)
-        if (c.begin[s] < c.end[s]) steps += ((long)(c.cu[s + 1] - c.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
-    p.tiles = (int)tiles;
-    p.steps = (int)steps;
-    // Workgroups that share a tile's rows: until the chip has two rounds of workgroups, as long as each has a few steps
-    const long want = c.d > 64 ? 512 : 1024;
-    while (p.parts < 16 && (long)p.tiles * c.nkv * p.parts * 2 <= want && steps >= 8l * p.parts && part_bytes(c) * p.parts * 2 <= size_t(96) << 20) p.parts *= 2;
-    return p;
-}
-
-// [D] [table of items] [nb, ne, first_step, cuts, first_tile] [steps] [parts]
-size_t cross_mfma_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p) {
-    size_t n = aligned((size_t)c.Tq * c.nh * sizeof(float)) + (p.table ? table_bytes(c.S) : 0);
-    if (p.dkv) n += 3 * table_bytes(c.S) + 2 * table_bytes(2 * c.S + 1) + aligned((size_t)p.steps * sizeof(int4)) + (p.parts > 1 ? p.parts * part_bytes(c) : 0);
-    return n;
-}
-
-hipError_t cross_mfma_bwd(const CrossArgs &args, const CrossBwdPlan &p, void *ws, hipStream_t st) {
-    CrossArgs a = args;
-    uint8_t *at = (uint8_t *)ws;
-    auto take = [&](size_t n) { void *q = at; at += n; return q; };
-    a.D = (float *)take(aligned((size_t)a.Tq * a.nh * sizeof(float)));
-    a.parts = p.parts;
-    if (p.table) {
-        a.prefix = (int *)take(table_bytes(a.S));
-        if (p.items) cross_item_table(a, p.rows, 0, const_cast<int *>(a.prefix), st);
-    }
-    if (p.dkv && p.tiles) {
-        int *nb = (int *)take(table_bytes(a.S)), *ne = (int *)take(table_bytes(a.S)), *first_step = (int *)take(table_bytes(a.S));
-        int *cuts = (int *)take(table_bytes(2 * a.S + 1)), *first_tile = (int *)take(table_bytes(2 * a.S + 1));
-        int4 *steps = (int4 *)take(aligned((size_t)p.steps * sizeof(int4)));
-        a.nb = nb; a.ne = ne; a.first_step = first_step; a.cuts = cuts; a.first_tile = first_tile; a.steps = steps;
-        a.dkv_part = (float *)at;
-        cross_plan_kernel<<<1, 1024, 0, st>>>(a, nb, ne, first_step, cuts, first_tile, steps);
-    }
-    if (!p.items && !(p.dkv && p.tiles)) return hipSuccess;
+hipError_t cross_mfma_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st) {
     return a.d <= 64 ? launch_bwd<64, 4, 2>(a, p, st) : a.d <= 80 ? launch_bwd<128, 5, 3>(a, p, st) : a.d <= 96 ? launch_bwd<128, 6, 3>(a, p, st)
                                                                                                           : launch_bwd<128, 8, 4>(a, p, st);
 }

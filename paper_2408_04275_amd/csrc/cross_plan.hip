@@ -1,0 +1,217 @@
+// How calls of cross attention are cut into workgroups: the tables that the kernels look their work up in, and the plans that the host makes of
+// the runs (the same from the same arrays, so that the size of a workspace and a call agree).
+#include "cross_tiles.h"
+#include <algorithm>
+
+namespace mmt {
+
+namespace {
+
+// exclusive sums of the runs' items, [S + 1]: one workgroup
+__global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int tile_rows, int chunk, int *out) {
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 1024) {
+        const int s = s0 + threadIdx.x;
+        const int n = s < a.S ? items_of(a.cu[s + 1] - a.cu[s], a.end[s] - a.begin[s], a.nh / a.nkv, tile_rows, chunk) : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += v;
+        }
+        __syncthreads();
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        int before = base, all = base;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) before += sums[w];
+            all += sums[w];
+        }
+        if (s < a.S) out[s] = before + sum - n;
+        base = all;
+    }
+    if (threadIdx.x == 0) out[a.S] = base;
+}
+
+// ---- dK, dV: what is walked ---------------------------------------------------------------------------------------------------
+// One workgroup.  Where the runs that see something begin and end, non-decreasing, is completed over the others (nb, ne: a run that sees nothing gets
+// the last one's); all those places together, sorted, cut the keys into pieces (cuts, [2 S + 2]); first_tile [2 S + 2]: tiles of
+// 128 keys in front of each piece; first_step [S + 1]: steps of 64 rows in front of each run; steps: {token, head of the group, rows} of each.
+__device__ __forceinline__ int block_scan(int v, bool max, int *sums) {      // inclusive, of 1024 threads
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int u = __shfl_up(v, o, 64);
+        if (lane >= o) v = max ? ::max(v, u) : v + u;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v = max ? ::max(v, sums[w]) : v + sums[w];
+    return v;
+}
+__global__ __launch_bounds__(1024) void cross_plan_kernel(CrossArgs a, int *nb, int *ne, int *first_step, int *cuts, int *first_tile, int4 *steps) {
+    __shared__ int sums[16], carry[3];
+    const int group = a.nh / a.nkv, S = a.S;
+    if (threadIdx.x < 3) carry[threadIdx.x] = 0;
+    __syncthreads();
+    for (int s0 = 0; s0 < S; s0 += 1024) {
+        const int s = s0 + threadIdx.x;
+        int b = 0, e = 0, n = 0;
+        if (s < S && a.begin[s] < a.end[s]) {
+            b = a.begin[s]; e = a.end[s];
+            n = ((a.cu[s + 1] - a.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
+        }
+        b = max(block_scan(b, true, sums), carry[0]);
+        e = max(block_scan(e, true, sums), carry[1]);
+        const int sum = block_scan(n, false, sums) + carry[2];
+        if (s < S) { nb[s] = b; ne[s] = e; first_step[s] = sum - n; }
+        __syncthreads();
+        if (threadIdx.x == 1023) { carry[0] = b; carry[1] = e; carry[2] = sum; }
+        __syncthreads();
+    }
+    const int all = carry[2];
+    if (threadIdx.x == 0) { first_step[S] = all; cuts[0] = 0; cuts[2 * S + 1] = a.Tk; carry[0] = 0; }
+    __threadfence_block();
+    __syncthreads();
+    for (int s = threadIdx.x; s < S; s += 1024) {
+        cuts[1 + s + lower_bound(ne, S, nb[s], false)] = nb[s];
+        cuts[1 + s + lower_bound(nb, S, ne[s], true)] = ne[s];
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int p0 = 0; p0 < 2 * S + 1; p0 += 1024) {
+        const int p = p0 + threadIdx.x, n = p < 2 * S + 1 ? (cuts[p + 1] - cuts[p] + TILE_KEYS - 1) / TILE_KEYS : 0;
+        const int sum = block_scan(n, false, sums) + carry[0];
+        if (p < 2 * S + 1) first_tile[p] = sum - n;
+        if (p == 2 * S) first_tile[2 * S + 1] = sum;
+        __syncthreads();
+        if (threadIdx.x == 1023) carry[0] = sum;
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < all; i += 1024) {
+        const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group;
+        steps[i] = make_int4(a.cu[s] + tok, row - tok * group, min((a.cu[s + 1] - a.cu[s]) * group - row, STEP_ROWS), 0);
+    }
+}
+
+size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
+size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
+
+}  // namespace
+
+// How a forward pass is cut: by the rows of the runs and the keys they see
+CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
+    const int group = c.nh / c.nkv;
+    auto count = [&](int rows, int chunk) {
+        long n = 0;
+        for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], group, rows, chunk);
+        return n;
+    };
+    // steps of 32 rows and 32 keys
+    long few = 0, many = 0, longest = 0;
+    for (int s = 0; s < c.S; ++s) {
+        const long keys = (c.end[s] - c.begin[s] + 31) / 32, rows = (long)(c.cu[s + 1] - c.cu[s]) * group;
+        few += (rows + 31) / 32 * keys;
+        many += (rows + 127) / 128 * 4 * keys;
+        longest = std::max(longest, keys);
+    }
+    CrossPlan p = {};
+    p.rows = dtype == DT_F32 ? 16 : many > 2 * few || count(128, 0) * c.nkv < 128 ? FEW_ROWS : c.d > 64 ? 256 : 128;
+    if (p.rows <= FEW_ROWS && count(p.rows, 0) * c.nkv < 512 && longest > 32) {
+        const long want = std::max(few * c.nkv / 1024, 8l);      // blocks of 32 keys a workgroup
+        p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
+        if (p.chunk >= longest * 32) p.chunk = 0;
+    }
+    p.items = (int)count(p.rows, p.chunk);
+    p.table = c.S > 64;
+    return p;
+}
+
+// [table of items] [parts] [their maxima and sums]
+size_t cross_fwd_bytes(const CrossShape &c, const CrossPlan &p) {
+    return (p.table ? table_bytes(c.S) : 0) + (p.chunk ? (size_t)p.items * c.nkv * p.rows * (c.d * sizeof(float) + sizeof(float2)) : 0);
+}
+
+hipError_t cross_fwd(int dtype, const CrossArgs &args, const CrossPlan &p, void *ws, hipStream_t st) {
+    CrossArgs a = args;
+    uint8_t *at = (uint8_t *)ws;
+    if (p.table) {
+        a.prefix = (int *)at;
+        cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, p.chunk, (int *)at);
+        at += table_bytes(a.S);
+    }
+    a.chunk = p.chunk;
+    if (p.chunk) {
+        a.part = (float *)at;
+        a.part_ml = (float2 *)(a.part + (size_t)p.items * a.nkv * p.rows * a.d);
+    }
+    return dtype == DT_F32 ? cross_f32_fwd(a, p, st) : cross_mfma_fwd(a, p, st);
+}
+
+CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
+    const int group = c.nh / c.nkv;
+    CrossBwdPlan p = {};
+    p.rows = dtype == DT_F32 ? 16 : c.d > 64 ? 256 : 128;
+    for (int s = 0; s < c.S; ++s) p.items += items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
+    p.table = c.S > 64;
+    p.dkv = dkv;
+    p.parts = 1;
+    if (!dkv) return p;
+    // the pieces of the keys: beginnings and ends of the runs that see something, merged
+    long tiles = 0, steps = 0;
+    int at = 0;
+    auto cut = [&](int place) {
+        tiles += (place - at + TILE_KEYS - 1) / TILE_KEYS;
+        at = place;
+    };
+    int b = 0, e = 0;
+    auto next = [&](int s) { while (s < c.S && c.begin[s] == c.end[s]) ++s; return s; };
+    for (b = next(0), e = b; e < c.S;) {
+        if (b < c.S && c.begin[b] <= c.end[e]) { cut(c.begin[b]); b = next(b + 1); }
+        else { cut(c.end[e]); e = next(e + 1); }
+    }
+    cut(c.Tk);
+    for (int s = 0; s < c.S; ++s)
+        if (c.begin[s] < c.end[s]) steps += ((long)(c.cu[s + 1] - c.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
+    p.tiles = (int)tiles;
+    p.steps = (int)steps;
+    if (dtype == DT_F32) return p;                       // (a workgroup per 16 keys: enough of them)
+    // Workgroups that share a tile's rows: until the chip has two rounds of workgroups, as long as each has a few steps
+    const long want = c.d > 64 ? 512 : 1024;
+    while (p.parts < 16 && (long)p.tiles * c.nkv * p.parts * 2 <= want && steps >= 8l * p.parts && part_bytes(c) * p.parts * 2 <= size_t(96) << 20) p.parts *= 2;
+    return p;
+}
+
+// [D] [table of items] [nb, ne, first_step, cuts, first_tile] [steps] [parts]
+size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p) {
+    size_t n = aligned((size_t)c.Tq * c.nh * sizeof(float)) + (p.table ? table_bytes(c.S) : 0);
+    if (p.dkv) n += 3 * table_bytes(c.S) + 2 * table_bytes(2 * c.S + 1) + aligned((size_t)p.steps * sizeof(int4)) + (p.parts > 1 ? p.parts * part_bytes(c) : 0);
+    return n;
+}
+
+hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossBwdPlan &p, void *ws, hipStream_t st) {
+    CrossArgs a = args;
+    uint8_t *at = (uint8_t *)ws;
+    auto take = [&](size_t n) { void *q = at; at += n; return q; };
+    a.D = (float *)take(aligned((size_t)a.Tq * a.nh * sizeof(float)));
+    a.parts = p.parts;
+    if (p.table) {
+        a.prefix = (int *)take(table_bytes(a.S));
+        if (p.items) cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, 0, const_cast<int *>(a.prefix));
+    }
+    if (p.dkv && p.tiles) {
+        int *nb = (int *)take(table_bytes(a.S)), *ne = (int *)take(table_bytes(a.S)), *first_step = (int *)take(table_bytes(a.S));
+        int *cuts = (int *)take(table_bytes(2 * a.S + 1)), *first_tile = (int *)take(table_bytes(2 * a.S + 1));
+        int4 *steps = (int4 *)take(aligned((size_t)p.steps * sizeof(int4)));
+        a.nb = nb; a.ne = ne; a.first_step = first_step; a.cuts = cuts; a.first_tile = first_tile; a.steps = steps;
+        a.dkv_part = (float *)at;
+        cross_plan_kernel<<<1, 1024, 0, st>>>(a, nb, ne, first_step, cuts, first_tile, steps);
+    }
+    if (!p.items && !(p.dkv && p.tiles)) return hipSuccess;
+    return dtype == DT_F32 ? cross_f32_bwd(a, p, st) : cross_mfma_bwd(a, p, st);
+}
+
+}  // namespace mmt

@@ -8,7 +8,9 @@ namespace mmt {
 
 namespace {
 
-constexpr int KEYS = 64;                                // a step of the tile kernel
+constexpr int KEYS = 64;                                // a step of the kernels with many rows
+constexpr int FEW_ROWS = 32;                            // rows of a workgroup of the form for few
+constexpr int STEP_ROWS = 64, TILE_KEYS = 128;          // dK/dV: rows of a step, keys of a tile
 template <int D> constexpr int ROWS32 = 32 * D * 2;     // bytes of 32 rows in LDS
 template <int D> constexpr int STAGE = 32 * (2 * D + 16);
 
@@ -132,6 +134,44 @@ __device__ __forceinline__ void store_rows_at(uint8_t *stage, const f32x16 (&acc
 
 __device__ __forceinline__ float natural_lse(float m, float l, float sl2) { return (m * sl2 + __builtin_amdgcn_logf(l)) * LN2; }
 
+__device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool upper) {     // entries below v, or up to it
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (x[mid] < v || (upper && x[mid] == v)) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+struct KeyTile {
+    int key, end;               // keys
+    int step, steps;            // first step, how many
+};
+__device__ __forceinline__ KeyTile find_tile(const CrossArgs &a, int y) {
+    KeyTile k;
+    const int p = find_segment(a.first_tile, 2 * a.S + 1, y), first = a.cuts[p];
+    k.key = first + (y - a.first_tile[p]) * TILE_KEYS;
+    k.end = a.cuts[p + 1];
+    int begin = 0, end = 0;                            // the runs that see the piece: behind the last that ends in front of it
+    if (a.S > 0) {
+        begin = a.first_step[lower_bound(a.ne, a.S, first, true)];
+        end = a.first_step[lower_bound(a.nb, a.S, first, true)];
+    }
+    const long n = max(end - begin, 0);
+    k.step = begin + (int)(n * blockIdx.y / a.parts);
+    k.steps = begin + (int)(n * (blockIdx.y + 1) / a.parts) - k.step;
+    k.key = __builtin_amdgcn_readfirstlane(k.key);
+    k.end = __builtin_amdgcn_readfirstlane(k.end);
+    k.step = __builtin_amdgcn_readfirstlane(k.step);
+    k.steps = __builtin_amdgcn_readfirstlane(k.steps);
+    return k;
+}
+__device__ __forceinline__ Rows rows_of(const int4 &e) {
+    Rows r;
+    r.t = __builtin_amdgcn_readfirstlane(e.x);
+    r.j = __builtin_amdgcn_readfirstlane(e.y);
+    r.left = __builtin_amdgcn_readfirstlane(e.z);
+    return r;
+}
 template <typename K>
 hipError_t set_smem(std::atomic<bool> &done, K kern, int bytes) {
     if (done.load(std::memory_order_acquire)) return hipSuccess;

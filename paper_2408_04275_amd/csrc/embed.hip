@@ -35,32 +35,42 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
 }
 
 // ---- the order --------------------------------------------------------------------------------------------------------------
-// Short packs: each token's place is the number of tokens in front of it, counted: 32 tokens a workgroup, whose wavefronts compare 64 others at a
+// Short packs: each token's place is the number of tokens in front of it, counted: 16 tokens a workgroup, whose wavefronts compare 64 others at a
 // time and count the answers with one scalar instruction.  One launch, T^2 / 64 comparisons.
-constexpr int RANK_TOKENS = 32;
+constexpr int RANK_TOKENS = 16, RANK_LOADS = 8;
 __global__ __launch_bounds__(256) void embed_rank_kernel(EmbedArgs a, int *order, int *key) {
     __shared__ int counts[4][RANK_TOKENS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = blockIdx.x * RANK_TOKENS, none = a.vocab + a.features;
-    const int mine = t0 + (lane & 31) < a.T ? source_of(a, a.ids[t0 + (lane & 31)]) : none;
+    const int mine = t0 + (lane & 15) < a.T ? source_of(a, a.ids[t0 + (lane & 15)]) : none;
     int key_of[RANK_TOKENS], count[RANK_TOKENS];
 #pragma unroll
     for (int i = 0; i < RANK_TOKENS; ++i) {
         key_of[i] = __builtin_amdgcn_readlane(mine, i);
         count[i] = 0;
     }
-    for (int u0 = 64 * wave; u0 < a.T; u0 += 256) {
-        const int u = u0 + lane;
-        const int other = u < a.T ? source_of(a, a.ids[u]) : none + 1;       // behind all
-        if (u0 + 64 <= t0) {
+    // eight loads on their way: one at a time the kernel waited for memory (8192 tokens 27.5 us)
+    for (int first = 64 * wave; first < a.T; first += 256 * RANK_LOADS) {
+        int other[RANK_LOADS];
 #pragma unroll
-            for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(other <= key_of[i]));
-        } else if (u0 >= t0 + RANK_TOKENS) {
+        for (int b = 0; b < RANK_LOADS; ++b) {
+            const int u = first + 256 * b + lane;
+            other[b] = u < a.T ? a.ids[u] : 0;
+        }
 #pragma unroll
-            for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(other < key_of[i]));
-        } else {
+        for (int b = 0; b < RANK_LOADS; ++b) {
+            const int u0 = first + 256 * b, u = u0 + lane;
+            if (u0 >= a.T) break;
+            const int k = u < a.T ? source_of(a, other[b]) : none + 1;       // behind all
+            if (u0 + 64 <= t0) {
 #pragma unroll
-            for (int i = 0; i < RANK_TOKENS; ++i)
-                count[i] += __popcll(__builtin_amdgcn_ballot_w64(other < key_of[i] || (other == key_of[i] && u < t0 + i)));
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k <= key_of[i]));
+            } else if (u0 >= t0 + RANK_TOKENS) {
+#pragma unroll
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k < key_of[i]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k < key_of[i] || (k == key_of[i] && u < t0 + i)));
+            }
         }
     }
 #pragma unroll

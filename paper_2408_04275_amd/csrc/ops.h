@@ -98,7 +98,7 @@ hipError_t embed_fwd(int dtype, const EmbedArgs &a, hipStream_t st);
 size_t embed_bwd_bytes(int T, int H);
 hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st);
 
-// cross_attn.hip
+// cross_plan.hip, cross_mfma.hip, cross_mfma_bwd.hip, cross_f32.hip
 constexpr int CROSS_MAX_SEGMENTS = 1 << 16;
 struct CrossArgs {
     int Tq, Tk, S, nh, nkv, d;
@@ -114,11 +114,10 @@ struct CrossArgs {
     void *dk; long lddk;
     void *dv; long lddv;
     float *D;                       // backward scratch [nh, Tq]: rowsum(dO * O)
-    // cross_mfma.hip
     const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
-    int chunk;                      // keys of a workgroup with few rows; 0: all of its run's
+    int chunk;                      // keys of a workgroup; 0: all of its run's
     float *part; float2 *part_ml;   // partial results of the chunks
-    // cross_mfma_bwd.hip, dK and dV: see cross_plan_kernel
+    // dK and dV: see cross_plan_kernel
     const int *nb, *ne, *first_step, *cuts, *first_tile;
     const int4 *steps;
     int parts;                      // workgroups that share the rows which see a tile of keys
@@ -130,21 +129,22 @@ struct CrossPlan {
     int rows, chunk, items;         // rows of a workgroup, keys of a chunk (0: not cut), workgroups per key/value head
     bool table;                     // items are found in a table
 };
-// bf16 forward.  The workspace is 256-byte aligned.
-CrossPlan cross_mfma_fwd_plan(const CrossShape &c);
-size_t cross_mfma_fwd_bytes(const CrossShape &c, const CrossPlan &p);
-hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, void *ws, hipStream_t st);
-// exclusive sums of the runs' items (tiles of rows times chunks of keys), [S + 1]
-void cross_item_table(const CrossArgs &a, int tile_rows, int chunk, int *out, hipStream_t st);
 struct CrossBwdPlan {
     int rows, items;                // dQ: rows of a workgroup, workgroups per key/value head
     bool table, dkv;
     int tiles, steps, parts;        // dK and dV: tiles of keys, tiles of rows of all runs, workgroups per tile of keys
 };
-CrossBwdPlan cross_mfma_bwd_plan(const CrossShape &c, bool dkv);
-size_t cross_mfma_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p);
-hipError_t cross_mfma_bwd(const CrossArgs &a, const CrossBwdPlan &p, void *ws, hipStream_t st);
-hipError_t cross_fwd(int dtype, const CrossArgs &a, hipStream_t st);
-hipError_t cross_bwd(int dtype, const CrossArgs &a, hipStream_t st);
+// Plans, workspaces (256-byte aligned) and calls.  dkv: the gradients of keys and values are wanted
+CrossPlan cross_fwd_plan(int dtype, const CrossShape &c);
+size_t cross_fwd_bytes(const CrossShape &c, const CrossPlan &p);
+hipError_t cross_fwd(int dtype, const CrossArgs &a, const CrossPlan &p, void *ws, hipStream_t st);
+CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv);
+size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p);
+hipError_t cross_bwd(int dtype, const CrossArgs &a, const CrossBwdPlan &p, void *ws, hipStream_t st);
+// bf16 on the matrix cores; fp32 on the fp32 matrix instruction
+hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st);
+hipError_t cross_mfma_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st);
+hipError_t cross_f32_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st);
+hipError_t cross_f32_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st);
 
 }  // namespace mmt
