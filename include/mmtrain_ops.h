@@ -195,7 +195,8 @@ MMTRAIN_API size_t mmtrain_embed_workspace_bytes(const mmtrain_embed_desc *desc,
 /* From dy [n_tokens, hidden] writes d_table and d_features (either may be NULL: not computed).  flags concern d_table:
  * MMTRAIN_BWD_WGRAD_F32: it is fp32; MMTRAIN_BWD_ACCUMULATE_WGRAD: the sums are added to it, and rows that no token names are not
  * touched; without that flag every row is written, zeros where no token names it.  d_features (the type of `dtype`) is always
- * written as a whole.  Sums are fp32, of chunks of up to 16 + n_tokens / 2048 tokens and then of the chunks. */
+ * written as a whole.  Sums are fp32, of chunks of at most 64 + n_tokens / 2048 neighbours in the order
+ * and then of the chunks. */
 MMTRAIN_API int mmtrain_embed_bwd(const mmtrain_embed_desc *desc, int32_t n_tokens, const int32_t *ids_dev, const void *dy,
                                   void *d_table, void *d_features, uint32_t flags, void *workspace, size_t workspace_bytes,
                                   void *hip_stream);

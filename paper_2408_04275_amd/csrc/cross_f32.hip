@@ -211,13 +211,32 @@ __global__ __launch_bounds__(256) void cross_f32_combine_kernel(CrossArgs a) {
         const float2 *ml = a.part_ml + (size_t)blockIdx.x * 16 + r;
         const float *part = a.part + ((size_t)blockIdx.x * 16 + r) * dh + c;
         float m = -INFINITY, l = 0.f;
-        for (int j = 0; j < parts; ++j) m = fmaxf(m, ml[j * stride].x);
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < parts; ++j) {
-            const float2 v = ml[j * stride];
-            const float w = v.x == -INFINITY ? 0.f : expf(v.x - m);
-            l += v.y * w;
-            x += *reinterpret_cast<const f32x4 *>(part + j * stride * dh) * w;
+        for (int j0 = 0; j0 < parts; j0 += 8) {
+            float2 v[8];
+            f32x4 y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = make_float2(-INFINITY, 0.f);
+                y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (j0 + i < parts) {
+                    v[i] = ml[(j0 + i) * stride];
+                    y[i] = *reinterpret_cast<const f32x4 *>(part + (j0 + i) * stride * dh);
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].x);
+            const float base = top == -INFINITY ? 0.f : top, corr = expf(m - base);
+            l *= corr;
+            x *= corr;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = expf(v[i].x - base);
+                l += v[i].y * w;
+                x += y[i] * w;
+            }
+            m = top;
         }
         const int tok = g.token(mine.j + r), h = head * g.n + mine.j + r - tok * g.n;
         *reinterpret_cast<f32x4 *>((float *)a.o + (mine.t + tok) * a.ldo + (long)h * dh + c) = x * (l > 0.f ? 1.f / l : 0.f);
@@ -228,10 +247,13 @@ __global__ __launch_bounds__(256) void cross_f32_combine_kernel(CrossArgs a) {
 // dQ_i = scale * sum_j dS_ij k_j,  dS_ij = P_ij (dO_i . v_j - D_i),  D_i = dO_i . O_i (kept in a.D),  P_ij = exp(s_ij - lse_i)
 template <int KB, int NW>
 __global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
-    __shared__ __attribute__((aligned(16))) Partials<KB, NW> part;
+    __shared__ __attribute__((aligned(16))) union { Partials<KB, NW> part; int plan[PLAN_LDS / 4]; } lds;
+    Partials<KB, NW> &part = lds.part;
+    int block = blockIdx.x;
+    if (a.n_tiles > 0 && block-- == 0) { make_plan<64 * NW>(a, lds.plan); return; }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = threadIdx.x & 15, q4 = ((threadIdx.x & 48) >> 4) * 4;
-    const int head = blockIdx.x % a.nkv, dh = a.d;
-    const Item it = find_item(a, blockIdx.x / a.nkv, 16, 0);
+    const int head = block % a.nkv, dh = a.d;
+    const Item it = find_item(a, block / a.nkv, 16, 0);
     const Group g(a);
     const Rows mine(it, g, it.index * 16);
     const long col = (long)head * g.n * dh;
@@ -367,8 +389,8 @@ hipError_t cross_f32_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st)
 hipError_t cross_f32_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st) {
     return by_width(a.d, [&](auto KB_) {
         constexpr int KB = decltype(KB_)::value;
-        if (p.items) cross_f32_dq_kernel<KB, WAVES<KB>><<<p.items * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
-        if (p.dkv && p.tiles) cross_f32_dkv_kernel<KB, WAVES<KB>><<<p.tiles * (TILE_KEYS / 16) * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
+        if (p.items || a.n_tiles) cross_f32_dq_kernel<KB, WAVES<KB>><<<p.items * a.nkv + (a.n_tiles > 0), 64 * WAVES<KB>, 0, st>>>(a);
+        if (a.n_tiles) cross_f32_dkv_kernel<KB, WAVES<KB>><<<a.n_tiles * (TILE_KEYS / 16) * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
         return hipGetLastError();
     });
 }

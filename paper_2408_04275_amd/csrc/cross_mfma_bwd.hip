@@ -1,7 +1,7 @@
 // Backward of attention from runs of queries to ranges of keys on the matrix cores (bf16 in, fp32 accumulate): the layout of
 // cross_mfma.hip, two kernels.  dQ holds one row per lane and walks the keys of its run; it also writes -D, D = rowsum(dO * O).
 // dK/dV holds one key per lane and walks the rows that see its keys.  For that the keys are cut wherever a run's range begins or ends
-// (cross_plan_kernel): all keys of a tile are seen by the same runs, which follow one another, so again nothing is masked.  Keys that several runs
+// (make_plan): all keys of a tile are seen by the same runs, which follow one another, so again nothing is masked.  Keys that several runs
 // see, and heads of a group, are summed in registers, in the order of the runs: nothing needs atomics.
 #include "cross_tiles.h"
 #include <algorithm>
@@ -25,54 +25,53 @@ __device__ __forceinline__ void copy_rows_part(const bf16_t *p, long ld, int dh,
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
-// LDS: two slots of a K and a V tile; the Q and dO rows stand behind the first slot and O then takes Q's place (eight wavefronts), or all three
-// one after the other in the second slot (four)
-template <int D, int WAVES> constexpr int DQ_LDS = WAVES == 8 ? 2 * KEYS * D * 2 + 8 * 2 * ROWS32<D> : 2 * 2 * KEYS * D * 2;
+// Four wavefronts of 32 rows, two workgroups a compute unit (eight and one are nowhere faster: us, 128 / 256 rows, both backward kernels: 4096 tokens of 32 heads
+// of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284).
+// LDS: two slots of a K and a V tile; the Q, dO and O rows stand in the second slot, one after the other.
+template <int D> constexpr int DQ_LDS = 2 * 2 * KEYS * D * 2;
 
-template <int D, int KS, int CB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void cross_dq_kernel(CrossArgs a) {
+template <int D, int KS, int CB>
+__global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
     constexpr int TILE = KEYS * D * 2, SLOT = 2 * TILE, COPIES = TILE / 1024 / 4;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    const int head = blockIdx.x % a.nkv, dh = a.d;
-    const Item it = find_item(a, blockIdx.x / a.nkv, WAVES * 32, 0);
+    int block = blockIdx.x;
+    if (a.n_tiles > 0 && block-- == 0) { make_plan<256>(a, (int *)smem); return; }
+    const int head = block % a.nkv, dh = a.d;
+    const Item it = find_item(a, block / a.nkv, 128, 0);
     const Group g(a);
-    const Rows mine(it, g, it.index * WAVES * 32 + wave * 32);
+    const Rows mine(it, g, it.index * 128 + wave * 32);
     const int kbeg = it.lo, kend = a.dq ? it.hi : it.lo;
     const bf16_t *const K = (const bf16_t *)a.k + (long)head * dh, *const V = (const bf16_t *)a.v + (long)head * dh;
     const long col = (long)head * g.n * dh;
 
     RowCopier<D, COPIES> cpk, cpv;
-    cpk.init((wave & 3) * COPIES, a.ldk, dh);
-    cpv.init((wave & 3) * COPIES, a.ldv, dh);
+    cpk.init(wave * COPIES, a.ldk, dh);
+    cpv.init(wave * COPIES, a.ldv, dh);
     auto copy_kv = [&](uint8_t *slot, int kt) {
-        if (WAVES == 4 || wave >= 4) cpk.issue(rows_rsrc(K, kt, a.ldk, kend - kt, dh), slot, 0, 0, 0);
-        if (WAVES == 4 || wave < 4) cpv.issue(rows_rsrc(V, kt, a.ldv, kend - kt, dh), slot + TILE, 0, 0, 0);
+        cpk.issue(rows_rsrc(K, kt, a.ldk, kend - kt, dh), slot, 0, 0, 0);
+        cpv.issue(rows_rsrc(V, kt, a.ldv, kend - kt, dh), slot + TILE, 0, 0, 0);
     };
     bf16x8 qf[KS], dof[KS];
     float Dq = 0.f;
     {
-        uint8_t *const st_q = smem + SLOT + wave * (WAVES == 8 ? 2 : 1) * ROWS32<D>;
-        uint8_t *const st_do = WAVES == 8 ? st_q + ROWS32<D> : st_q;
-        copy_rows<D>((const bf16_t *)a.q + col, a.ldq, dh, mine, g, st_q);
-        if constexpr (WAVES == 8) copy_rows<D>((const bf16_t *)a.d_o + col, a.lddo, dh, mine, g, st_do);
+        uint8_t *const stage = smem + SLOT + wave * ROWS32<D>;
+        copy_rows<D>((const bf16_t *)a.q + col, a.ldq, dh, mine, g, stage);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = frag_k<D>(stage, l32, ks, half);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // read: dO may take the place
+        copy_rows<D>((const bf16_t *)a.d_o + col, a.lddo, dh, mine, g, stage);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dof[ks] = frag_k<D>(stage, l32, ks, half);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        copy_rows<D>((const bf16_t *)a.o + col, a.ldo, dh, mine, g, stage);
         if (kbeg < kend) copy_kv(smem, kbeg);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[ks] = frag_k<D>(st_q, l32, ks, half);
-        if constexpr (WAVES == 4) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            copy_rows<D>((const bf16_t *)a.d_o + col, a.lddo, dh, mine, g, st_do);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dof[ks] = frag_k<D>(st_do, l32, ks, half);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // read: O may take the place
-        copy_rows<D>((const bf16_t *)a.o + col, a.ldo, dh, mine, g, st_q);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const bf16x8 of = frag_k<D>(st_q, l32, ks, half);
+            const bf16x8 of = frag_k<D>(stage, l32, ks, half);
             const uint4 w = *reinterpret_cast<const uint4 *>(&dof[ks]), x = *reinterpret_cast<const uint4 *>(&of);
             const uint32_t dw[4] = {w.x, w.y, w.z, w.w}, ow[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -511,21 +510,22 @@ __global__ __launch_bounds__(256) void cross_dkv_sum_kernel(CrossArgs a) {
     *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
-template <int D, int KS, int CB, int WAVES>
+template <int D, int KS, int CB>
 hipError_t launch_dq(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
-    constexpr int LDS = std::max(DQ_LDS<D, WAVES>, WAVES * STAGE<D>);
-    const hipError_t e = set_smem(done, cross_dq_kernel<D, KS, CB, WAVES>, LDS);
+    constexpr int LDS = std::max(DQ_LDS<D>, 4 * STAGE<D>);
+    static_assert(PLAN_LDS <= LDS, "room for the plan");
+    const hipError_t e = set_smem(done, cross_dq_kernel<D, KS, CB>, LDS);
     if (e != hipSuccess) return e;
-    cross_dq_kernel<D, KS, CB, WAVES><<<items * a.nkv, WAVES * 64, LDS, st>>>(a);
+    cross_dq_kernel<D, KS, CB><<<items * a.nkv + (a.n_tiles > 0), 256, LDS, st>>>(a);
     return hipGetLastError();
 }
 
 template <int D, int KS, int CB>
 hipError_t launch_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st) {
     hipError_t e = hipSuccess;
-    if (p.items) e = p.rows == 256 ? launch_dq<D, KS, CB, 8>(a, p.items, st) : launch_dq<D, KS, CB, 4>(a, p.items, st);
-    if (e != hipSuccess || !p.dkv || !p.tiles) return e;
+    if (p.items || a.n_tiles) e = launch_dq<D, KS, CB>(a, p.items, st);
+    if (e != hipSuccess || !a.n_tiles) return e;
     static std::atomic<bool> done{false};
     const dim3 grid(p.tiles * a.nkv, a.parts);
     if constexpr (D <= 64) {

@@ -35,68 +35,6 @@ __global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int til
     if (threadIdx.x == 0) out[a.S] = base;
 }
 
-// ---- dK, dV: what is walked ---------------------------------------------------------------------------------------------------
-// One workgroup.  Where the runs that see something begin and end, non-decreasing, is completed over the others (nb, ne: a run that sees nothing gets
-// the last one's); all those places together, sorted, cut the keys into pieces (cuts, [2 S + 2]); first_tile [2 S + 2]: tiles of
-// 128 keys in front of each piece; first_step [S + 1]: steps of 64 rows in front of each run; steps: {token, head of the group, rows} of each.
-__device__ __forceinline__ int block_scan(int v, bool max, int *sums) {      // inclusive, of 1024 threads
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int u = __shfl_up(v, o, 64);
-        if (lane >= o) v = max ? ::max(v, u) : v + u;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = v;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) v = max ? ::max(v, sums[w]) : v + sums[w];
-    return v;
-}
-__global__ __launch_bounds__(1024) void cross_plan_kernel(CrossArgs a, int *nb, int *ne, int *first_step, int *cuts, int *first_tile, int4 *steps) {
-    __shared__ int sums[16], carry[3];
-    const int group = a.nh / a.nkv, S = a.S;
-    if (threadIdx.x < 3) carry[threadIdx.x] = 0;
-    __syncthreads();
-    for (int s0 = 0; s0 < S; s0 += 1024) {
-        const int s = s0 + threadIdx.x;
-        int b = 0, e = 0, n = 0;
-        if (s < S && a.begin[s] < a.end[s]) {
-            b = a.begin[s]; e = a.end[s];
-            n = ((a.cu[s + 1] - a.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
-        }
-        b = max(block_scan(b, true, sums), carry[0]);
-        e = max(block_scan(e, true, sums), carry[1]);
-        const int sum = block_scan(n, false, sums) + carry[2];
-        if (s < S) { nb[s] = b; ne[s] = e; first_step[s] = sum - n; }
-        __syncthreads();
-        if (threadIdx.x == 1023) { carry[0] = b; carry[1] = e; carry[2] = sum; }
-        __syncthreads();
-    }
-    const int all = carry[2];
-    if (threadIdx.x == 0) { first_step[S] = all; cuts[0] = 0; cuts[2 * S + 1] = a.Tk; carry[0] = 0; }
-    __threadfence_block();
-    __syncthreads();
-    for (int s = threadIdx.x; s < S; s += 1024) {
-        cuts[1 + s + lower_bound(ne, S, nb[s], false)] = nb[s];
-        cuts[1 + s + lower_bound(nb, S, ne[s], true)] = ne[s];
-    }
-    __threadfence_block();
-    __syncthreads();
-    for (int p0 = 0; p0 < 2 * S + 1; p0 += 1024) {
-        const int p = p0 + threadIdx.x, n = p < 2 * S + 1 ? (cuts[p + 1] - cuts[p] + TILE_KEYS - 1) / TILE_KEYS : 0;
-        const int sum = block_scan(n, false, sums) + carry[0];
-        if (p < 2 * S + 1) first_tile[p] = sum - n;
-        if (p == 2 * S) first_tile[2 * S + 1] = sum;
-        __syncthreads();
-        if (threadIdx.x == 1023) carry[0] = sum;
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < all; i += 1024) {
-        const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group;
-        steps[i] = make_int4(a.cu[s] + tok, row - tok * group, min((a.cu[s + 1] - a.cu[s]) * group - row, STEP_ROWS), 0);
-    }
-}
-
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
 size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
 
@@ -119,7 +57,10 @@ CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
         longest = std::max(longest, keys);
     }
     CrossPlan p = {};
-    p.rows = dtype == DT_F32 ? 16 : many > 2 * few || count(128, 0) * c.nkv < 128 ? FEW_ROWS : c.d > 64 ? 256 : 128;
+    // Workgroups of 128 rows, two of which share a compute unit and cover each other's beginnings and ends, or of 256, which read keys half as often: where
+    // a tile walks 64 steps of 64 keys and more on average.  us, 128 / 256 rows, heads of 128: 4096 tokens of 32 heads on 8 in one run of 8192 keys 524 / 492,
+    // of 32 heads in four runs of 2304 175 / 184; of 80, 8 runs of 1024 38 / 42; of 64, 16 runs of 576 34 / 42.
+    p.rows = dtype == DT_F32 ? 16 : many > 2 * few || count(128, 0) * c.nkv < 128 ? FEW_ROWS : c.d > 64 && many >= 512 * count(128, 0) ? 256 : 128;
     if (p.rows <= FEW_ROWS && count(p.rows, 0) * c.nkv < 512 && longest > 32) {
         const long want = std::max(few * c.nkv / 1024, 8l);      // blocks of 32 keys a workgroup
         p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
@@ -154,7 +95,7 @@ hipError_t cross_fwd(int dtype, const CrossArgs &args, const CrossPlan &p, void 
 CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     const int group = c.nh / c.nkv;
     CrossBwdPlan p = {};
-    p.rows = dtype == DT_F32 ? 16 : c.d > 64 ? 256 : 128;
+    p.rows = dtype == DT_F32 ? 16 : 128;
     for (int s = 0; s < c.S; ++s) p.items += items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
     p.table = c.S > 64;
     p.dkv = dkv;
@@ -185,10 +126,12 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     return p;
 }
 
-// [D] [table of items] [nb, ne, first_step, cuts, first_tile] [steps] [parts]
+size_t plan_bytes(int runs) { return runs > PLAN_LDS_RUNS ? aligned((size_t)PLAN_INTS(runs) * sizeof(int)) : 0; }
+
+// [D] [table of items] [tiles] [steps] [what they are made of] [parts]
 size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p) {
     size_t n = aligned((size_t)c.Tq * c.nh * sizeof(float)) + (p.table ? table_bytes(c.S) : 0);
-    if (p.dkv) n += 3 * table_bytes(c.S) + 2 * table_bytes(2 * c.S + 1) + aligned((size_t)p.steps * sizeof(int4)) + (p.parts > 1 ? p.parts * part_bytes(c) : 0);
+    if (p.dkv) n += aligned((size_t)p.tiles * sizeof(int4)) + aligned((size_t)p.steps * sizeof(int4)) + plan_bytes(c.S) + (p.parts > 1 ? p.parts * part_bytes(c) : 0);
     return n;
 }
 
@@ -203,12 +146,11 @@ hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossBwdPlan &p, vo
         if (p.items) cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, 0, const_cast<int *>(a.prefix));
     }
     if (p.dkv && p.tiles) {
-        int *nb = (int *)take(table_bytes(a.S)), *ne = (int *)take(table_bytes(a.S)), *first_step = (int *)take(table_bytes(a.S));
-        int *cuts = (int *)take(table_bytes(2 * a.S + 1)), *first_tile = (int *)take(table_bytes(2 * a.S + 1));
-        int4 *steps = (int4 *)take(aligned((size_t)p.steps * sizeof(int4)));
-        a.nb = nb; a.ne = ne; a.first_step = first_step; a.cuts = cuts; a.first_tile = first_tile; a.steps = steps;
+        a.tiles = (int4 *)take(aligned((size_t)p.tiles * sizeof(int4)));
+        a.steps = (int4 *)take(aligned((size_t)p.steps * sizeof(int4)));
+        a.plan = (int *)take(plan_bytes(a.S));
+        a.n_tiles = p.tiles; a.n_steps = p.steps;
         a.dkv_part = (float *)at;
-        cross_plan_kernel<<<1, 1024, 0, st>>>(a, nb, ne, first_step, cuts, first_tile, steps);
     }
     if (!p.items && !(p.dkv && p.tiles)) return hipSuccess;
     return dtype == DT_F32 ? cross_f32_bwd(a, p, st) : cross_mfma_bwd(a, p, st);

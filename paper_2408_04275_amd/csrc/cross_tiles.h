@@ -24,6 +24,17 @@ __host__ __device__ inline int items_of(int tokens, int keys, int group, int til
     return tiles * (parts > 0 ? parts : 1);
 }
 
+// inclusive sums over the wavefront, in the vector ALU
+template <int CTRL, int ROWS> __device__ __forceinline__ int scan_step(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+    v = scan_step<0x111, 0xf>(v);           // row_shr 1, 2, 4, 8
+    v = scan_step<0x112, 0xf>(v);
+    v = scan_step<0x114, 0xf>(v);
+    v = scan_step<0x118, 0xf>(v);
+    v = scan_step<0x142, 0xa>(v);           // row_bcast 15 to rows 1 and 3
+    return scan_step<0x143, 0xc>(v);        // row_bcast 31 to rows 2 and 3
+}
+
 struct Item {
     int q0, rows, lo, hi;       // run: first token, rows of a key/value head, keys
     int index, first;           // the item's number within its run; of the run's first item among all
@@ -38,12 +49,7 @@ __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_ro
         int c0 = 0, c1 = 0, lo = 0, hi = 0;
         if (lane < a.S) { c0 = a.cu[lane]; c1 = a.cu[lane + 1]; lo = a.begin[lane]; hi = a.end[lane]; }
         const int n = lane < a.S ? items_of(c1 - c0, hi - lo, group, tile_rows, chunk) : 0;
-        int sum = n;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const int v = __shfl_up(sum, o, 64);
-            if (lane >= o) sum += v;
-        }
+        const int sum = wave_scan(n);
         const int s = min(__popcll(__builtin_amdgcn_ballot_w64(sum <= y)), 63);
         it.q0 = __builtin_amdgcn_readlane(c0, s);
         it.rows = (__builtin_amdgcn_readlane(c1, s) - it.q0) * group;
@@ -142,27 +148,99 @@ __device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool uppe
     }
     return lo;
 }
+// ---- dK, dV: what is walked ---------------------------------------------------------------------------------------------------
+// The runs that see something begin and end in their order; the others get the last one's beginning and end (nb, ne).  All those places
+// together, sorted, cut the keys into pieces (cuts, [2 S + 2]) whose keys are seen by the same runs, and these follow one another.  A tile is up to
+// 128 keys of a piece: {key, end of the piece, first step, steps}; a step up to 64 rows of a run: {token, head of the group, rows}.
+// One workgroup makes both lists; it stands in front of dQ's, which do not need them.
+constexpr int PLAN_LDS_RUNS = 256;      // as many runs' places are kept in LDS while they are searched (more: in the workspace)
+constexpr int PLAN_INTS(int runs) { return 3 * (runs + 1) + 2 * (2 * runs + 2); }
+constexpr int PLAN_LDS = (PLAN_INTS(PLAN_LDS_RUNS) + 32) * 4;
+template <int THREADS>
+__device__ __forceinline__ int block_scan(int v, bool max, int *sums) {      // inclusive
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int u = __shfl_up(v, o, 64);
+        if (lane >= o) v = max ? ::max(v, u) : v + u;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w)
+        if (w < wave) v = max ? ::max(v, sums[w]) : v + sums[w];
+    return v;
+}
+template <int THREADS>
+__device__ void make_plan(const CrossArgs &a, int *lds) {
+    int *const sums = lds, *const carry = lds + 16;
+    const int group = a.nh / a.nkv, S = a.S;
+    int *const nb = S <= PLAN_LDS_RUNS ? lds + 32 : a.plan, *const ne = nb + S + 1, *const first_step = ne + S + 1, *const cuts = first_step + S + 1,
+        *const first_tile = cuts + 2 * S + 2;
+    if (threadIdx.x < 3) carry[threadIdx.x] = 0;
+    __syncthreads();
+    for (int s0 = 0; s0 < S; s0 += THREADS) {
+        const int s = s0 + threadIdx.x;
+        int b = 0, e = 0, n = 0;
+        if (s < S) {
+            const int lo = a.begin[s], hi = a.end[s], c0 = a.cu[s], c1 = a.cu[s + 1];
+            if (lo < hi) { b = lo; e = hi; n = ((c1 - c0) * group + STEP_ROWS - 1) / STEP_ROWS; }
+        }
+        b = max(block_scan<THREADS>(b, true, sums), carry[0]);
+        e = max(block_scan<THREADS>(e, true, sums), carry[1]);
+        const int sum = block_scan<THREADS>(n, false, sums) + carry[2];
+        if (s < S) { nb[s] = b; ne[s] = e; first_step[s] = sum - n; }
+        __syncthreads();
+        if (threadIdx.x == THREADS - 1) { carry[0] = b; carry[1] = e; carry[2] = sum; }
+        __syncthreads();
+    }
+    const int all = carry[2];
+    __syncthreads();
+    if (threadIdx.x == 0) { first_step[S] = all; cuts[0] = 0; cuts[2 * S + 1] = a.Tk; carry[0] = 0; }
+    __threadfence_block();
+    __syncthreads();
+    for (int s = threadIdx.x; s < S; s += THREADS) {
+        cuts[1 + s + lower_bound(ne, S, nb[s], false)] = nb[s];
+        cuts[1 + s + lower_bound(nb, S, ne[s], true)] = ne[s];
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int p0 = 0; p0 < 2 * S + 1; p0 += THREADS) {
+        const int p = p0 + threadIdx.x, n = p < 2 * S + 1 ? (cuts[p + 1] - cuts[p] + TILE_KEYS - 1) / TILE_KEYS : 0;
+        const int sum = block_scan<THREADS>(n, false, sums) + carry[0];
+        if (p < 2 * S + 1) first_tile[p] = sum - n;
+        __syncthreads();
+        if (threadIdx.x == THREADS - 1) carry[0] = sum;
+        __syncthreads();
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int y = threadIdx.x; y < a.n_tiles; y += THREADS) {
+        const int p = find_segment(first_tile, 2 * S + 1, y), first = cuts[p];
+        // the runs that see the piece: behind the last that ends in front of it
+        const int begin = S > 0 ? first_step[lower_bound(ne, S, first, true)] : 0, end = S > 0 ? first_step[lower_bound(nb, S, first, true)] : 0;
+        a.tiles[y] = make_int4(first + (y - first_tile[p]) * TILE_KEYS, cuts[p + 1], begin, max(end - begin, 0));
+    }
+    for (int i = threadIdx.x; i < a.n_steps; i += THREADS) {
+        const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group, c0 = a.cu[s];
+        a.steps[i] = make_int4(c0 + tok, row - tok * group, min((a.cu[s + 1] - c0) * group - row, STEP_ROWS), 0);
+    }
+}
+
 struct KeyTile {
     int key, end;               // keys
     int step, steps;            // first step, how many
 };
 __device__ __forceinline__ KeyTile find_tile(const CrossArgs &a, int y) {
+    const int4 v = a.tiles[y];
     KeyTile k;
-    const int p = find_segment(a.first_tile, 2 * a.S + 1, y), first = a.cuts[p];
-    k.key = first + (y - a.first_tile[p]) * TILE_KEYS;
-    k.end = a.cuts[p + 1];
-    int begin = 0, end = 0;                            // the runs that see the piece: behind the last that ends in front of it
-    if (a.S > 0) {
-        begin = a.first_step[lower_bound(a.ne, a.S, first, true)];
-        end = a.first_step[lower_bound(a.nb, a.S, first, true)];
-    }
-    const long n = max(end - begin, 0);
+    k.key = __builtin_amdgcn_readfirstlane(v.x);
+    k.end = __builtin_amdgcn_readfirstlane(v.y);
+    const int begin = __builtin_amdgcn_readfirstlane(v.z);
+    const long n = __builtin_amdgcn_readfirstlane(v.w);
     k.step = begin + (int)(n * blockIdx.y / a.parts);
     k.steps = begin + (int)(n * (blockIdx.y + 1) / a.parts) - k.step;
-    k.key = __builtin_amdgcn_readfirstlane(k.key);
-    k.end = __builtin_amdgcn_readfirstlane(k.end);
-    k.step = __builtin_amdgcn_readfirstlane(k.step);
-    k.steps = __builtin_amdgcn_readfirstlane(k.steps);
     return k;
 }
 __device__ __forceinline__ Rows rows_of(const int4 &e) {

@@ -6,6 +6,7 @@
 #include "ops.h"
 #include "vec8.h"
 #include <algorithm>
+#include <atomic>
 
 namespace mmt {
 namespace {
@@ -35,12 +36,12 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
 }
 
 // ---- the order --------------------------------------------------------------------------------------------------------------
-// Short packs: each token's place is the number of tokens in front of it, counted: 16 tokens a workgroup, whose wavefronts compare 64 others at a
-// time and count the answers with one scalar instruction.  One launch, T^2 / 64 comparisons.
+// Short packs: each token's place is the number of tokens in front of it, counted: 16 tokens a workgroup, whose threads compare every other token
+// with all of them.  One launch, 2 T^2 / 64 vector instructions.
 constexpr int RANK_TOKENS = 16, RANK_LOADS = 8;
 __global__ __launch_bounds__(256) void embed_rank_kernel(EmbedArgs a, int *order, int *key) {
-    __shared__ int counts[4][RANK_TOKENS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = blockIdx.x * RANK_TOKENS, none = a.vocab + a.features;
+    __shared__ int counts[RANK_TOKENS][256 + 4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t0 = blockIdx.x * RANK_TOKENS, none = a.vocab + a.features;
     const int mine = t0 + (lane & 15) < a.T ? source_of(a, a.ids[t0 + (lane & 15)]) : none;
     int key_of[RANK_TOKENS], count[RANK_TOKENS];
 #pragma unroll
@@ -59,29 +60,111 @@ __global__ __launch_bounds__(256) void embed_rank_kernel(EmbedArgs a, int *order
 #pragma unroll
         for (int b = 0; b < RANK_LOADS; ++b) {
             const int u0 = first + 256 * b, u = u0 + lane;
-            if (u0 >= a.T) break;
             const int k = u < a.T ? source_of(a, other[b]) : none + 1;       // behind all
             if (u0 + 64 <= t0) {
 #pragma unroll
-                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k <= key_of[i]));
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += k <= key_of[i];
             } else if (u0 >= t0 + RANK_TOKENS) {
 #pragma unroll
-                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k < key_of[i]));
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += k < key_of[i];
             } else {
 #pragma unroll
-                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += __popcll(__builtin_amdgcn_ballot_w64(k < key_of[i] || (k == key_of[i] && u < t0 + i)));
+                for (int i = 0; i < RANK_TOKENS; ++i) count[i] += k < key_of[i] || (k == key_of[i] && u < t0 + i);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < RANK_TOKENS; ++i)
-        if (lane == 0) counts[wave][i] = count[i];
+    for (int i = 0; i < RANK_TOKENS; ++i) counts[i][threadIdx.x] = count[i];
     __syncthreads();
-    const int t = t0 + threadIdx.x;
-    if (threadIdx.x < RANK_TOKENS && t < a.T) {
-        const int at = counts[0][threadIdx.x] + counts[1][threadIdx.x] + counts[2][threadIdx.x] + counts[3][threadIdx.x];
+    const int i = threadIdx.x >> 4, x = threadIdx.x & 15;                    // 16 threads a token
+    int at = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) at += counts[i][16 * j + x];
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) at += __shfl_xor(at, o, 64);
+    const int t = t0 + i;
+    if (x == 0 && t < a.T) {
         order[at] = t;
-        key[at] = mine;
+        key[at] = source_of(a, a.ids[t]);
+    }
+}
+
+// Longer ones: blocks of 512 tokens are put in order by themselves (halves by counting, then by a search in the other half), and a token's
+// place is then what a search in every other block says is in front of it; equal ones count in the blocks before its own.  A workgroup of the second
+// launch has 64 tokens of a block and all keys in LDS, and each of its wavefronts searches some of the blocks, four at a time.
+constexpr int SORT_BLOCK = 512;
+typedef __attribute__((address_space(3))) void lds_void;
+// entries of N sorted ones (a power of two) that are below v
+template <int N>
+__device__ __forceinline__ int entries_below(const int *x, int v) {
+    int lo = 0;
+#pragma unroll
+    for (int step = N / 2; step > 0; step /= 2) lo += x[lo + step - 1] < v ? step : 0;
+    return lo + (x[lo] < v);
+}
+__global__ __launch_bounds__(SORT_BLOCK) void embed_blocks_kernel(EmbedArgs a, int *order, int *key) {
+    __shared__ __attribute__((aligned(16))) int keys[SORT_BLOCK], sorted[SORT_BLOCK];
+    const int i = threadIdx.x, t = blockIdx.x * SORT_BLOCK + i, wave = __builtin_amdgcn_readfirstlane(i >> 6), none = a.vocab + a.features;
+    const int mine = t < a.T ? source_of(a, a.ids[t]) : none + 1;            // behind all
+    keys[i] = mine;
+    __syncthreads();
+    const int half = wave / 4 * 256;
+    int at = 0;
+    auto count = [&](int first, auto f) {
+#pragma unroll 4
+        for (int j = first; j < first + 64; j += 4) {
+            const int4 k = *reinterpret_cast<const int4 *>(keys + j);
+            at += f(k.x, j) + f(k.y, j + 1) + f(k.z, j + 2) + f(k.w, j + 3);
+        }
+    };
+    for (int w = 0; w < 4; ++w) {
+        if (w < (wave & 3)) count(half + 64 * w, [&](int k, int) { return (int)(k <= mine); });
+        else if (w > (wave & 3)) count(half + 64 * w, [&](int k, int) { return (int)(k < mine); });
+        else count(half + 64 * w, [&](int k, int j) { return (int)(k < mine || (k == mine && j < i)); });
+    }
+    sorted[half + at] = mine;
+    __syncthreads();
+    at += entries_below<256>(sorted + (256 - half), mine + (half > 0));
+    key[blockIdx.x * SORT_BLOCK + at] = mine;
+    order[blockIdx.x * SORT_BLOCK + at] = t;
+}
+__global__ __launch_bounds__(256) void embed_merge_kernel(EmbedArgs a, const int *block_order, const int *block_key, int *order, int *key) {
+    extern __shared__ __attribute__((aligned(16))) int keys[];               // [blocks][512], then [4][64] counts
+    const int blocks = (a.T + SORT_BLOCK - 1) / SORT_BLOCK;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), own = blockIdx.x / (SORT_BLOCK / 64);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<int *>(block_key), 0, blocks * SORT_BLOCK * 4, 0x00020000);
+    for (int i = wave; i < blocks * (SORT_BLOCK / 256); i += 4)              // 256 keys each
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(keys + i * 256), 16, i * 1024 + lane * 16, 0, 0, 0);
+    int *const counts = keys + blocks * SORT_BLOCK;
+    const int at = blockIdx.x * 64 + lane;
+    const int t = block_order[at], mine = block_key[at];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int before = 0;
+    for (int b0 = wave; b0 < blocks; b0 += 16) {
+        int lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lo[i] = 0;
+#pragma unroll
+        for (int step = SORT_BLOCK / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = min(b0 + 4 * i, blocks - 1);
+                lo[i] += keys[b * SORT_BLOCK + lo[i] + step - 1] < mine + (b < own) ? step : 0;
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = min(b0 + 4 * i, blocks - 1);
+            const int n = lo[i] + (keys[b * SORT_BLOCK + lo[i]] < mine + (b < own));
+            before += b0 + 4 * i < blocks && b != own ? n : 0;
+        }
+    }
+    counts[wave * 64 + lane] = before;
+    __syncthreads();
+    if (wave == 0 && t < a.T) {
+        const int place = counts[lane] + counts[64 + lane] + counts[128 + lane] + counts[192 + lane] + at % SORT_BLOCK;
+        order[place] = t;
+        key[place] = mine;
     }
 }
 
@@ -259,21 +342,30 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s
         }
         return;
     }
-    const int c = (blockIdx.x % slabs) * s.columns + threadIdx.x * 8;
-    if (c >= a.H || (int)threadIdx.x * 8 >= s.columns) return;
-    const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, a.T);
-    const int before = p0 > 0 ? s.key[p0 - 1] : -1;
+    const int column = (blockIdx.x % slabs) * s.columns + threadIdx.x * 8;
+    const bool live = column < a.H;
+    const int c = live ? column : 0;                   // (a wavefront stays whole: its lanes hold the places)
+    const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, a.T), lane = threadIdx.x & 63;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    bool whole = s.key[p0] != before;                  // the present row's first token is in this chunk
+    bool whole = true;                                 // the present row's first token is in this chunk
+    int keys = 0, tokens = 0;                          // lane i: key and token of place base - 1 + i
+    int base = p0;
     for (int p = p0; p < p1; p += SUM_ROWS) {
+        if (p == p0 || p - base > 62 - SUM_ROWS - 1) {
+            base = p;
+            const int at = base - 1 + lane;
+            keys = at >= 0 && at < a.T ? s.key[at] : -1;
+            tokens = at >= 0 && at < a.T ? s.order[at] : 0;
+            if (p == p0) whole = __builtin_amdgcn_readlane(keys, 0) != __builtin_amdgcn_readlane(keys, 1);
+        }
         int row[SUM_ROWS + 1];
         Raw8<T> x[SUM_ROWS];
         float old[SUM_ROWS][8];
 #pragma unroll
-        for (int i = 0; i <= SUM_ROWS; ++i) row[i] = p + i < a.T ? s.key[p + i] : -1;
+        for (int i = 0; i <= SUM_ROWS; ++i) row[i] = __builtin_amdgcn_readlane(keys, p - base + 1 + i);
 #pragma unroll
         for (int i = 0; i < SUM_ROWS; ++i)
-            if (p + i < p1 && row[i] != none) x[i] = load_plain8((const T *)a.dy + (long)s.order[p + i] * a.H + c);
+            if (p + i < p1 && row[i] != none) x[i] = load_plain8((const T *)a.dy + (long)__builtin_amdgcn_readlane(tokens, p - base + 1 + i) * a.H + c);
         if (a.accumulate && a.d_table) {
 #pragma unroll
             for (int i = 0; i < SUM_ROWS; ++i)
@@ -287,8 +379,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += v[e];
             const bool ends = row[i] != row[i + 1], last = p + i + 1 == p1;
-            if (ends && whole) put_row<T, G>(a, row[i], c, sum, old[i]);
-            else if (ends || last) store8(s.part + ((size_t)chunk * 2 + (whole ? 1 : 0)) * a.H + c, sum);
+            if (ends && whole) { if (live) put_row<T, G>(a, row[i], c, sum, old[i]); }
+            else if ((ends || last) && live) store8(s.part + ((size_t)chunk * 2 + (whole ? 1 : 0)) * a.H + c, sum);
             if (ends) {
                 whole = true;
 #pragma unroll
@@ -298,22 +390,25 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s
     }
 }
 
-// Rows whose tokens stand in several chunks: the workgroup of the chunk that a row begins in adds up the chunks' sums, four threads of one
-// column eight at a time
+// Rows whose tokens stand in several chunks: the workgroup of the chunk that a row begins in adds up the chunks' sums, four threads per eight
+// columns, a quarter of the chunks each
+constexpr int JOIN_COLUMNS = 512;
 template <typename T, typename G>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedSums s) {
     __shared__ float red[3][64][9];
-    const int slabs = (a.H + 511) / 512, chunk = blockIdx.x / slabs;
-    const int last = min((chunk + 1) * s.chunk, a.T) - 1, row = s.key[last];
-    if (last + 1 >= a.T || row == a.vocab + a.features || s.key[last + 1] != row) return;          // ends here
-    if (chunk > 0 && s.key[chunk * s.chunk - 1] == row) return;                                     // began earlier
+    const int slabs = (a.H + JOIN_COLUMNS - 1) / JOIN_COLUMNS, chunk = blockIdx.x / slabs;
+    const int last = min((chunk + 1) * s.chunk, a.T) - 1;
+    if (last + 1 >= a.T) return;
+    const int row = s.key[last], next = s.key[last + 1], first = s.key[max(chunk * s.chunk - 1, 0)];
+    if (row == a.vocab + a.features || next != row) return;          // ends here
+    if (chunk > 0 && first == row) return;                           // began earlier
     int lo = last + 1, hi = a.T;                       // the row's end in the order
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (s.key[mid] == row) lo = mid + 1; else hi = mid;
     }
     const int n = (lo - 1) / s.chunk - chunk;          // chunks behind this one
-    const int c = (blockIdx.x % slabs) * 512 + (threadIdx.x & 63) * 8, q = threadIdx.x >> 6;
+    const int c = (blockIdx.x % slabs) * JOIN_COLUMNS + (threadIdx.x & 63) * 8, q = threadIdx.x >> 6;
     const bool live = c < a.H;
     const size_t stride = (size_t)2 * a.H;
     const float *part = s.part + (size_t)(chunk + 1) * stride + c;       // their first rows
@@ -354,9 +449,14 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedSums 
 }
 
 // ---- sizes ---------------------------------------------------------------------------------------------------------------------------
-constexpr int RANK_MAX = 32768;                        // the longest pack that is ordered by counting
-// tokens a chunk: as few as keep their number within 2048
-int chunk_of(int T) { return std::max(16, (T / 2048 + 8) / 8 * 8); }
+constexpr int RANK_MAX = 4096, MERGE_MAX = 32768;      // the longest packs that are ordered by counting, and by blocks (whose keys fill 128 KB of LDS)
+// Tokens a chunk: 16 at least, and up to 64 while the chip has work enough (fewer rows reach into other chunks, whose partial sums are written and read
+// back); as many as keep the chunks' number within 2048.
+int chunk_of(int T, int H) {
+    int c = 16;
+    while (c < 64 && (long)ceil_div(T, 2 * c) * ceil_div(H, 2048) >= 1024) c *= 2;
+    return std::max(c, (T / 2048 + 8) / 8 * 8);
+}
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
 int radix_blocks(int T) { return ceil_div(T, RADIX_BLOCK); }
 
@@ -366,7 +466,7 @@ hipError_t sums(const EmbedArgs &a, const EmbedSums &s, hipStream_t st) {
     const int first = a.accumulate || !a.d_table ? a.vocab : 0, rows = (a.d_rows ? a.vocab + a.features : a.vocab) - first;
     const int blocks = s.chunks * slabs + ceil_div(rows, s.fill_rows);
     if (blocks) embed_sum_kernel<T, G><<<blocks, threads, 0, st>>>(a, s);
-    if (s.chunks > 1) embed_join_kernel<T, G><<<s.chunks * ceil_div(a.H, 512), 256, 0, st>>>(a, s);
+    if (s.chunks > 1) embed_join_kernel<T, G><<<s.chunks * ceil_div(a.H, JOIN_COLUMNS), 256, 0, st>>>(a, s);
     return blocks ? hipGetLastError() : hipSuccess;
 }
 
@@ -380,14 +480,11 @@ hipError_t embed_fwd(int dtype, const EmbedArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// [key] [order] [partial sums], and for long packs [key] [order] [counts] of the sort
+// [key] [order] [partial sums], and for longer packs [key] [order] [counts] of the sort
 size_t embed_bwd_bytes(int T, int H) {
-    size_t most = 0;
-    // (a longer pack has fewer chunks where theirs become longer: the most of any up to T)
-    auto parts = [&](int t) { return (size_t)ceil_div(t, chunk_of(t)) * 2 * H * sizeof(float); };
-    most = std::max(parts(T), T >= 2048 * 16 ? (size_t)2050 * 2 * H * sizeof(float) : 0);
+    const size_t most = (size_t)std::min(ceil_div(T, 16), 2048) * 2 * H * sizeof(float);        // (never falls; longer chunks need less)
     return 2 * aligned((size_t)T * sizeof(int)) + aligned(most) +
-           (T > RANK_MAX ? 2 * aligned((size_t)T * sizeof(int)) + aligned(256ul * radix_blocks(T) * sizeof(int)) : 0) + 256;
+           (T > RANK_MAX ? 2 * aligned(((size_t)T + SORT_BLOCK) * sizeof(int)) : 0) + (T > MERGE_MAX ? aligned(256ul * radix_blocks(T) * sizeof(int)) : 0) + 256;
 }
 
 hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st) {
@@ -395,8 +492,12 @@ hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st) {
     uint8_t *at = (uint8_t *)a.ws;
     auto take = [&](size_t n) { void *p = at; at += aligned(n); return p; };
     int *key = (int *)take((size_t)a.T * sizeof(int)), *order = (int *)take((size_t)a.T * sizeof(int));
+    int *key2 = nullptr, *order2 = nullptr;
     if (a.T > RANK_MAX) {
-        int *key2 = (int *)take((size_t)a.T * sizeof(int)), *order2 = (int *)take((size_t)a.T * sizeof(int));
+        key2 = (int *)take(((size_t)a.T + SORT_BLOCK) * sizeof(int));
+        order2 = (int *)take(((size_t)a.T + SORT_BLOCK) * sizeof(int));
+    }
+    if (a.T > MERGE_MAX) {
         RadixPass p = {};
         p.blocks = radix_blocks(a.T);
         p.hist = (int *)take(256ul * p.blocks * sizeof(int));
@@ -412,9 +513,19 @@ hipError_t embed_bwd(int dtype, const EmbedArgs &a, hipStream_t st) {
             embed_radix_move_kernel<<<p.blocks, 256, 0, st>>>(a, p);
             p.key_in = p.key_out; p.order_in = p.order_out;
         }
+    } else if (a.T > RANK_MAX) {
+        static std::atomic<bool> done{false};
+        const int blocks = ceil_div(a.T, SORT_BLOCK), lds = (blocks * SORT_BLOCK + 256) * (int)sizeof(int);
+        if (!done.load(std::memory_order_acquire)) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(embed_merge_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (MERGE_MAX + 256) * (int)sizeof(int));
+            if (e != hipSuccess) return e;
+            done.store(true, std::memory_order_release);
+        }
+        embed_blocks_kernel<<<blocks, SORT_BLOCK, 0, st>>>(a, order2, key2);
+        embed_merge_kernel<<<ceil_div(a.T, 64), 256, lds, st>>>(a, order2, key2, order, key);
     } else if (a.T > 0) embed_rank_kernel<<<ceil_div(a.T, RANK_TOKENS), 256, 0, st>>>(a, order, key);
     s.key = key; s.order = order;
-    s.chunk = chunk_of(a.T);
+    s.chunk = chunk_of(a.T, a.H);
     s.chunks = ceil_div(a.T, s.chunk);
     s.part = (float *)at;
     s.fill_rows = 16;

@@ -117,9 +117,10 @@ struct CrossArgs {
     const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
     int chunk;                      // keys of a workgroup; 0: all of its run's
     float *part; float2 *part_ml;   // partial results of the chunks
-    // dK and dV: see cross_plan_kernel
-    const int *nb, *ne, *first_step, *cuts, *first_tile;
-    const int4 *steps;
+    // dK and dV: see make_plan
+    int4 *tiles, *steps;
+    int n_tiles, n_steps;           // n_tiles 0: not wanted
+    int *plan;                      // scratch for many runs
     int parts;                      // workgroups that share the rows which see a tile of keys
     float *dkv_part;                // [parts][Tk][2 nkv d], where there are several
 };

@@ -15,6 +15,7 @@ struct QkShape {
     int lanes;                  // threads a head
     int units, rot_units, copy_chunks;      // chunk pairs of a head: first the rotated ones, then those that pass through
     int tile;                   // tokens whose rotations are in LDS at a time
+    int step_tokens, step_heads;// heads that a workgroup has at work at once: step_tokens * heads + step_heads
 };
 
 template <int V>
@@ -31,8 +32,15 @@ struct Place {                  // a thread's two chunks of a head
     }
 };
 
+// Sum over the head's lanes, the same in all of them; up to 16 lanes are added with DPP moves, which stay in the vector ALU
+template <int CTRL> __device__ __forceinline__ float add_dpp(float v) { return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)); }
 __device__ __forceinline__ float head_sum(float v, int lanes) {
-    for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o, 64);
+    if (lanes > 1) v = add_dpp<0xb1>(v);            // quad_perm 1 0 3 2
+    if (lanes > 2) v = add_dpp<0x4e>(v);            // quad_perm 2 3 0 1
+    if (lanes > 4) v = add_dpp<0x141>(v);           // row_half_mirror
+    if (lanes > 8) v = add_dpp<0x140>(v);           // row_mirror
+    if (lanes > 16) v += __shfl_xor(v, 16, 64);
+    if (lanes > 32) v += __shfl_xor(v, 32, 64);
     return v;
 }
 
@@ -68,15 +76,25 @@ __device__ __forceinline__ void rotate(float (&lo)[V], float (&hi)[V], const flo
 }
 
 template <typename T, int V>
-__device__ __forceinline__ void load_pair(const T *x, const Place<V> &p, float (&lo)[V], float (&hi)[V]) {
+struct Pair {                   // a thread's chunks as loaded
     Chunk<T, V> c0, c1;
-    if (p.first) c0.load(x + p.o0);
-    if (p.second) c1.load(x + p.o1);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        lo[i] = p.first ? c0.get(i) : 0.f;
-        hi[i] = p.second ? c1.get(i) : 0.f;
+    __device__ __forceinline__ void load(const T *x, const Place<V> &p) {
+        if (p.first) c0.load(x + p.o0);
+        if (p.second) c1.load(x + p.o1);
     }
+    __device__ __forceinline__ void get(const Place<V> &p, float (&lo)[V], float (&hi)[V]) const {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            lo[i] = p.first ? c0.get(i) : 0.f;
+            hi[i] = p.second ? c1.get(i) : 0.f;
+        }
+    }
+};
+template <typename T, int V>
+__device__ __forceinline__ void load_pair(const T *x, const Place<V> &p, float (&lo)[V], float (&hi)[V]) {
+    Pair<T, V> c;
+    c.load(x, p);
+    c.get(p, lo, hi);
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_pair(T *y, const Place<V> &p, const float (&lo)[V], const float (&hi)[V]) {
@@ -110,37 +128,69 @@ __device__ __forceinline__ float normalise(float (&lo)[V], float (&hi)[V], const
     return rstd;
 }
 
+// gains (and biases) of both kinds in LDS, [2][d] each
+template <typename T, bool LAYER>
+__device__ __forceinline__ void put_gains(const QkNormArgs &a, float *gains) {
+    const int d = a.r.d;
+    for (int i = threadIdx.x; i < (LAYER ? 4 : 2) * d; i += 256) {
+        const int k = i / d;
+        const void *p = k == 0 ? a.q_w : k == 1 ? a.k_w : k == 2 ? a.q_b : a.k_b;
+        gains[i] = p ? Elem<T>::load((const T *)p + i % d) : 0.f;
+    }
+}
+template <int V>
+__device__ __forceinline__ void get_gains(const float *g, const Place<V> &p, float (&lo)[V], float (&hi)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) { lo[i] = 0.f; hi[i] = 0.f; }
+    if (p.first) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) lo[i] = g[p.o0 + i];
+    }
+    if (p.second) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) hi[i] = g[p.o1 + i];
+    }
+}
+
+// The first heads' rows are requested in front of everything else, and the next ones' in front of each turn's arithmetic.
 template <typename T, int V, bool INTERLEAVED, bool LAYER>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a, QkShape s) {
     extern __shared__ float2 turned[];
     const RopeArgs &r = a.r;
+    float *const gains = (float *)(turned + s.tile * r.half);
     const long first = (blockIdx.y * (long)gridDim.x + blockIdx.x) * s.tile;
     if (first >= r.T) return;
     const int t0 = (int)first, tokens = min(s.tile, r.T - t0);
-    const int u = threadIdx.x & (s.lanes - 1), g = threadIdx.x / s.lanes, groups = 256 / s.lanes;
+    const int u = threadIdx.x & (s.lanes - 1), g = threadIdx.x / s.lanes;
     const Place<V> p(s, r.half, u);
     const float inv_d = 1.f / r.d;
+    int tok = g / r.heads, head = g % r.heads;
+    Pair<T, V> next;
+    auto request = [&] { next.load((const T *)r.x + (t0 + tok) * r.ldx + (long)head * r.d, p); };
+    if (tok < tokens) request();
+    put_gains<T, LAYER>(a, gains);
     put_rotations(r, turned, t0, tokens);
     __syncthreads();
-    for (int kind = 0; kind < 2; ++kind) {
-        const int h0 = kind ? a.nq : 0, heads = kind ? r.heads - a.nq : a.nq;
-        if (!heads) continue;
-        float w0[V], w1[V], b0[V], b1[V];
-        load_pair((const T *)(kind ? a.k_w : a.q_w), p, w0, w1);
-        if constexpr (LAYER) load_pair((const T *)(kind ? a.k_b : a.q_b), p, b0, b1);
-        for (int i = g; i < tokens * heads; i += groups) {
-            const int tok = i / heads, head = h0 + i % heads;
-            float lo[V], hi[V];
-            load_pair((const T *)r.x + (t0 + tok) * r.ldx + (long)head * r.d, p, lo, hi);
-            normalise<V, LAYER>(lo, hi, p, s.lanes, inv_d, a.eps);
+    while (tok < tokens) {
+        T *const y = (T *)r.y + (t0 + tok) * r.ldy + (long)head * r.d;
+        const float2 *cs = turned + tok * r.half;
+        const float *w = gains + (head < a.nq ? 0 : r.d);
+        float lo[V], hi[V], w0[V], w1[V], b0[V], b1[V];
+        const Pair<T, V> now = next;
+        tok += s.step_tokens; head += s.step_heads;
+        if (head >= r.heads) { head -= r.heads; ++tok; }
+        if (tok < tokens) request();
+        now.get(p, lo, hi);
+        normalise<V, LAYER>(lo, hi, p, s.lanes, inv_d, a.eps);
+        get_gains(w, p, w0, w1);
+        if constexpr (LAYER) get_gains(w + 2 * r.d, p, b0, b1);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                lo[e] = LAYER ? lo[e] * w0[e] + b0[e] : lo[e] * w0[e];
-                hi[e] = LAYER ? hi[e] * w1[e] + b1[e] : hi[e] * w1[e];
-            }
-            if (p.rotates) rotate<V, INTERLEAVED>(lo, hi, turned + tok * r.half, p, u);
-            store_pair((T *)r.y + (t0 + tok) * r.ldy + (long)head * r.d, p, lo, hi);
+        for (int e = 0; e < V; ++e) {
+            lo[e] = LAYER ? lo[e] * w0[e] + b0[e] : lo[e] * w0[e];
+            hi[e] = LAYER ? hi[e] * w1[e] + b1[e] : hi[e] * w1[e];
         }
+        if (p.rotates) rotate<V, INTERLEAVED>(lo, hi, cs, p, u);
+        store_pair(y, p, lo, hi);
     }
 }
 
@@ -155,22 +205,34 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, QkShape 
     for (int kind = 0; kind < 2; ++kind) {
         const int h0 = kind ? a.nq : 0, heads = kind ? r.heads - a.nq : a.nq;
         if (!heads) continue;
+        const int step_tokens = groups / heads, step_heads = groups % heads;
         float w0[V], w1[V], gw0[V], gw1[V], gb0[V], gb1[V];
         load_pair((const T *)(kind ? a.k_w : a.q_w), p, w0, w1);
 #pragma unroll
         for (int e = 0; e < V; ++e) gw0[e] = gw1[e] = gb0[e] = gb1[e] = 0.f;
         for (long first = (long)blockIdx.x * s.tile; first < r.T; first += (long)gridDim.x * s.tile) {
             const int t0 = (int)first, tokens = min(s.tile, r.T - t0);
-            __syncthreads();
+            int tok = g / heads, head = g % heads;
+            Pair<T, V> next_x, next_d;
+            auto request = [&] {
+                next_x.load((const T *)r.x + (t0 + tok) * r.ldx + (long)(h0 + head) * r.d, p);
+                next_d.load((const T *)a.dy + (t0 + tok) * a.lddy + (long)(h0 + head) * r.d, p);
+            };
+            if (tok < tokens) request();
+            __syncthreads();                                 // the last tile's rotations are done with
             put_rotations(r, turned, t0, tokens);
             __syncthreads();
-            for (int i = g; i < tokens * heads; i += groups) {
-                const int tok = i / heads, head = h0 + i % heads;
+            while (tok < tokens) {
                 float lo[V], hi[V], d0[V], d1[V];
-                load_pair((const T *)r.x + (t0 + tok) * r.ldx + (long)head * r.d, p, lo, hi);
-                load_pair((const T *)a.dy + (t0 + tok) * a.lddy + (long)head * r.d, p, d0, d1);
+                next_x.get(p, lo, hi);
+                next_d.get(p, d0, d1);
+                const float2 *cs = turned + tok * r.half;
+                T *const out = (T *)r.y + (t0 + tok) * r.ldy + (long)(h0 + head) * r.d;
+                tok += step_tokens; head += step_heads;
+                if (head >= heads) { head -= heads; ++tok; }
+                if (tok < tokens) request();
                 const float rstd = normalise<V, LAYER>(lo, hi, p, s.lanes, inv_d, a.eps);
-                if (p.rotates) rotate<V, INTERLEAVED>(d0, d1, turned + tok * r.half, p, u);
+                if (p.rotates) rotate<V, INTERLEAVED>(d0, d1, cs, p, u);
                 float dot = 0.f, mean = 0.f;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
@@ -187,7 +249,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, QkShape 
                     d0[e] = rstd * (d0[e] - mean - lo[e] * dot);
                     d1[e] = rstd * (d1[e] - mean - hi[e] * dot);
                 }
-                if (r.y) store_pair((T *)r.y + (t0 + tok) * r.ldy + (long)head * r.d, p, d0, d1);
+                if (r.y) store_pair(out, p, d0, d1);
             }
         }
         for (int k = 0; k < (LAYER ? 2 : 1); ++k) {
@@ -216,6 +278,8 @@ template <int V> QkShape shape_of(const QkNormArgs &a) {
     s.units = s.rot_units + (s.copy_chunks + 1) / 2;         // at most 64
     s.lanes = 1;
     while (s.lanes < s.units) s.lanes *= 2;
+    s.step_tokens = 256 / s.lanes / a.r.heads;
+    s.step_heads = 256 / s.lanes % a.r.heads;
     return s;
 }
 
@@ -237,7 +301,7 @@ hipError_t launch(const QkNormArgs &a, bool back, hipStream_t st) {
     }
     const int by_units = (511 + a.r.heads * s.lanes) / (a.r.heads * s.lanes);
     s.tile = std::max(1, std::min({by_units, by_angles, a.r.T / 512}));
-    const size_t lds = (size_t)s.tile * a.r.half * sizeof(float2);
+    const size_t lds = (size_t)s.tile * a.r.half * sizeof(float2) + (layer ? 4 : 2) * a.r.d * sizeof(float);
     const int blocks = ceil_div(a.r.T, s.tile);
     const dim3 grid(std::min(blocks, 1 << 20), ceil_div(blocks, 1 << 20));
     if (a.r.interleaved) {
@@ -259,7 +323,7 @@ hipError_t dispatch(int dtype, const QkNormArgs &a, bool back, hipStream_t st) {
 
 hipError_t qk_norm_fwd(int dtype, const QkNormArgs &a, hipStream_t st) { return a.r.T == 0 ? hipSuccess : dispatch(dtype, a, false, st); }
 
-int qk_norm_bwd_blocks(int T) { return std::max(1, std::min(T, 1024)); }
+int qk_norm_bwd_blocks(int T) { return std::max(1, std::min(T, 512)); }
 
 hipError_t qk_norm_bwd(int dtype, const QkNormArgs &a, hipStream_t st) {
     if (a.r.T > 0) {
