@@ -93,7 +93,7 @@ int mmtrain_cross_attn_fwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
     const CrossShape c = shape_of(*desc, *batch);
     const CrossPlan plan = cross_fwd_plan(desc->dtype, c);
     if (!workspace || workspace_bytes < cross_fwd_bytes(c, plan) + 256) return MMTRAIN_ERR_WORKSPACE;
-    HIP_TRY(cross_fwd(desc->dtype, a, plan, workspace, (hipStream_t)hip_stream));
+    HIP_TRY(cross_fwd(desc->dtype, a, c, plan, workspace, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 
@@ -122,7 +122,7 @@ int mmtrain_cross_attn_bwd(const mmtrain_cross_attn_desc *desc, const mmtrain_cr
     if (!workspace || workspace_bytes < cross_bwd_bytes(c, plan) + 256) return MMTRAIN_ERR_WORKSPACE;
     a.d_o = g.d_o; a.lddo = g.ld_do;
     a.dq = g.d_q; a.lddq = g.ld_dq; a.dk = g.d_k; a.lddk = g.ld_dk; a.dv = g.d_v; a.lddv = g.ld_dv;
-    HIP_TRY(cross_bwd(desc->dtype, a, plan, workspace, (hipStream_t)hip_stream));
+    HIP_TRY(cross_bwd(desc->dtype, a, c, plan, workspace, (hipStream_t)hip_stream));
     return MMTRAIN_OK;
 }
 

@@ -103,7 +103,7 @@ int qk_norm_common(const mmtrain_qk_norm_desc *d, const mmtrain_rope_desc *rope,
     return MMTRAIN_OK;
 }
 
-size_t qk_norm_part_bytes(const mmtrain_qk_norm_desc &d, int32_t T) { return ((size_t)qk_norm_bwd_blocks(T) * d.head_dim * sizeof(float) + 255) & ~size_t(255); }
+size_t qk_norm_part_bytes(const mmtrain_qk_norm_desc &d, int32_t T) { return ((size_t)qk_norm_bwd_blocks(T, d.norm) * d.head_dim * sizeof(float) + 255) & ~size_t(255); }
 
 // ---- embedding ---------------------------------------------------------------------------------
 int check_embed(const mmtrain_embed_desc *d) {

@@ -38,6 +38,12 @@ __global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int til
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
 size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
 
+void order_runs(const CrossShape &c, CrossArgs &a) {
+    const int n = c.S <= 64 ? c.S : 0;
+    for (int s = 0; s < 64; ++s) a.order[s] = (uint8_t)s;
+    std::stable_sort(a.order, a.order + n, [&](uint8_t x, uint8_t y) { return c.end[x] - c.begin[x] > c.end[y] - c.begin[y]; });
+}
+
 }  // namespace
 
 // How a forward pass is cut: by the rows of the runs and the keys they see
@@ -76,8 +82,9 @@ size_t cross_fwd_bytes(const CrossShape &c, const CrossPlan &p) {
     return (p.table ? table_bytes(c.S) : 0) + (p.chunk ? (size_t)p.items * c.nkv * p.rows * (c.d * sizeof(float) + sizeof(float2)) : 0);
 }
 
-hipError_t cross_fwd(int dtype, const CrossArgs &args, const CrossPlan &p, void *ws, hipStream_t st) {
+hipError_t cross_fwd(int dtype, const CrossArgs &args, const CrossShape &c, const CrossPlan &p, void *ws, hipStream_t st) {
     CrossArgs a = args;
+    order_runs(c, a);
     uint8_t *at = (uint8_t *)ws;
     if (p.table) {
         a.prefix = (int *)at;
@@ -135,8 +142,9 @@ size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p) {
     return n;
 }
 
-hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossBwdPlan &p, void *ws, hipStream_t st) {
+hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossShape &c, const CrossBwdPlan &p, void *ws, hipStream_t st) {
     CrossArgs a = args;
+    order_runs(c, a);
     uint8_t *at = (uint8_t *)ws;
     auto take = [&](size_t n) { void *q = at; at += n; return q; };
     a.D = (float *)take(aligned((size_t)a.Tq * a.nh * sizeof(float)));

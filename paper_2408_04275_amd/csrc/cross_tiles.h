@@ -40,14 +40,19 @@ struct Item {
     int index, first;           // the item's number within its run; of the run's first item among all
 };
 
-// Item y of all runs' items.  Up to 64 runs: one per lane, their items added up across the wavefront; more: from the table that
-// cross_prefix_kernel left.
+// Item y of all runs' items.  Up to 64 runs: one per lane, those with the most keys first (the workgroups that start last are then the
+// shortest), their items added up across the wavefront; more: from the table that cross_prefix_kernel left.
 __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_rows, int chunk) {
     const int group = a.nh / a.nkv, lane = threadIdx.x & 63;
     Item it;
     if (a.S <= 64) {
         int c0 = 0, c1 = 0, lo = 0, hi = 0;
+        const int from = a.order[lane] * 4;                  // the lane's place, from the run of that number
         if (lane < a.S) { c0 = a.cu[lane]; c1 = a.cu[lane + 1]; lo = a.begin[lane]; hi = a.end[lane]; }
+        c0 = __builtin_amdgcn_ds_bpermute(from, c0);
+        c1 = __builtin_amdgcn_ds_bpermute(from, c1);
+        lo = __builtin_amdgcn_ds_bpermute(from, lo);
+        hi = __builtin_amdgcn_ds_bpermute(from, hi);
         const int n = lane < a.S ? items_of(c1 - c0, hi - lo, group, tile_rows, chunk) : 0;
         const int sum = wave_scan(n);
         const int s = min(__popcll(__builtin_amdgcn_ballot_w64(sum <= y)), 63);

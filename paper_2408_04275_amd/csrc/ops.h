@@ -78,7 +78,7 @@ struct QkNormArgs {
 };
 constexpr int QK_MAX_ROWS = 1 << 30;
 hipError_t qk_norm_fwd(int dtype, const QkNormArgs &a, hipStream_t st);
-int qk_norm_bwd_blocks(int T);      // never fewer for more rows
+int qk_norm_bwd_blocks(int T, int norm);        // never fewer for more rows
 hipError_t qk_norm_bwd(int dtype, const QkNormArgs &a, hipStream_t st);
 
 // embed.hip
@@ -114,6 +114,7 @@ struct CrossArgs {
     void *dk; long lddk;
     void *dv; long lddv;
     float *D;                       // backward scratch [nh, Tq]: rowsum(dO * O)
+    uint8_t order[64];              // runs by falling number of keys, where there are at most 64
     const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
     int chunk;                      // keys of a workgroup; 0: all of its run's
     float *part; float2 *part_ml;   // partial results of the chunks
@@ -138,10 +139,10 @@ struct CrossBwdPlan {
 // Plans, workspaces (256-byte aligned) and calls.  dkv: the gradients of keys and values are wanted
 CrossPlan cross_fwd_plan(int dtype, const CrossShape &c);
 size_t cross_fwd_bytes(const CrossShape &c, const CrossPlan &p);
-hipError_t cross_fwd(int dtype, const CrossArgs &a, const CrossPlan &p, void *ws, hipStream_t st);
+hipError_t cross_fwd(int dtype, const CrossArgs &a, const CrossShape &c, const CrossPlan &p, void *ws, hipStream_t st);
 CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv);
 size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p);
-hipError_t cross_bwd(int dtype, const CrossArgs &a, const CrossBwdPlan &p, void *ws, hipStream_t st);
+hipError_t cross_bwd(int dtype, const CrossArgs &a, const CrossShape &c, const CrossBwdPlan &p, void *ws, hipStream_t st);
 // bf16 on the matrix cores; fp32 on the fp32 matrix instruction
 hipError_t cross_mfma_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st);
 hipError_t cross_mfma_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st);

@@ -15,26 +15,30 @@ struct QkShape {
     int lanes;                  // threads a head
     int units, rot_units, copy_chunks;      // chunk pairs of a head: first the rotated ones, then those that pass through
     int tile;                   // tokens whose rotations are in LDS at a time
-    int step_tokens, step_heads;// heads that a workgroup has at work at once: step_tokens * heads + step_heads
+    int q_blocks;               // backward: workgroups of the query heads
 };
 
-template <int V>
-struct Place {                  // a thread's two chunks of a head
+// Where a thread's two chunks of a head stand.  LANES: threads a head, where each of them has two chunks (4, 8 or 16); 0: any shape, and chunks that a
+// thread does not have are those of unit 0, loaded to no purpose.
+template <int V, int LANES>
+struct Place {
     int o0, o1;
     bool rotates, first, second;
     __device__ __forceinline__ Place(const QkShape &s, int half, int u) {
         rotates = u < s.rot_units;
-        first = u < s.units;
         const int copy = u - s.rot_units, copy_units = s.units - s.rot_units;
-        o0 = rotates ? u * V : 2 * half + copy * V;
-        o1 = rotates ? o0 + half : o0 + copy_units * V;
-        second = rotates || (first && copy + copy_units < s.copy_chunks);
+        first = LANES > 0 || u < s.units;
+        second = LANES > 0 || rotates || (first && copy + copy_units < s.copy_chunks);
+        o0 = !first ? 0 : rotates ? u * V : 2 * half + copy * V;
+        o1 = !second ? 0 : rotates ? o0 + half : o0 + copy_units * V;
     }
 };
 
 // Sum over the head's lanes, the same in all of them; up to 16 lanes are added with DPP moves, which stay in the vector ALU
 template <int CTRL> __device__ __forceinline__ float add_dpp(float v) { return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)); }
+template <int LANES>
 __device__ __forceinline__ float head_sum(float v, int lanes) {
+    if constexpr (LANES > 0) lanes = LANES;
     if (lanes > 1) v = add_dpp<0xb1>(v);            // quad_perm 1 0 3 2
     if (lanes > 2) v = add_dpp<0x4e>(v);            // quad_perm 2 3 0 1
     if (lanes > 4) v = add_dpp<0x141>(v);           // row_half_mirror
@@ -45,10 +49,12 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 }
 
 // the rotations of tokens t0 .. t0 + tokens - 1, [tokens][half] (cosine, sine)
-__device__ __forceinline__ void put_rotations(const RopeArgs &a, float2 *turned, int t0, int tokens) {
-    for (int k = threadIdx.x; k < tokens * a.half; k += 256) {
-        const int t = t0 + k / a.half;
-        const int pos = a.positions ? a.positions[t] : t - a.cu[find_segment(a.cu, a.S, t)];
+__device__ __forceinline__ int position_of(const RopeArgs &a, int t) { return a.positions ? a.positions[t] : t - a.cu[find_segment(a.cu, a.S, t)]; }
+// pos: their positions in LDS (null: each thread looks for its own)
+template <int THREADS>
+__device__ __forceinline__ void put_rotations(const RopeArgs &a, float2 *turned, int t0, int tokens, const int *pos_in_lds) {
+    for (int k = threadIdx.x; k < tokens * a.half; k += THREADS) {
+        const int pos = pos_in_lds ? pos_in_lds[k / a.half] : position_of(a, t0 + k / a.half);
         const double turn = pos * a.turns[k % a.half];
         float si, co;
         sincospif(2.f * (float)(turn - rint(turn)), &si, &co);
@@ -56,8 +62,9 @@ __device__ __forceinline__ void put_rotations(const RopeArgs &a, float2 *turned,
     }
 }
 
-template <int V, bool INTERLEAVED>
-__device__ __forceinline__ void rotate(float (&lo)[V], float (&hi)[V], const float2 *cs, const Place<V> &p, int u) {
+template <int V, bool INTERLEAVED, int LANES>
+__device__ __forceinline__ void rotate(float (&lo)[V], float (&hi)[V], const float2 *cs, const Place<V, LANES> &p, int u) {
+    if (!p.rotates) return;
     auto turn = [](float &x, float &y, float2 r) {
         const float v = x;
         x = v * r.x - y * r.y;
@@ -75,14 +82,14 @@ __device__ __forceinline__ void rotate(float (&lo)[V], float (&hi)[V], const flo
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, int LANES>
 struct Pair {                   // a thread's chunks as loaded
     Chunk<T, V> c0, c1;
-    __device__ __forceinline__ void load(const T *x, const Place<V> &p) {
-        if (p.first) c0.load(x + p.o0);
-        if (p.second) c1.load(x + p.o1);
+    __device__ __forceinline__ void load(const T *x, const Place<V, LANES> &p) {
+        c0.load(x + p.o0);
+        c1.load(x + p.o1);
     }
-    __device__ __forceinline__ void get(const Place<V> &p, float (&lo)[V], float (&hi)[V]) const {
+    __device__ __forceinline__ void get(const Place<V, LANES> &p, float (&lo)[V], float (&hi)[V]) const {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             lo[i] = p.first ? c0.get(i) : 0.f;
@@ -90,14 +97,8 @@ struct Pair {                   // a thread's chunks as loaded
         }
     }
 };
-template <typename T, int V>
-__device__ __forceinline__ void load_pair(const T *x, const Place<V> &p, float (&lo)[V], float (&hi)[V]) {
-    Pair<T, V> c;
-    c.load(x, p);
-    c.get(p, lo, hi);
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_pair(T *y, const Place<V> &p, const float (&lo)[V], const float (&hi)[V]) {
+template <typename T, int V, int LANES>
+__device__ __forceinline__ void store_pair(T *y, const Place<V, LANES> &p, const float (&lo)[V], const float (&hi)[V]) {
     Chunk<T, V> c0, c1;
     c0.set(lo);
     c1.set(hi);
@@ -106,13 +107,13 @@ __device__ __forceinline__ void store_pair(T *y, const Place<V> &p, const float 
 }
 
 // v -> (v - mean) rstd; returns rstd.  Chunks that a thread does not have are zero before and after.
-template <int V, bool LAYER>
-__device__ __forceinline__ float normalise(float (&lo)[V], float (&hi)[V], const Place<V> &p, int lanes, float inv_d, float eps) {
+template <int V, bool LAYER, int LANES>
+__device__ __forceinline__ float normalise(float (&lo)[V], float (&hi)[V], const Place<V, LANES> &p, int lanes, float inv_d, float eps) {
     if constexpr (LAYER) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) s += lo[i] + hi[i];
-        const float mean = head_sum(s, lanes) * inv_d;
+        const float mean = head_sum<LANES>(s, lanes) * inv_d;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             lo[i] = p.first ? lo[i] - mean : 0.f;
@@ -122,7 +123,7 @@ __device__ __forceinline__ float normalise(float (&lo)[V], float (&hi)[V], const
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) s += lo[i] * lo[i] + hi[i] * hi[i];
-    const float rstd = 1.f / sqrtf(head_sum(s, lanes) * inv_d + eps);
+    const float rstd = 1.f / sqrtf(head_sum<LANES>(s, lanes) * inv_d + eps);
 #pragma unroll
     for (int i = 0; i < V; ++i) { lo[i] *= rstd; hi[i] *= rstd; }
     return rstd;
@@ -138,137 +139,181 @@ __device__ __forceinline__ void put_gains(const QkNormArgs &a, float *gains) {
         gains[i] = p ? Elem<T>::load((const T *)p + i % d) : 0.f;
     }
 }
-template <int V>
-__device__ __forceinline__ void get_gains(const float *g, const Place<V> &p, float (&lo)[V], float (&hi)[V]) {
+template <int V, int LANES>
+__device__ __forceinline__ void get_gains(const float *g, const Place<V, LANES> &p, float (&lo)[V], float (&hi)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) { lo[i] = 0.f; hi[i] = 0.f; }
-    if (p.first) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) lo[i] = g[p.o0 + i];
-    }
-    if (p.second) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) hi[i] = g[p.o1 + i];
-    }
+    for (int i = 0; i < V; ++i) { lo[i] = g[p.o0 + i]; hi[i] = g[p.o1 + i]; }
 }
 
-// The first heads' rows are requested in front of everything else, and the next ones' in front of each turn's arithmetic.
-template <typename T, int V, bool INTERLEAVED, bool LAYER>
+// The (token, head) pairs of a tile that a group of threads has, one after the other; behind the last it stays at a pair that exists, so that
+// a load ahead needs no branch (with one the compiler waits for all loads on their way in each turn).
+struct Walk {
+    int tok, head, tokens, heads, step_tokens, step_heads;
+    __device__ __forceinline__ Walk(int g, int groups, int tokens_, int heads_)
+        : tok(g / heads_), head(g % heads_), tokens(tokens_), heads(heads_), step_tokens(groups / heads_), step_heads(groups % heads_) {}
+    __device__ __forceinline__ bool live() const { return tok < tokens; }
+    __device__ __forceinline__ void next() {
+        tok += step_tokens; head += step_heads;
+        if (head >= heads) { head -= heads; ++tok; }
+    }
+    __device__ __forceinline__ long row() const { return min(tok, tokens - 1); }
+};
+
+// The first heads' rows are requested in front of everything else, and the next ones' in front of each turn's arithmetic, into the other of
+// two sets of registers.
+template <typename T, int V, bool INTERLEAVED, bool LAYER, int LANES>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a, QkShape s) {
     extern __shared__ float2 turned[];
     const RopeArgs &r = a.r;
     float *const gains = (float *)(turned + s.tile * r.half);
     const long first = (blockIdx.y * (long)gridDim.x + blockIdx.x) * s.tile;
     if (first >= r.T) return;
-    const int t0 = (int)first, tokens = min(s.tile, r.T - t0);
-    const int u = threadIdx.x & (s.lanes - 1), g = threadIdx.x / s.lanes;
-    const Place<V> p(s, r.half, u);
+    const int t0 = (int)first, tokens = min(s.tile, r.T - t0), lanes = LANES > 0 ? LANES : s.lanes;
+    const int u = threadIdx.x & (lanes - 1);
+    const Place<V, LANES> p(s, r.half, u);
     const float inv_d = 1.f / r.d;
-    int tok = g / r.heads, head = g % r.heads;
-    Pair<T, V> next;
-    auto request = [&] { next.load((const T *)r.x + (t0 + tok) * r.ldx + (long)head * r.d, p); };
-    if (tok < tokens) request();
-    put_gains<T, LAYER>(a, gains);
-    put_rotations(r, turned, t0, tokens);
-    __syncthreads();
-    while (tok < tokens) {
-        T *const y = (T *)r.y + (t0 + tok) * r.ldy + (long)head * r.d;
-        const float2 *cs = turned + tok * r.half;
-        const float *w = gains + (head < a.nq ? 0 : r.d);
+    Walk w(threadIdx.x / lanes, 256 / lanes, tokens, r.heads);
+    auto request = [&](Pair<T, V, LANES> &to) { to.load((const T *)r.x + (t0 + w.row()) * r.ldx + (long)w.head * r.d, p); };
+    auto turn = [&](const Pair<T, V, LANES> &now, Pair<T, V, LANES> &next) {
+        T *const y = (T *)r.y + (t0 + w.tok) * r.ldy + (long)w.head * r.d;
+        const float2 *cs = turned + w.tok * r.half;
+        const float *gain = gains + (w.head < a.nq ? 0 : r.d);
+        w.next();
+        request(next);
         float lo[V], hi[V], w0[V], w1[V], b0[V], b1[V];
-        const Pair<T, V> now = next;
-        tok += s.step_tokens; head += s.step_heads;
-        if (head >= r.heads) { head -= r.heads; ++tok; }
-        if (tok < tokens) request();
         now.get(p, lo, hi);
-        normalise<V, LAYER>(lo, hi, p, s.lanes, inv_d, a.eps);
-        get_gains(w, p, w0, w1);
-        if constexpr (LAYER) get_gains(w + 2 * r.d, p, b0, b1);
+        normalise<V, LAYER>(lo, hi, p, lanes, inv_d, a.eps);
+        get_gains(gain, p, w0, w1);
+        if constexpr (LAYER) get_gains(gain + 2 * r.d, p, b0, b1);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             lo[e] = LAYER ? lo[e] * w0[e] + b0[e] : lo[e] * w0[e];
             hi[e] = LAYER ? hi[e] * w1[e] + b1[e] : hi[e] * w1[e];
         }
-        if (p.rotates) rotate<V, INTERLEAVED>(lo, hi, cs, p, u);
+        rotate<V, INTERLEAVED>(lo, hi, cs, p, u);
         store_pair(y, p, lo, hi);
+    };
+    Pair<T, V, LANES> even, odd;
+    request(even);
+    put_gains<T, LAYER>(a, gains);
+    put_rotations<256>(r, turned, t0, tokens, nullptr);
+    __syncthreads();
+    while (w.live()) {
+        turn(even, odd);
+        if (!w.live()) break;
+        turn(odd, even);
     }
 }
 
-template <typename T, int V, bool INTERLEAVED, bool LAYER>
-__global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, QkShape s) {
+// A workgroup has heads of one kind, of every so many tiles of tokens: query heads the first s.q_blocks, key heads the others.  Sixteen wavefronts a
+// compute unit, in two workgroups of 512 threads: smaller ones would leave more partial rows, whose sum is a launch of its own.  The LayerNorm needs more than the
+// 128 registers that leaves (8192 tokens of 72 heads: 163 us with 28 of them in memory): twelve wavefronts in three workgroups.
+template <bool LAYER> constexpr int BWD_THREADS = LAYER ? 256 : 512;
+template <bool LAYER> constexpr int BWD_BLOCKS = LAYER ? 768 : 512;
+constexpr int BWD_TILE = 64;
+template <typename T, int V, bool INTERLEAVED, bool LAYER, int LANES>
+__global__ __launch_bounds__(BWD_THREADS<LAYER>, LAYER ? 3 : 4) void qk_norm_bwd_kernel(QkNormArgs a, QkShape s) {
     extern __shared__ float2 turned[];
+    constexpr int THREADS = BWD_THREADS<LAYER>;
     const RopeArgs &r = a.r;
-    const int u = threadIdx.x & (s.lanes - 1), g = threadIdx.x / s.lanes, groups = 256 / s.lanes;
-    const Place<V> p(s, r.half, u);
+    const int lanes = LANES > 0 ? LANES : s.lanes;
+    const int u = threadIdx.x & (lanes - 1), g = threadIdx.x / lanes, groups = THREADS / lanes;
+    const Place<V, LANES> p(s, r.half, u);
     const float inv_d = 1.f / r.d;
-    float *const sums = (float *)turned;                     // [groups][d], when the rotations are done with
-    for (int kind = 0; kind < 2; ++kind) {
-        const int h0 = kind ? a.nq : 0, heads = kind ? r.heads - a.nq : a.nq;
-        if (!heads) continue;
-        const int step_tokens = groups / heads, step_heads = groups % heads;
-        float w0[V], w1[V], gw0[V], gw1[V], gb0[V], gb1[V];
-        load_pair((const T *)(kind ? a.k_w : a.q_w), p, w0, w1);
+    float *const sums = (float *)(turned + s.tile * r.half);  // [wavefronts][d]
+    __shared__ int positions[BWD_TILE];
+    const int kind = (int)blockIdx.x >= s.q_blocks, block = kind ? blockIdx.x - s.q_blocks : blockIdx.x, blocks = kind ? gridDim.x - s.q_blocks : s.q_blocks;
+    const int h0 = kind ? a.nq : 0, heads = kind ? r.heads - a.nq : a.nq;
+    Pair<T, V, LANES> gain;
+    gain.load((const T *)(kind ? a.k_w : a.q_w), p);
+    float w0[V], w1[V], gw0[V], gw1[V], gb0[V], gb1[V];
+    gain.get(p, w0, w1);
 #pragma unroll
-        for (int e = 0; e < V; ++e) gw0[e] = gw1[e] = gb0[e] = gb1[e] = 0.f;
-        for (long first = (long)blockIdx.x * s.tile; first < r.T; first += (long)gridDim.x * s.tile) {
-            const int t0 = (int)first, tokens = min(s.tile, r.T - t0);
-            int tok = g / heads, head = g % heads;
-            Pair<T, V> next_x, next_d;
-            auto request = [&] {
-                next_x.load((const T *)r.x + (t0 + tok) * r.ldx + (long)(h0 + head) * r.d, p);
-                next_d.load((const T *)a.dy + (t0 + tok) * a.lddy + (long)(h0 + head) * r.d, p);
-            };
-            if (tok < tokens) request();
-            __syncthreads();                                 // the last tile's rotations are done with
-            put_rotations(r, turned, t0, tokens);
-            __syncthreads();
-            while (tok < tokens) {
-                float lo[V], hi[V], d0[V], d1[V];
-                next_x.get(p, lo, hi);
-                next_d.get(p, d0, d1);
-                const float2 *cs = turned + tok * r.half;
-                T *const out = (T *)r.y + (t0 + tok) * r.ldy + (long)(h0 + head) * r.d;
-                tok += step_tokens; head += step_heads;
-                if (head >= heads) { head -= heads; ++tok; }
-                if (tok < tokens) request();
-                const float rstd = normalise<V, LAYER>(lo, hi, p, s.lanes, inv_d, a.eps);
-                if (p.rotates) rotate<V, INTERLEAVED>(d0, d1, cs, p, u);
-                float dot = 0.f, mean = 0.f;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    gw0[e] += d0[e] * lo[e]; gw1[e] += d1[e] * hi[e];
-                    if constexpr (LAYER) { gb0[e] += d0[e]; gb1[e] += d1[e]; }
-                    d0[e] *= w0[e]; d1[e] *= w1[e];
-                    dot += d0[e] * lo[e] + d1[e] * hi[e];
-                    if constexpr (LAYER) mean += d0[e] + d1[e];
-                }
-                dot = head_sum(dot, s.lanes) * inv_d;
-                if constexpr (LAYER) mean = head_sum(mean, s.lanes) * inv_d;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    d0[e] = rstd * (d0[e] - mean - lo[e] * dot);
-                    d1[e] = rstd * (d1[e] - mean - hi[e] * dot);
-                }
-                if (r.y) store_pair(out, p, d0, d1);
-            }
-        }
-        for (int k = 0; k < (LAYER ? 2 : 1); ++k) {
-            float *out = a.part[2 * kind + k];
-            if (!out) continue;
-            __syncthreads();
+    for (int e = 0; e < V; ++e) gw0[e] = gw1[e] = gb0[e] = gb1[e] = 0.f;
+    for (long first = (long)block * s.tile; first < r.T; first += (long)blocks * s.tile) {
+        const int t0 = (int)first, tokens = min(s.tile, r.T - t0);
+        Walk w(g, groups, tokens, heads);
+        struct Rows { Pair<T, V, LANES> x, d; } even, odd;
+        auto request = [&](Rows &to) {
+            to.x.load((const T *)r.x + (t0 + w.row()) * r.ldx + (long)(h0 + w.head) * r.d, p);
+            to.d.load((const T *)a.dy + (t0 + w.row()) * a.lddy + (long)(h0 + w.head) * r.d, p);
+        };
+        auto turn = [&](const Rows &now, Rows &next) {
+            const float2 *cs = turned + w.tok * r.half;
+            T *const out = (T *)r.y + (t0 + w.tok) * r.ldy + (long)(h0 + w.head) * r.d;
+            w.next();
+            request(next);
+            float lo[V], hi[V], d0[V], d1[V];
+            now.x.get(p, lo, hi);
+            now.d.get(p, d0, d1);
+            const float rstd = normalise<V, LAYER>(lo, hi, p, lanes, inv_d, a.eps);
+            rotate<V, INTERLEAVED>(d0, d1, cs, p, u);
+            float dot = 0.f, mean = 0.f;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                if (p.first) sums[g * r.d + p.o0 + e] = k ? gb0[e] : gw0[e];
-                if (p.second) sums[g * r.d + p.o1 + e] = k ? gb1[e] : gw1[e];
+                gw0[e] += d0[e] * lo[e]; gw1[e] += d1[e] * hi[e];
+                if constexpr (LAYER) { gb0[e] += d0[e]; gb1[e] += d1[e]; }
+                d0[e] *= w0[e]; d1[e] *= w1[e];
+                dot += d0[e] * lo[e] + d1[e] * hi[e];
+                if constexpr (LAYER) mean += d0[e] + d1[e];
             }
-            __syncthreads();
-            for (int f = threadIdx.x; f < r.d; f += 256) {
-                float t = 0.f;
-                for (int j = 0; j < groups; ++j) t += sums[j * r.d + f];
-                out[(size_t)blockIdx.x * r.d + f] = t;
+            dot = head_sum<LANES>(dot, lanes) * inv_d;
+            if constexpr (LAYER) mean = head_sum<LANES>(mean, lanes) * inv_d;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                d0[e] = rstd * (d0[e] - mean - lo[e] * dot);
+                d1[e] = rstd * (d1[e] - mean - hi[e] * dot);
             }
+            if (r.y) store_pair(out, p, d0, d1);
+        };
+        request(even);
+        __syncthreads();                                 // the last tile's rotations are done with
+        if (r.half && (int)threadIdx.x < tokens) positions[threadIdx.x] = position_of(r, t0 + threadIdx.x);
+        __syncthreads();
+        put_rotations<THREADS>(r, turned, t0, tokens, positions);
+        __syncthreads();
+        while (w.live()) {
+            turn(even, odd);
+            if (!w.live()) break;
+            turn(odd, even);
         }
     }
+    // the heads of a wavefront, then the wavefronts
+    auto fold = [&](float (&v)[V]) {
+        for (int o = lanes; o < 64; o *= 2)
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] += __shfl_xor(v[e], o, 64);
+    };
+    for (int k = 0; k < (LAYER ? 2 : 1); ++k) {
+        float *out = a.part[2 * kind + k];
+        if (!out) continue;
+        if (k) { fold(gb0); fold(gb1); }
+        else { fold(gw0); fold(gw1); }
+        __syncthreads();
+        if ((int)(threadIdx.x & 63) < lanes) {
+            float *mine = sums + (threadIdx.x >> 6) * r.d;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (p.first) mine[p.o0 + e] = k ? gb0[e] : gw0[e];
+                if (p.second) mine[p.o1 + e] = k ? gb1[e] : gw1[e];
+            }
+        }
+        __syncthreads();
+        for (int f = threadIdx.x; f < r.d; f += THREADS) {
+            float t = 0.f;
+#pragma unroll
+            for (int j = 0; j < THREADS / 64; ++j) t += sums[j * r.d + f];
+            out[(size_t)block * r.d + f] = t;
+        }
+    }
+}
+
+// workgroups of the backward pass: of the query heads, and of all; work as the heads are
+int bwd_blocks(int T, bool layer) { return (int)std::max(1l, std::min(2l * T, (long)(layer ? BWD_BLOCKS<true> : BWD_BLOCKS<false>))); }
+int bwd_q_blocks(const QkNormArgs &a) {
+    const int all = bwd_blocks(a.r.T, a.norm == NORM_LAYER);
+    if (!a.nq || a.nq == a.r.heads) return a.nq ? all : 0;
+    return std::min(std::max((int)((long)all * a.nq / a.r.heads), 1), all - 1);
 }
 
 template <int V> QkShape shape_of(const QkNormArgs &a) {
@@ -278,38 +323,48 @@ template <int V> QkShape shape_of(const QkNormArgs &a) {
     s.units = s.rot_units + (s.copy_chunks + 1) / 2;         // at most 64
     s.lanes = 1;
     while (s.lanes < s.units) s.lanes *= 2;
-    s.step_tokens = 256 / s.lanes / a.r.heads;
-    s.step_heads = 256 / s.lanes % a.r.heads;
     return s;
+}
+
+template <typename T, int V, bool INTERLEAVED, bool LAYER, int LANES>
+hipError_t launch(const QkNormArgs &a, QkShape s, bool back, hipStream_t st) {
+    const int by_angles = a.r.half ? 1024 / a.r.half : 1024;
+    if (back) {
+        const int all = bwd_blocks(a.r.T, LAYER);
+        s.q_blocks = bwd_q_blocks(a);
+        s.tile = std::max(1, std::min({2 * by_angles, BWD_TILE, ceil_div(a.r.T, std::max(s.q_blocks, all - s.q_blocks))}));
+        const size_t lds = (size_t)s.tile * a.r.half * sizeof(float2) + (size_t)(BWD_THREADS<LAYER> / 64) * a.r.d * sizeof(float);
+        qk_norm_bwd_kernel<T, V, INTERLEAVED, LAYER, LANES><<<all, BWD_THREADS<LAYER>, lds, st>>>(a, s);
+        return hipGetLastError();
+    }
+    // Four turns a thread: with fewer the load behind the last is felt, with more the workgroups end apart.  us, 1 / 2 / 4 / 8 tokens a workgroup: 16411 tokens of
+    // 72 heads of 128 134 / 125 / 129 / 135, 9536 of 32 of 64 21.3 / 20.0 / 17.7 / 17.0.
+    const int by_units = (1023 + a.r.heads * s.lanes) / (a.r.heads * s.lanes);
+    s.tile = std::max(1, std::min({by_units, by_angles, a.r.T / 512}));
+    const size_t lds = (size_t)s.tile * a.r.half * sizeof(float2) + (LAYER ? 4 : 2) * a.r.d * sizeof(float);
+    const int blocks = ceil_div(a.r.T, s.tile);
+    const dim3 grid(std::min(blocks, 1 << 20), ceil_div(blocks, 1 << 20));
+    qk_norm_fwd_kernel<T, V, INTERLEAVED, LAYER, LANES><<<grid, 256, lds, st>>>(a, s);
+    return hipGetLastError();
+}
+
+template <typename T, int V, bool INTERLEAVED, bool LAYER>
+hipError_t by_lanes(const QkNormArgs &a, bool back, hipStream_t st) {
+    const QkShape s = shape_of<V>(a);
+    if constexpr (V * sizeof(T) == 16)
+        if (s.copy_chunks % 2 == 0 && s.units == s.lanes) {  // heads of 64, 128 or 256, however much of them rotates
+            if (s.lanes == 4) return launch<T, V, INTERLEAVED, LAYER, 4>(a, s, back, st);
+            if (s.lanes == 8) return launch<T, V, INTERLEAVED, LAYER, 8>(a, s, back, st);
+            if (s.lanes == 16) return launch<T, V, INTERLEAVED, LAYER, 16>(a, s, back, st);
+        }
+    return launch<T, V, INTERLEAVED, LAYER, 0>(a, s, back, st);
 }
 
 template <typename T, int V>
 hipError_t launch(const QkNormArgs &a, bool back, hipStream_t st) {
-    QkShape s = shape_of<V>(a);
-    const int by_angles = a.r.half ? 1024 / a.r.half : 1024;
     const bool layer = a.norm == NORM_LAYER;
-    if (back) {
-        s.tile = std::max(1, std::min(by_angles, 16));
-        const size_t lds = std::max((size_t)s.tile * a.r.half * sizeof(float2), (size_t)(256 / s.lanes) * a.r.d * sizeof(float));
-        const int grid = qk_norm_bwd_blocks(a.r.T);
-        if (a.r.interleaved) {
-            if (layer) qk_norm_bwd_kernel<T, V, true, true><<<grid, 256, lds, st>>>(a, s);
-            else qk_norm_bwd_kernel<T, V, true, false><<<grid, 256, lds, st>>>(a, s);
-        } else if (layer) qk_norm_bwd_kernel<T, V, false, true><<<grid, 256, lds, st>>>(a, s);
-        else qk_norm_bwd_kernel<T, V, false, false><<<grid, 256, lds, st>>>(a, s);
-        return hipGetLastError();
-    }
-    const int by_units = (511 + a.r.heads * s.lanes) / (a.r.heads * s.lanes);
-    s.tile = std::max(1, std::min({by_units, by_angles, a.r.T / 512}));
-    const size_t lds = (size_t)s.tile * a.r.half * sizeof(float2) + (layer ? 4 : 2) * a.r.d * sizeof(float);
-    const int blocks = ceil_div(a.r.T, s.tile);
-    const dim3 grid(std::min(blocks, 1 << 20), ceil_div(blocks, 1 << 20));
-    if (a.r.interleaved) {
-        if (layer) qk_norm_fwd_kernel<T, V, true, true><<<grid, 256, lds, st>>>(a, s);
-        else qk_norm_fwd_kernel<T, V, true, false><<<grid, 256, lds, st>>>(a, s);
-    } else if (layer) qk_norm_fwd_kernel<T, V, false, true><<<grid, 256, lds, st>>>(a, s);
-    else qk_norm_fwd_kernel<T, V, false, false><<<grid, 256, lds, st>>>(a, s);
-    return hipGetLastError();
+    if (a.r.interleaved) return layer ? by_lanes<T, V, true, true>(a, back, st) : by_lanes<T, V, true, false>(a, back, st);
+    return layer ? by_lanes<T, V, false, true>(a, back, st) : by_lanes<T, V, false, false>(a, back, st);
 }
 
 hipError_t dispatch(int dtype, const QkNormArgs &a, bool back, hipStream_t st) {
@@ -323,16 +378,16 @@ hipError_t dispatch(int dtype, const QkNormArgs &a, bool back, hipStream_t st) {
 
 hipError_t qk_norm_fwd(int dtype, const QkNormArgs &a, hipStream_t st) { return a.r.T == 0 ? hipSuccess : dispatch(dtype, a, false, st); }
 
-int qk_norm_bwd_blocks(int T) { return std::max(1, std::min(T, 512)); }
+int qk_norm_bwd_blocks(int T, int norm) { return bwd_blocks(T, norm == NORM_LAYER); }
 
 hipError_t qk_norm_bwd(int dtype, const QkNormArgs &a, hipStream_t st) {
     if (a.r.T > 0) {
         const hipError_t e = dispatch(dtype, a, true, st);
         if (e != hipSuccess) return e;
     }
-    const int rows = a.r.T > 0 ? qk_norm_bwd_blocks(a.r.T) : 0;
+    const int q_rows = a.r.T > 0 ? bwd_q_blocks(a) : 0, k_rows = a.r.T > 0 ? bwd_blocks(a.r.T, a.norm == NORM_LAYER) - q_rows : 0;
     ReduceJob jobs[4];
-    for (int i = 0; i < 4; ++i) jobs[i] = {a.part[i], a.part[i] ? a.grad[i] : nullptr, rows, a.r.d};
+    for (int i = 0; i < 4; ++i) jobs[i] = {a.part[i], a.part[i] ? a.grad[i] : nullptr, i < 2 ? q_rows : k_rows, a.r.d};
     return reduce_jobs(a.grad_f32 ? DT_F32 : DT_BF16, jobs, 4, a.accumulate, st);
 }
 
