@@ -315,7 +315,7 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dkv_kernel(CrossArgs a) {
 #pragma unroll
     for (int i = 0; i < KB; ++i) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int i = wave; i < 4 * kt.steps; i += NW) {
-        const Rows step = rows_of(a.steps[kt.step + i / 4]);
+        const Rows step = rows_of(entry_of(a.steps, kt.step + i / 4));
         Rows at;
         const int first = step.j + i % 4 * 16, tok = g.token(first);
         at.t = step.t + tok; at.j = first - tok * g.n; at.left = step.left - i % 4 * 16;

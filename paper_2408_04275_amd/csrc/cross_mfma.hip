@@ -153,11 +153,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
         }
         follow(mx, std::false_type{});
     };
+    const bool live = mine.left > 0;                     // (a wavefront behind a run's last row copies its share, and leaves the units to others)
     auto step = [&](auto SLOT_, int kt) {
         constexpr int slot = decltype(SLOT_)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this step's tiles have landed
         lds_barrier();                                               // ... and everyone is done with the other slot
-        if (kt == kbeg) {
+        if (kt == kbeg && live) {
             f32x16 x = zero16();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) x = MFMA(lds_load<bf16x8>(kadr[ks] + K_FIRST), qf[ks], x);
@@ -165,10 +166,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
             s[0] = x;
             follow(max16(x), std::true_type{});
         }
-        block(SLOT_, std::integral_constant<int, 0>{}, kt + 32);
+        if (live) block(SLOT_, std::integral_constant<int, 0>{}, kt + 32);
         // (behind the first block: right behind the barrier all wavefronts would wait for each other at the copies)
         if (kt + KEYS < kend) copy_kv(smem + (slot ^ 1) * SLOT, kt + KEYS);
-        if (kt + 32 < kend) block(SLOT_, std::integral_constant<int, 1>{}, kt + KEYS);
+        if (kt + 32 < kend && live) block(SLOT_, std::integral_constant<int, 1>{}, kt + KEYS);
     };
     for (int kt = kbeg; kt < kend; kt += 2 * KEYS) {
         step(std::integral_constant<int, 0>{}, kt);

@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
         auto block = [&](auto B_) {
             constexpr int b = decltype(B_)::value;
             const int kb = kt + 32 * b;
-            if (kb >= kend) return;
+            if (kb >= kend || mine.left <= 0) return;
             f32x16 s = zero16(), dp = negD;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -213,6 +213,7 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
     const int pair = wv & 3, head = blockIdx.x % a.nkv, dh = a.d;
     const KeyTile kt = find_tile(a, blockIdx.x / a.nkv);
     const int key = kt.key + pair * 32, n_steps = kt.steps;
+    const bool live = key < kt.end;                     // (a pair behind the last key copies its share of the rows and no more)
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     const uint32_t box0 = lds0 + 3 * SLOT + pair * PDS_BYTES + lane * 16;        // this lane's part of the pair's first buffer
     auto next_slot = [](uint32_t tile) { return tile == 2 * SLOT ? 0u : tile + SLOT; };
@@ -285,14 +286,14 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
             box[128] = rawx4{dd[0], dd[1], dd[2], dd[3]};
             box[192] = rawx4{dd[4], dd[5], dd[6], dd[7]};
         };
-        int left = steps[0].z;
+        int left = entry_of(steps, 0).z;
         for (int step = 0; step < n_steps; ++step) {
-            const int now = __builtin_amdgcn_readfirstlane(left);
-            if (step + 1 < n_steps) left = steps[step + 1].z;
+            const int now = left;
+            if (step + 1 < n_steps) left = entry_of(steps, step + 1).z;
             lds_barrier();
-            block(std::integral_constant<int, 0>{});
+            if (live) block(std::integral_constant<int, 0>{});
             lds_barrier();
-            if (now > 32) block(std::integral_constant<int, 1>{});
+            if (now > 32 && live) block(std::integral_constant<int, 1>{});
             tile = next_slot(tile);
         }
         lds_barrier();                                 // the last block's P and dS are there
@@ -342,15 +343,15 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
             });
         };
         // rows of steps t, t + 1 (copied) and t + 2 (next to be copied, its entry requested a step ahead)
-        Rows now = rows_of(steps[0]), next = now, after = now;
+        int4 entry = entry_of(steps, 0), second = n_steps > 1 ? entry_of(steps, 1) : entry;
+        Rows now = rows_of(entry), next = rows_of(second), after = now;
+        if (n_steps > 2) entry = entry_of(steps, 2);
         copy_q(0, now);
         copy_do(0, now);
         if (n_steps > 1) {
-            next = rows_of(steps[1]);
             copy_q(SLOT, next);
             copy_do(SLOT, next);
         }
-        int4 entry = n_steps > 2 ? steps[2] : make_int4(0, 0, 0, 0);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         // Barrier 2 t stands in front of the first wavefront's block 0 of step t (tile t has landed, block 1 of step t - 1 is in its
         // buffer), barrier 2 t + 1 in front of its block 1.  Behind the latter nobody reads tile t - 1 any more: its slot is tile t + 2's,
@@ -361,15 +362,15 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
             lds_barrier();
             if (step > 0) {
                 if (step + 1 < n_steps) copy_do(next_slot(tile), next);
-                if (left_before > 32) block(std::integral_constant<int, 1>{}, before);
+                if (left_before > 32 && live) block(std::integral_constant<int, 1>{}, before);
             }
             lds_barrier();
             if (step + 2 < n_steps) {
                 after = rows_of(entry);
-                if (step + 3 < n_steps) entry = steps[step + 3];
+                if (step + 3 < n_steps) entry = entry_of(steps, step + 3);
                 copy_q(before, after);
             }
-            block(std::integral_constant<int, 0>{}, tile);
+            if (live) block(std::integral_constant<int, 0>{}, tile);
             // tile t + 1 has landed; the copies of Q for tile t + 2 may be in flight (memory operations retire in order)
             if (step + 2 < n_steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
             next = after;
         }
         lds_barrier();
-        if (left_before > 32) block(std::integral_constant<int, 1>{}, before);
+        if (left_before > 32 && live) block(std::integral_constant<int, 1>{}, before);
     }
     lds_barrier();                                     // the tiles are done with: LDS now stages the output rows
     store_dkv<D, CB>(a, smem, pair, head, key, kt.end - key, dk, dv);
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(256, 2) void cross_dkv_plain_kernel(CrossArgs a) {
         TrReader<D> tr;
         tr.init((uint32_t)(uintptr_t)(lds_void *)smem);
         bf16x8 kf[KS], vf[KS];
-        Rows now = rows_of(steps[0]);
+        Rows now = rows_of(entry_of(steps, 0));
         {
             RowCopier<D, ROWS32<D> / 1024> cpk, cpv;
             cpk.init(0, a.ldk, dh);
@@ -431,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void cross_dkv_plain_kernel(CrossArgs a) {
                 vf[ks] = frag_k<D>(stage_v, l32, ks, half);
             }
         }
-        int4 entry = n_steps > 1 ? steps[1] : make_int4(0, 0, 0, 0);
+        int4 entry = n_steps > 1 ? entry_of(steps, 1) : make_int4(0, 0, 0, 0);
         int slot = 0;
         for (int step = 0; step < n_steps; ++step, slot ^= 1) {
             const uint8_t *sQ = smem + slot * SLOT, *sdO = sQ + TILE;
@@ -441,12 +442,12 @@ __global__ __launch_bounds__(256, 2) void cross_dkv_plain_kernel(CrossArgs a) {
             lds_barrier();                                               // ... and everyone is done with the other slot
             if (step + 1 < n_steps) {
                 now = rows_of(entry);
-                if (step + 2 < n_steps) entry = steps[step + 2];
+                if (step + 2 < n_steps) entry = entry_of(steps, step + 2);
                 copy_tile(smem + (slot ^ 1) * SLOT, now);
             }
             auto block = [&](auto B_) {
                 constexpr int b = decltype(B_)::value;
-                if (32 * b >= left) return;
+                if (32 * b >= left || key >= kt.end) return;
                 f32x16 s = zero16(), dp = zero16();
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {

@@ -160,7 +160,8 @@ __device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool uppe
 // One workgroup makes both lists; it stands in front of dQ's, which do not need them.
 constexpr int PLAN_LDS_RUNS = 256;      // as many runs' places are kept in LDS while they are searched (more: in the workspace)
 constexpr int PLAN_INTS(int runs) { return 3 * (runs + 1) + 2 * (2 * runs + 2); }
-constexpr int PLAN_LDS = (PLAN_INTS(PLAN_LDS_RUNS) + 32) * 4;
+constexpr int PLAN_SORTED = 1024;
+constexpr int PLAN_LDS = (PLAN_INTS(PLAN_LDS_RUNS) + 32 + PLAN_SORTED) * 4;
 template <int THREADS>
 __device__ __forceinline__ int block_scan(int v, bool max, int *sums) {      // inclusive
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -221,11 +222,28 @@ __device__ void make_plan(const CrossArgs &a, int *lds) {
     }
     __threadfence_block();
     __syncthreads();
-    for (int y = threadIdx.x; y < a.n_tiles; y += THREADS) {
+    // tiles with the most steps first, as far as LDS holds their numbers: the workgroups that start last are then the shortest
+    int *const lengths = lds + 32 + PLAN_INTS(PLAN_LDS_RUNS);
+    const bool sorted = a.n_tiles <= PLAN_SORTED;
+    auto tile_of = [&](int y) {
         const int p = find_segment(first_tile, 2 * S + 1, y), first = cuts[p];
         // the runs that see the piece: behind the last that ends in front of it
         const int begin = S > 0 ? first_step[lower_bound(ne, S, first, true)] : 0, end = S > 0 ? first_step[lower_bound(nb, S, first, true)] : 0;
-        a.tiles[y] = make_int4(first + (y - first_tile[p]) * TILE_KEYS, cuts[p + 1], begin, max(end - begin, 0));
+        return make_int4(first + (y - first_tile[p]) * TILE_KEYS, cuts[p + 1], begin, max(end - begin, 0));
+    };
+    for (int y = threadIdx.x; y < a.n_tiles; y += THREADS) {
+        const int4 v = tile_of(y);
+        if (sorted) lengths[y] = v.w;
+        else a.tiles[y] = v;
+    }
+    if (sorted) {
+        __syncthreads();
+        for (int y = threadIdx.x; y < a.n_tiles; y += THREADS) {
+            const int4 v = tile_of(y);
+            int at = 0;
+            for (int i = 0; i < a.n_tiles; ++i) at += lengths[i] > v.w || (lengths[i] == v.w && i < y);
+            a.tiles[at] = v;
+        }
     }
     for (int i = threadIdx.x; i < a.n_steps; i += THREADS) {
         const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group, c0 = a.cu[s];
@@ -237,22 +255,27 @@ struct KeyTile {
     int key, end;               // keys
     int step, steps;            // first step, how many
 };
+// Entries of the lists, which an earlier launch has written: scalar loads, which do not queue up behind the copies into LDS (as vector loads they cost dK/dV
+// up to a tenth: the compiler waits for every copy in flight)
+__device__ __forceinline__ int4 entry_of(const int4 *list, long i) {
+    typedef int Four __attribute__((ext_vector_type(4)));
+    const Four v = *(const __attribute__((address_space(4))) Four *)(uintptr_t)(list + i);
+    return make_int4(v.x, v.y, v.z, v.w);
+}
 __device__ __forceinline__ KeyTile find_tile(const CrossArgs &a, int y) {
-    const int4 v = a.tiles[y];
+    const int4 v = entry_of(a.tiles, y);
     KeyTile k;
-    k.key = __builtin_amdgcn_readfirstlane(v.x);
-    k.end = __builtin_amdgcn_readfirstlane(v.y);
-    const int begin = __builtin_amdgcn_readfirstlane(v.z);
-    const long n = __builtin_amdgcn_readfirstlane(v.w);
+    k.key = v.x;
+    k.end = v.y;
+    const int begin = v.z;
+    const long n = v.w;
     k.step = begin + (int)(n * blockIdx.y / a.parts);
     k.steps = begin + (int)(n * (blockIdx.y + 1) / a.parts) - k.step;
     return k;
 }
 __device__ __forceinline__ Rows rows_of(const int4 &e) {
     Rows r;
-    r.t = __builtin_amdgcn_readfirstlane(e.x);
-    r.j = __builtin_amdgcn_readfirstlane(e.y);
-    r.left = __builtin_amdgcn_readfirstlane(e.z);
+    r.t = e.x; r.j = e.y; r.left = e.z;
     return r;
 }
 template <typename K>
