@@ -99,22 +99,26 @@ __device__ __forceinline__ void add_rows(f32x4 (&acc)[KB], const Columns<KB> &x,
     }
 }
 
+// a lane's share of the [owned row][feature] result, handed to out(row, first of four features, value)
+template <int KB, typename F>
+__device__ __forceinline__ void lane_parts(const f32x4 (&acc)[KB], F out) {
+    const int r = threadIdx.x & 15, q = (threadIdx.x & 48) >> 4;
+    constexpr int C = Columns<KB>::C;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out(r, 64 * c + 16 * q + 4 * e, f32x4{acc[4 * c][e], acc[4 * c + 1][e], acc[4 * c + 2][e], acc[4 * c + 3][e]});
+#pragma unroll
+    for (int i = 0; i < Columns<KB>::R; ++i) out(r, 64 * C + 16 * i + 4 * q, acc[4 * C + i]);
+}
+
 // the wavefronts' [16 owned rows][D] results
 template <int KB, int NW>
 struct Partials {
     static constexpr int D = 16 * KB, PITCH = D + 4;
     float v[NW][16][PITCH];
     __device__ __forceinline__ void put(int wave, const f32x4 (&acc)[KB]) {
-        const int r = threadIdx.x & 15, q = (threadIdx.x & 48) >> 4;
-        constexpr int C = Columns<KB>::C;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<f32x4 *>(&v[wave][r][64 * c + 16 * q + 4 * e]) =
-                    f32x4{acc[4 * c][e], acc[4 * c + 1][e], acc[4 * c + 2][e], acc[4 * c + 3][e]};
-#pragma unroll
-        for (int i = 0; i < Columns<KB>::R; ++i) *reinterpret_cast<f32x4 *>(&v[wave][r][64 * C + 16 * i + 4 * q]) = acc[4 * C + i];
+        lane_parts(acc, [&](int row, int col, f32x4 x) { *reinterpret_cast<f32x4 *>(&v[wave][row][col]) = x; });
     }
     // sums times `scale`, handed to out(row, first of four features, value)
     template <typename F>
@@ -253,9 +257,11 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
     if (a.n_tiles > 0 && block-- == 0) { make_plan<64 * NW>(a, lds.plan); return; }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = threadIdx.x & 15, q4 = ((threadIdx.x & 48) >> 4) * 4;
     const int head = block % a.nkv, dh = a.d;
-    const Item it = find_item(a, block / a.nkv, 16, 0);
+    const Item it = find_item(a, block / a.nkv, 16, a.chunk);
+    const int parts = a.chunk ? max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1) : 1;
     const Group g(a);
-    const Rows mine(it, g, it.index * 16);
+    const Rows mine(it, g, it.index / parts * 16);
+    const int kbeg = it.lo + it.index % parts * a.chunk, kend = parts > 1 ? min(kbeg + a.chunk, it.hi) : it.hi;
     const long col = (long)head * g.n * dh;
     const float *const K = (const float *)a.k + (long)head * dh, *const V = (const float *)a.v + (long)head * dh;
     Pieces<KB> q, go, o;
@@ -272,39 +278,46 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
         const int tok = g.token(mine.j + r), h = head * g.n + mine.j + r - tok * g.n;
         const long at = (long)h * a.Tq + mine.t + tok;
         lse = a.lse[at];
-        if (threadIdx.x < 16) a.D[at] = D;
+        if (threadIdx.x < 16 && kbeg == it.lo) a.D[at] = D;
     }
     if (!a.dq) return;
     f32x4 acc[KB];
 #pragma unroll
     for (int i = 0; i < KB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = it.lo + 16 * wave; k0 < it.hi; k0 += 16 * NW) {
+    for (int k0 = kbeg + 16 * wave; k0 < kend; k0 += 16 * NW) {
         Pieces<KB> k, v;
         Columns<KB> kc;
-        const Block kb = key_block(K, a.ldk, dh, k0, it.hi);
+        const Block kb = key_block(K, a.ldk, dh, k0, kend);
         pieces(kb, k);
-        pieces(key_block(V, a.ldv, dh, k0, it.hi), v);
+        pieces(key_block(V, a.ldv, dh, k0, kend), v);
         columns(kb, kc);
         const f32x4 s = dot_rows(k, q) * a.scale, dp = dot_rows(v, go);
         f32x4 ds;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ds[e] = k0 + q4 + e < it.hi ? expf(s[e] - lse) * (dp[e] - D) : 0.f;
+        for (int e = 0; e < 4; ++e) ds[e] = k0 + q4 + e < kend ? expf(s[e] - lse) * (dp[e] - D) : 0.f;
         add_rows(acc, kc, ds);
     }
     part.put(wave, acc);
     __syncthreads();
+    if (parts > 1) {
+        float *out = a.part + (size_t)block * 16 * dh;
+        part.each(1.f, [&](int row, int c, f32x4 v) { if (row < mine.left) *reinterpret_cast<f32x4 *>(out + row * dh + c) = v; });
+        return;
+    }
     float *out = (float *)a.dq + mine.t * a.lddq + col;
     part.each(a.scale, [&](int row, int c, f32x4 v) { if (row < mine.left) *reinterpret_cast<f32x4 *>(out + mine.offset(g, row, a.lddq, dh) + c) = v; });
 }
 
 // dK_j = scale * sum_i dS_ij q_i,   dV_j = sum_i P_ij dO_i over the rows i of the runs that see the keys
-template <int KB, int NW>
+// OWN: each wavefront has 16 keys to itself and walks all rows, without LDS
+template <int KB, int NW, bool OWN>
 __global__ __launch_bounds__(64 * NW) void cross_f32_dkv_kernel(CrossArgs a) {
-    __shared__ __attribute__((aligned(16))) Partials<KB, NW> part;
+    __shared__ __attribute__((aligned(16))) std::conditional_t<OWN, int, Partials<KB, NW>> part;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = ((threadIdx.x & 48) >> 4) * 4;
     const int head = blockIdx.x % a.nkv, dh = a.d, block = blockIdx.x / a.nkv;
-    KeyTile kt = find_tile(a, block / (TILE_KEYS / 16));
-    kt.key += block % (TILE_KEYS / 16) * 16;
+    constexpr int BLOCKS = TILE_KEYS / 16 / (OWN ? NW : 1);          // workgroups of a tile
+    KeyTile kt = find_tile(a, block / BLOCKS);
+    kt.key += (OWN ? block % BLOCKS * NW + wave : block % BLOCKS) * 16;
     if (kt.key >= kt.end) return;
     const Group g(a);
     const long col = (long)head * g.n * dh;
@@ -314,11 +327,13 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dkv_kernel(CrossArgs a) {
     f32x4 dk[KB], dv[KB];
 #pragma unroll
     for (int i = 0; i < KB; ++i) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = wave; i < 4 * kt.steps; i += NW) {
-        const Rows step = rows_of(entry_of(a.steps, kt.step + i / 4));
+    // blocks of 16 rows: the first of all steps, then the second ... (of short runs no more than the first exists)
+    for (int i = OWN ? 0 : wave; i < 4 * kt.steps; i += OWN ? 1 : NW) {
+        const int quarter = (i >= kt.steps) + (i >= 2 * kt.steps) + (i >= 3 * kt.steps);
+        const Rows step = rows_of(entry_of(a.steps, kt.step + i - quarter * kt.steps));
         Rows at;
-        const int first = step.j + i % 4 * 16, tok = g.token(first);
-        at.t = step.t + tok; at.j = first - tok * g.n; at.left = step.left - i % 4 * 16;
+        const int first = step.j + quarter * 16, tok = g.token(first);
+        at.t = step.t + tok; at.j = first - tok * g.n; at.left = step.left - quarter * 16;
         if (at.left <= 0) continue;
         Pieces<KB> q, go;
         Columns<KB> qc, gc;
@@ -344,17 +359,20 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dkv_kernel(CrossArgs a) {
         add_rows(dk, qc, ds);
     }
     const int rows = kt.end - kt.key;
-    auto store = [&](void *p, long ld, float scale) {
+    auto store = [&](const f32x4 (&acc)[KB], void *p, long ld, float scale) {
         float *out = (float *)p + kt.key * ld + (long)head * dh;
-        part.each(scale, [&](int row, int c, f32x4 x) { if (row < rows) *reinterpret_cast<f32x4 *>(out + row * ld + c) = x; });
+        auto to = [&](int row, int c, f32x4 x) { if (row < rows) *reinterpret_cast<f32x4 *>(out + row * ld + c) = x; };
+        if constexpr (OWN) {
+            lane_parts(acc, [&](int row, int c, f32x4 x) { to(row, c, x * scale); });
+        } else {
+            __syncthreads();
+            part.put(wave, acc);
+            __syncthreads();
+            part.each(scale, to);
+        }
     };
-    part.put(wave, dk);
-    __syncthreads();
-    store(a.dk, a.lddk, a.scale);
-    __syncthreads();
-    part.put(wave, dv);
-    __syncthreads();
-    store(a.dv, a.lddv, 1.f);
+    store(dk, a.dk, a.lddk, a.scale);
+    store(dv, a.dv, a.lddv, 1.f);
 }
 
 // eight wavefronts for heads of up to 64 features; four for wider ones, whose partial results are as large
@@ -390,7 +408,10 @@ hipError_t cross_f32_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t 
     return by_width(a.d, [&](auto KB_) {
         constexpr int KB = decltype(KB_)::value;
         if (p.items || a.n_tiles) cross_f32_dq_kernel<KB, WAVES<KB>><<<p.items * a.nkv + (a.n_tiles > 0), 64 * WAVES<KB>, 0, st>>>(a);
-        if (a.n_tiles) cross_f32_dkv_kernel<KB, WAVES<KB>><<<a.n_tiles * (TILE_KEYS / 16) * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
+        if (a.chunk) cross_dq_sum_kernel<float, 16><<<p.items * a.nkv, 256, 0, st>>>(a);
+        if (!a.n_tiles) return hipGetLastError();
+        if (p.own) cross_f32_dkv_kernel<KB, 4, true><<<a.n_tiles * (TILE_KEYS / 64) * a.nkv, 256, 0, st>>>(a);
+        else cross_f32_dkv_kernel<KB, WAVES<KB>, false><<<a.n_tiles * (TILE_KEYS / 16) * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
         return hipGetLastError();
     });
 }

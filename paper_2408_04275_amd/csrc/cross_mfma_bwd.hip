@@ -24,6 +24,27 @@ __device__ __forceinline__ void copy_rows_part(const bf16_t *p, long ld, int dh,
     }
 }
 
+template <int D> constexpr int STAGE32 = 32 * (4 * D + 16);
+// a wavefront's 32 keys' results, unscaled, as fp32 rows of a workgroup's part
+template <int D, int CB>
+__device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[CB], float *dst, long ld, int rows, int dh) {
+    constexpr int RS = 4 * D + 16, LPR = D / 4, RPI = 64 / LPR;
+    const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int gq = 0; gq < 4; ++gq)
+            *reinterpret_cast<f32x4 *>(stage + l32 * RS + (32 * c + 8 * gq + 4 * half) * 4) =
+                f32x4{acc[c][4 * gq], acc[c][4 * gq + 1], acc[c][4 * gq + 2], acc[c][4 * gq + 3]};
+    const int r0 = lane / LPR, cb = (lane % LPR) * 4;
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+        const int r = i * RPI + r0;
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(stage + r * RS + cb * 4);
+        if (r < rows && cb < dh) *reinterpret_cast<f32x4 *>(dst + (long)r * ld + cb) = v;
+    }
+}
+
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 // Four wavefronts of 32 rows, two workgroups a compute unit (eight and one are nowhere faster: us, 128 / 256 rows, both backward kernels: 4096 tokens of 32 heads
 // of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284).
@@ -38,10 +59,11 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
     int block = blockIdx.x;
     if (a.n_tiles > 0 && block-- == 0) { make_plan<256>(a, (int *)smem); return; }
     const int head = block % a.nkv, dh = a.d;
-    const Item it = find_item(a, block / a.nkv, 128, 0);
+    const Item it = find_item(a, block / a.nkv, 128, a.chunk);
+    const int parts = a.chunk ? max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1) : 1, part = it.index % parts;
     const Group g(a);
-    const Rows mine(it, g, it.index * 128 + wave * 32);
-    const int kbeg = it.lo, kend = a.dq ? it.hi : it.lo;
+    const Rows mine(it, g, it.index / parts * 128 + wave * 32);
+    const int kbeg = it.lo + part * a.chunk, kend = !a.dq ? kbeg : parts > 1 ? min(kbeg + a.chunk, it.hi) : it.hi;
     const bf16_t *const K = (const bf16_t *)a.k + (long)head * dh, *const V = (const bf16_t *)a.v + (long)head * dh;
     const long col = (long)head * g.n * dh;
 
@@ -87,7 +109,7 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
         const int tok = g.token(mine.j + l32), h = head * g.n + mine.j + l32 - tok * g.n;
         const long at = (long)h * a.Tq + mine.t + tok;
         lse2 = a.lse[at] * LOG2E;
-        if (half == 0) a.D[at] = -Dq;
+        if (half == 0 && part == 0) a.D[at] = -Dq;
     }
     if (!a.dq) return;
     // with 64-wide heads dP - D comes out of the matrix core (see attn_mfma.hip)
@@ -150,7 +172,8 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
         block(std::integral_constant<int, 1>{});
     }
     lds_barrier();                                     // the tiles are done with: LDS now stages the output rows
-    store_rows_at<D, CB>(smem + wave * STAGE<D>, dq, a.scale, (bf16_t *)a.dq + col, a.lddq, dh, mine, g);
+    if (parts > 1) store_part<D, CB>(smem + wave * STAGE32<D>, dq, a.part + ((size_t)block * 128 + wave * 32) * dh, dh, mine.left, dh);
+    else store_rows_at<D, CB>(smem + wave * STAGE<D>, dq, a.scale, (bf16_t *)a.dq + col, a.lddq, dh, mine, g);
 }
 
 // 64 values of a [heads, Tq] array, those of a step's rows, into LDS
@@ -162,26 +185,6 @@ __device__ __forceinline__ void copy_stats(const float *x, const CrossArgs &a, i
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)to, 4, (int)off, 0, 0, 0);
 }
 
-template <int D> constexpr int STAGE32 = 32 * (4 * D + 16);
-// a wavefront's 32 keys' results, unscaled, as fp32 rows of a workgroup's part
-template <int D, int CB>
-__device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[CB], float *dst, long ld, int rows, int dh) {
-    constexpr int RS = 4 * D + 16, LPR = D / 4, RPI = 64 / LPR;
-    const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int gq = 0; gq < 4; ++gq)
-            *reinterpret_cast<f32x4 *>(stage + l32 * RS + (32 * c + 8 * gq + 4 * half) * 4) =
-                f32x4{acc[c][4 * gq], acc[c][4 * gq + 1], acc[c][4 * gq + 2], acc[c][4 * gq + 3]};
-    const int r0 = lane / LPR, cb = (lane % LPR) * 4;
-#pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i) {
-        const int r = i * RPI + r0;
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(stage + r * RS + cb * 4);
-        if (r < rows && cb < dh) *reinterpret_cast<f32x4 *>(dst + (long)r * ld + cb) = v;
-    }
-}
 template <int D, int CB>
 __device__ __forceinline__ void store_dkv(const CrossArgs &a, uint8_t *smem, int wave, int head, int key, int rows, const f32x16 (&dk)[CB], const f32x16 (&dv)[CB]) {
     const int dh = a.d, nk = a.nkv * dh;
@@ -514,11 +517,12 @@ __global__ __launch_bounds__(256) void cross_dkv_sum_kernel(CrossArgs a) {
 template <int D, int KS, int CB>
 hipError_t launch_dq(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
-    constexpr int LDS = std::max(DQ_LDS<D>, 4 * STAGE<D>);
+    constexpr int LDS = std::max(DQ_LDS<D>, 4 * STAGE32<D>);
     static_assert(PLAN_LDS <= LDS, "room for the plan");
     const hipError_t e = set_smem(done, cross_dq_kernel<D, KS, CB>, LDS);
     if (e != hipSuccess) return e;
     cross_dq_kernel<D, KS, CB><<<items * a.nkv + (a.n_tiles > 0), 256, LDS, st>>>(a);
+    if (a.chunk) cross_dq_sum_kernel<bf16_t, 128><<<items * a.nkv, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -36,6 +36,11 @@ __global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int til
 }
 
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
+int items(const CrossShape &c, int rows, int chunk) {
+    int n = 0;
+    for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], c.nh / c.nkv, rows, chunk);
+    return n;
+}
 size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
 
 void order_runs(const CrossShape &c, CrossArgs &a) {
@@ -49,11 +54,7 @@ void order_runs(const CrossShape &c, CrossArgs &a) {
 // How a forward pass is cut: by the rows of the runs and the keys they see
 CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
     const int group = c.nh / c.nkv;
-    auto count = [&](int rows, int chunk) {
-        long n = 0;
-        for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], group, rows, chunk);
-        return n;
-    };
+    auto count = [&](int rows, int chunk) { return (long)items(c, rows, chunk); };
     // steps of 32 rows and 32 keys
     long few = 0, many = 0, longest = 0;
     for (int s = 0; s < c.S; ++s) {
@@ -99,67 +100,138 @@ hipError_t cross_fwd(int dtype, const CrossArgs &args, const CrossShape &c, cons
     return dtype == DT_F32 ? cross_f32_fwd(a, p, st) : cross_mfma_fwd(a, p, st);
 }
 
+// Keys between two places where a run's range begins or ends: steps of the rows that see them, tiles of keys
+struct Piece { long steps, tiles; };
+constexpr int MOST_PIECES = 1024;      // (a call with more tiles than this has workgroups enough)
+
+// How many workgroups share a tile's rows.  `slots` workgroups run at a time, those with the most steps first: they take at least as long as the k-th round's
+// longest k times over, or all steps spread evenly.  A step takes about 2 us (64-wide heads 1.4), a workgroup's beginning and end 5, and what several share
+// is written and read once more.  us, 1 / 2 / 4 / 8 parts, the whole backward pass: 4096 tokens of 16 heads of 128 in a run of 700 keys 144 / 111 / 123 / 129,
+// 4000 tokens of 16 heads of 64, on 4 in five runs that see 2000 keys 376 / 216 / 137 / 105, 4096 of 64 heads of 128, on 8 in eight runs of 625 320 / 344 / 358 / 425.
+int dkv_parts(const CrossShape &c, Piece *pieces, int n_pieces, long tiles) {
+    const long slots = c.d > 64 ? 256 : 512, all = tiles * c.nkv;
+    if (all == 0 || all >= 2 * slots) return 1;
+    std::sort(pieces, pieces + n_pieces, [](const Piece &x, const Piece &y) { return x.steps > y.steps; });
+    double work = 0;
+    for (int i = 0; i < n_pieces; ++i) work += (double)pieces[i].steps * pieces[i].tiles;
+    const double step_us = c.d > 64 ? 2. : 1.4;
+    double best = 0;
+    int parts = 1;
+    for (int n = 1; n <= 16 && (n == 1 || part_bytes(c) * n <= size_t(96) << 20); ++n) {
+        const long rounds = (all * n + slots - 1) / slots;
+        double steps = work * c.nkv / slots;
+        int at = 0;
+        long before = 0;                                 // tiles of the pieces in front
+        for (long k = 0; k < rounds; ++k) {
+            while (at + 1 < n_pieces && (before + pieces[at].tiles) * c.nkv * n <= k * slots) before += pieces[at++].tiles;
+            steps = std::max(steps, (double)((k + 1) * ((pieces[at].steps + n - 1) / n)));
+        }
+        const double us = steps * step_us + rounds * 5 + (n > 1 ? 4 + n * (double)part_bytes(c) / 3e6 : 0);
+        if (n == 1 || us < best) { best = us; parts = n; }
+    }
+    return parts;
+}
+
 CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     const int group = c.nh / c.nkv;
     CrossBwdPlan p = {};
     p.rows = dtype == DT_F32 ? 16 : 128;
-    for (int s = 0; s < c.S; ++s) p.items += items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
+    // Keys are cut into chunks where tiles of rows leave the chip empty and some walk 12 steps of 64 keys and more; a chunk has four steps at least (fp32: two).
+    // us, uncut / cut, the whole backward pass, one run of 8 heads of 128: 100 tokens, 768 keys 36 / 30, 2304 keys 79 / 32; 1500 tokens, 768 keys 53 / 55, 2304 keys
+    // 113 / 91; fp32, heads of 64, 100 tokens, 2304 keys 86 / 66.
+    long walk = 0, longest = 0;
+    for (int s = 0; s < c.S; ++s) {
+        const int n = items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
+        const long keys = (c.end[s] - c.begin[s] + 63) / 64;
+        p.items += n;
+        walk += n * keys;
+        if (n) longest = std::max(longest, keys);
+    }
+    if ((long)p.items * c.nkv < 256 && longest >= 12) {
+        const long want = std::max(walk * c.nkv / 512, dtype == DT_F32 ? 2l : 4l);
+        if (want < longest) {
+            p.chunk = (int)want * 64;
+            p.items = items(c, p.rows, p.chunk);
+        }
+    }
     p.table = c.S > 64;
     p.dkv = dkv;
     p.parts = 1;
     if (!dkv) return p;
     // the pieces of the keys: beginnings and ends of the runs that see something, merged
-    long tiles = 0, steps = 0;
+    long tiles = 0, steps = 0, open = 0;                 // steps of all runs, of those that see a piece
+    long open16 = 0, walk16 = 0;                         // blocks of 16 rows of the runs that see a piece; that all tiles walk
+    Piece pieces[MOST_PIECES];
+    int n_pieces = 0;
     int at = 0;
+    auto blocks_of = [&](int s, int rows) { return ((long)(c.cu[s + 1] - c.cu[s]) * group + rows - 1) / rows; };
     auto cut = [&](int place) {
-        tiles += (place - at + TILE_KEYS - 1) / TILE_KEYS;
+        const long n = (place - at + TILE_KEYS - 1) / TILE_KEYS;
+        tiles += n;
+        walk16 += n * open16;
+        if (n && tiles < MOST_PIECES) pieces[n_pieces++] = {open, n};
         at = place;
     };
     int b = 0, e = 0;
     auto next = [&](int s) { while (s < c.S && c.begin[s] == c.end[s]) ++s; return s; };
     for (b = next(0), e = b; e < c.S;) {
-        if (b < c.S && c.begin[b] <= c.end[e]) { cut(c.begin[b]); b = next(b + 1); }
-        else { cut(c.end[e]); e = next(e + 1); }
+        if (b < c.S && c.begin[b] <= c.end[e]) {
+            cut(c.begin[b]);
+            steps += blocks_of(b, STEP_ROWS);
+            open += blocks_of(b, STEP_ROWS);
+            open16 += blocks_of(b, 16);
+            b = next(b + 1);
+        } else {
+            cut(c.end[e]);
+            open -= blocks_of(e, STEP_ROWS);
+            open16 -= blocks_of(e, 16);
+            e = next(e + 1);
+        }
     }
     cut(c.Tk);
-    for (int s = 0; s < c.S; ++s)
-        if (c.begin[s] < c.end[s]) steps += ((long)(c.cu[s + 1] - c.cu[s]) * group + STEP_ROWS - 1) / STEP_ROWS;
     p.tiles = (int)tiles;
     p.steps = (int)steps;
-    if (dtype == DT_F32) return p;                       // (a workgroup per 16 keys: enough of them)
-    // Workgroups that share a tile's rows: until the chip has two rounds of workgroups, as long as each has a few steps
-    const long want = c.d > 64 ? 512 : 1024;
-    while (p.parts < 16 && (long)p.tiles * c.nkv * p.parts * 2 <= want && steps >= 8l * p.parts && part_bytes(c) * p.parts * 2 <= size_t(96) << 20) p.parts *= 2;
+    if (dtype == DT_F32) {
+        // A workgroup for each 16 keys, or, where that gives every SIMD two wavefronts and there are few rows to share out, a wavefront.  us, workgroup / wavefront,
+        // the whole backward pass, heads of 64: 400 tokens of 16 heads in 40 runs of 200 keys 154 / 73, of 4 heads 54 / 30; 1000 of 16 heads in eight runs of 1000 keys
+        // 314 / 232; heads of 80: 1031 tokens of 16 heads in five runs of 420 keys 115 / 135, 1000 in one of 8000 keys 1931 / 1997.
+        p.own = (long)p.tiles * (TILE_KEYS / 16) * c.nkv >= 2048 && walk16 <= 8 * tiles;
+        return p;
+    }
+    p.parts = dkv_parts(c, pieces, n_pieces, tiles);
     return p;
 }
 
 size_t plan_bytes(int runs) { return runs > PLAN_LDS_RUNS ? aligned((size_t)PLAN_INTS(runs) * sizeof(int)) : 0; }
 
-// [D] [table of items] [tiles] [steps] [what they are made of] [parts]
+// [D] [table of items] [tiles] [steps] [what they are made of] [parts: of dQ, then of dK and dV]
 size_t cross_bwd_bytes(const CrossShape &c, const CrossBwdPlan &p) {
     size_t n = aligned((size_t)c.Tq * c.nh * sizeof(float)) + (p.table ? table_bytes(c.S) : 0);
-    if (p.dkv) n += aligned((size_t)p.tiles * sizeof(int4)) + aligned((size_t)p.steps * sizeof(int4)) + plan_bytes(c.S) + (p.parts > 1 ? p.parts * part_bytes(c) : 0);
-    return n;
+    if (p.dkv) n += aligned((size_t)p.tiles * sizeof(int4)) + aligned((size_t)p.steps * sizeof(int4)) + plan_bytes(c.S);
+    return n + std::max(p.dkv && p.parts > 1 ? p.parts * part_bytes(c) : 0, p.chunk ? (size_t)p.items * c.nkv * p.rows * c.d * sizeof(float) : 0);
 }
 
-hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossShape &c, const CrossBwdPlan &p, void *ws, hipStream_t st) {
+hipError_t cross_bwd(int dtype, const CrossArgs &args, const CrossShape &c, const CrossBwdPlan &plan, void *ws, hipStream_t st) {
     CrossArgs a = args;
+    CrossBwdPlan p = plan;
+    if (!a.dq && p.chunk) { p.chunk = 0; p.items = items(c, p.rows, 0); }
     order_runs(c, a);
     uint8_t *at = (uint8_t *)ws;
     auto take = [&](size_t n) { void *q = at; at += n; return q; };
     a.D = (float *)take(aligned((size_t)a.Tq * a.nh * sizeof(float)));
     a.parts = p.parts;
+    a.chunk = p.chunk;
     if (p.table) {
         a.prefix = (int *)take(table_bytes(a.S));
-        if (p.items) cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, 0, const_cast<int *>(a.prefix));
+        if (p.items) cross_prefix_kernel<<<1, 1024, 0, st>>>(a, p.rows, p.chunk, const_cast<int *>(a.prefix));
     }
     if (p.dkv && p.tiles) {
         a.tiles = (int4 *)take(aligned((size_t)p.tiles * sizeof(int4)));
         a.steps = (int4 *)take(aligned((size_t)p.steps * sizeof(int4)));
         a.plan = (int *)take(plan_bytes(a.S));
         a.n_tiles = p.tiles; a.n_steps = p.steps;
-        a.dkv_part = (float *)at;
     }
+    a.part = a.dkv_part = (float *)at;                   // one after the other
     if (!p.items && !(p.dkv && p.tiles)) return hipSuccess;
     return dtype == DT_F32 ? cross_f32_bwd(a, p, st) : cross_mfma_bwd(a, p, st);
 }

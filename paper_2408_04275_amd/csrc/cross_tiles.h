@@ -286,6 +286,37 @@ hipError_t set_smem(std::atomic<bool> &done, K kern, int bytes) {
     return e;
 }
 
+// dQ from the sums over chunks of keys: the workgroups of a tile's chunks share out its rows
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossArgs a) {
+    const int head = blockIdx.x % a.nkv, dh = a.d;
+    const Item it = find_item(a, blockIdx.x / a.nkv, ROWS, a.chunk);
+    const int parts = max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1), mine_of = it.index % parts;
+    if (parts == 1) return;
+    const Group g(a);
+    const Rows mine(it, g, it.index / parts * ROWS);
+    const int quads = dh / 4, rows = min(mine.left, ROWS);
+    const size_t stride = (size_t)a.nkv * ROWS * dh;
+    const float *part = a.part + (size_t)(blockIdx.x - mine_of * a.nkv) * ROWS * dh;
+    T *const out = (T *)a.dq + mine.t * a.lddq + (long)head * g.n * dh;
+    for (int e = mine_of * 256 + threadIdx.x; e < rows * quads; e += parts * 256) {
+        const int r = e / quads, c = e % quads * 4;
+        const float *p = part + r * dh + c;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int j0 = 0; j0 < parts; j0 += 8) {
+            f32x4 y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = j0 + i < parts ? *reinterpret_cast<const f32x4 *>(p + (j0 + i) * stride) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x += y[i];
+        }
+        x *= a.scale;
+        T *const to = out + mine.offset(g, r, a.lddq, dh) + c;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(to) = x;
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    }
+}
+
 inline size_t table_bytes(int runs) { return ((size_t)(runs + 1) * sizeof(int) + 255) & ~size_t(255); }
 
 }  // namespace

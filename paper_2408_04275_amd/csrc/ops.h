@@ -117,7 +117,7 @@ struct CrossArgs {
     uint8_t order[64];              // runs by falling number of keys, where there are at most 64
     const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
     int chunk;                      // keys of a workgroup; 0: all of its run's
-    float *part; float2 *part_ml;   // partial results of the chunks
+    float *part; float2 *part_ml;   // partial results of the chunks [item, head][rows][d], their maxima and sums (forward)
     // dK and dV: see make_plan
     int4 *tiles, *steps;
     int n_tiles, n_steps;           // n_tiles 0: not wanted
@@ -132,9 +132,10 @@ struct CrossPlan {
     bool table;                     // items are found in a table
 };
 struct CrossBwdPlan {
-    int rows, items;                // dQ: rows of a workgroup, workgroups per key/value head
+    int rows, chunk, items;         // dQ: as above
     bool table, dkv;
     int tiles, steps, parts;        // dK and dV: tiles of keys, tiles of rows of all runs, workgroups per tile of keys
+    bool own;                       // ... fp32: a wavefront has 16 keys to itself
 };
 // Plans, workspaces (256-byte aligned) and calls.  dkv: the gradients of keys and values are wanted
 CrossPlan cross_fwd_plan(int dtype, const CrossShape &c);
