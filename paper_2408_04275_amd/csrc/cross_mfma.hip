@@ -187,15 +187,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
 }
 
 // ---- forward, few rows ----------------------------------------------------------------------------------------------------
-// Up to 32 rows per workgroup, whose four wavefronts share out the blocks of 32 keys, each with LDS slots of its own (four with 64-wide heads, two
-// with wider ones) and no barrier on the way: the next blocks are in flight while one is multiplied.  Where that leaves the chip empty or one workgroup with a long walk, the keys
-// are cut into chunks, one per workgroup, whose partial results (32 rows of fp32, maximum and sum) cross_combine_kernel joins.
-template <int D> constexpr int FEW_SLOTS = D <= 64 ? 4 : 2;
-template <int D> constexpr int FEW_LDS = 4 * FEW_SLOTS<D> * 2 * ROWS32<D>;
+// Up to 32 rows per workgroup, whose wavefronts (eight with 64-wide heads, four with wider ones) share out the blocks of 32 keys, each with two LDS slots of its
+// own and no barrier on the way: the next block is in flight while one is multiplied.  Three tokens of 16 heads of 64, 577 keys each: 6.7 us, 8.6 with four
+// wavefronts and four slots.  Where that leaves the chip empty or one workgroup with a long walk, the keys are cut into chunks, one per workgroup, whose partial
+// results (32 rows of fp32, maximum and sum) cross_combine_kernel joins.
+constexpr int FEW_SLOTS = 2;
+template <int D> constexpr int FEW_WAVES = D <= 64 ? 8 : 4;
+template <int D> constexpr int FEW_LDS = FEW_WAVES<D> * FEW_SLOTS * 2 * ROWS32<D>;
 
 template <int D, int KS, int CB>
-__global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
-    constexpr int N = ROWS32<D> / 1024, SLOT = 2 * ROWS32<D>, SLOTS = FEW_SLOTS<D>, MINE = SLOTS * SLOT;
+__global__ __launch_bounds__(64 * FEW_WAVES<D>, 1) void cross_fwd_few_kernel(CrossArgs a) {
+    constexpr int N = ROWS32<D> / 1024, SLOT = 2 * ROWS32<D>, SLOTS = FEW_SLOTS, MINE = SLOTS * SLOT, NW = FEW_WAVES<D>, NEXT = 32 * NW;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_all[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     uint8_t *const smem = smem_all + wave * MINE;
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
     // SLOTS - 1 blocks are on their way at any time; what stands behind the last key is copied as zeros, so that a wait counts the same everywhere
     int kb = kbeg + 32 * wave;
     copy_rows<D>((const bf16_t *)a.q + (long)head * g.n * dh, a.ldq, dh, mine, g, smem + (SLOTS - 1) * SLOT);
-    static_for<0, SLOTS - 1>([&](auto S_) { copy_kv(smem + decltype(S_)::value * SLOT, kb + 128 * decltype(S_)::value); });
+    static_for<0, SLOTS - 1>([&](auto S_) { copy_kv(smem + decltype(S_)::value * SLOT, kb + NEXT * decltype(S_)::value); });
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N * (SLOTS - 1)) : "memory");
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
     uint32_t kadr[KS];
@@ -290,10 +292,10 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
             constexpr int slot = decltype(S_)::value;
             if (kb >= kend) return;
             asm volatile("" ::: "memory");               // (the slot in front has been read: its reads have been waited for)
-            copy_kv(smem + (slot + SLOTS - 1) % SLOTS * SLOT, kb + 128 * (SLOTS - 1));
+            copy_kv(smem + (slot + SLOTS - 1) % SLOTS * SLOT, kb + NEXT * (SLOTS - 1));
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N * (SLOTS - 1)) : "memory");
             block(S_, kb);
-            kb += 128;
+            kb += NEXT;
         });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // four partial softmaxes over disjoint keys become one: each wavefront joins one block of 32 features
@@ -302,15 +304,15 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
     float2 *const ml = reinterpret_cast<float2 *>(smem + SLOT);
     if (half == 0) ml[l32] = make_float2(m_run, l_own);
     lds_barrier();
-    float m = -INFINITY, l = 0.f, mw[4], f[4];
+    float m = -INFINITY, l = 0.f, mw[NW], f[NW];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
         const float2 v = reinterpret_cast<const float2 *>(smem_all + w * MINE + SLOT)[l32];
         mw[w] = v.x; f[w] = v.y;
         m = fmaxf(m, v.x);
     }
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
         const float e = mw[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw[w] - m) * sl2);
         l += f[w] * e;
         f[w] = e;
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
         for (int i = 0; i < 4; ++i) {
             x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x[i] += reinterpret_cast<const f32x4 *>(smem_all + w * MINE)[(4 * wave + i) * 64 + lane] * f[w];
+            for (int w = 0; w < NW; ++w) x[i] += reinterpret_cast<const f32x4 *>(smem_all + w * MINE)[(4 * wave + i) * 64 + lane] * f[w];
         }
         const int c0 = 32 * wave + 4 * half;
         if (parts > 1) {
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(256, 1) void cross_fwd_few_kernel(CrossArgs a) {
                     *reinterpret_cast<uint2 *>(out + 8 * i) = make_uint2(pack_bf16x2(x[i][0] * r, x[i][1] * r), pack_bf16x2(x[i][2] * r, x[i][3] * r));
         }
     }
-    if (wave == 3 && half == 0 && live) {
+    if (wave == NW - 1 && half == 0 && live) {
         if (parts > 1) a.part_ml[(size_t)blockIdx.x * FEW_ROWS + l32] = make_float2(m, l);
         else if (a.lse) a.lse[(long)(head * g.n + h) * a.Tq + mine.t + tok] = natural_lse(m, l, sl2);
     }
@@ -412,7 +414,7 @@ hipError_t launch_few(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
     const hipError_t e = set_smem(done, cross_fwd_few_kernel<D, KS, CB>, FEW_LDS<D>);
     if (e != hipSuccess) return e;
-    cross_fwd_few_kernel<D, KS, CB><<<items * a.nkv, 256, FEW_LDS<D>, st>>>(a);
+    cross_fwd_few_kernel<D, KS, CB><<<items * a.nkv, 64 * FEW_WAVES<D>, FEW_LDS<D>, st>>>(a);
     if (a.chunk) cross_combine_kernel<<<items * a.nkv, 256, 0, st>>>(a);
     return hipGetLastError();
 }

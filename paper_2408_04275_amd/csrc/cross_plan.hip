@@ -7,14 +7,17 @@ namespace mmt {
 
 namespace {
 
-// exclusive sums of the runs' items, [S + 1]: one workgroup
+// exclusive sums of the runs' items [S + 1], those of a sequence of runs with the same keys at its first; the first run behind its sequence [S]: one workgroup
 __global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int tile_rows, int chunk, int *out) {
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int base = 0;
     for (int s0 = 0; s0 < a.S; s0 += 1024) {
         const int s = s0 + threadIdx.x;
-        const int n = s < a.S ? items_of(a.cu[s + 1] - a.cu[s], a.end[s] - a.begin[s], a.nh / a.nkv, tile_rows, chunk) : 0;
+        const bool first = first_of_sequence(a, s);
+        const int end = behind_sequence(a, s, first);
+        const int n = s < a.S && first ? items_of(a.cu[end] - a.cu[s], a.end[s] - a.begin[s], a.nh / a.nkv, tile_rows, chunk) : 0;
+        if (s < a.S) out[a.S + 1 + s] = end;
         int sum = n;
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) {
@@ -36,18 +39,35 @@ __global__ __launch_bounds__(1024) void cross_prefix_kernel(CrossArgs a, int til
 }
 
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
+// runs that follow one another and see the same keys, from s on: the first behind them.  The kernels work on them as on one: 16 continuations of a token each, four
+// to a prompt of 6400 keys, 16 heads of 64: 64 us one by one, 43 as four
+int behind(const CrossShape &c, int s) {
+    int e = s + 1;
+    while (e < c.S && e % 64 && c.begin[e] == c.begin[s] && c.end[e] == c.end[s]) ++e;
+    return e;
+}
+// f(first token, first behind, keys) for each such sequence
+template <typename F>
+void each_sequence(const CrossShape &c, F f) {
+    for (int s = 0, e; s < c.S; s = e) {
+        e = behind(c, s);
+        f(c.cu[s], c.cu[e], c.end[s] - c.begin[s]);
+    }
+}
+
+void order_runs(const CrossShape &c, CrossArgs &a) {
+    if (c.S > 64) return;
+    for (int s = 0; s < c.S; s = behind(c, s)) a.order[a.n_sequences++] = (uint8_t)s;
+    std::stable_sort(a.order, a.order + a.n_sequences, [&](uint8_t x, uint8_t y) { return c.end[x] - c.begin[x] > c.end[y] - c.begin[y]; });
+    for (int i = 0; i < a.n_sequences; ++i) a.last[i] = (uint8_t)(behind(c, a.order[i]) - 1);
+}
+
 int items(const CrossShape &c, int rows, int chunk) {
     int n = 0;
-    for (int s = 0; s < c.S; ++s) n += items_of(c.cu[s + 1] - c.cu[s], c.end[s] - c.begin[s], c.nh / c.nkv, rows, chunk);
+    each_sequence(c, [&](int c0, int c1, int keys) { n += items_of(c1 - c0, keys, c.nh / c.nkv, rows, chunk); });
     return n;
 }
 size_t part_bytes(const CrossShape &c) { return (size_t)c.Tk * 2 * c.nkv * c.d * sizeof(float); }
-
-void order_runs(const CrossShape &c, CrossArgs &a) {
-    const int n = c.S <= 64 ? c.S : 0;
-    for (int s = 0; s < 64; ++s) a.order[s] = (uint8_t)s;
-    std::stable_sort(a.order, a.order + n, [&](uint8_t x, uint8_t y) { return c.end[x] - c.begin[x] > c.end[y] - c.begin[y]; });
-}
 
 }  // namespace
 
@@ -57,20 +77,28 @@ CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
     auto count = [&](int rows, int chunk) { return (long)items(c, rows, chunk); };
     // steps of 32 rows and 32 keys
     long few = 0, many = 0, longest = 0;
-    for (int s = 0; s < c.S; ++s) {
-        const long keys = (c.end[s] - c.begin[s] + 31) / 32, rows = (long)(c.cu[s + 1] - c.cu[s]) * group;
+    each_sequence(c, [&](int c0, int c1, int n_keys) {
+        const long keys = (n_keys + 31) / 32, rows = (long)(c1 - c0) * group;
         few += (rows + 31) / 32 * keys;
         many += (rows + 127) / 128 * 4 * keys;
         longest = std::max(longest, keys);
-    }
+    });
     CrossPlan p = {};
     // Workgroups of 128 rows, two of which share a compute unit and cover each other's beginnings and ends, or of 256, which read keys half as often: where
     // a tile walks 64 steps of 64 keys and more on average.  us, 128 / 256 rows, heads of 128: 4096 tokens of 32 heads on 8 in one run of 8192 keys 524 / 492,
     // of 32 heads in four runs of 2304 175 / 184; of 80, 8 runs of 1024 38 / 42; of 64, 16 runs of 576 34 / 42.
     p.rows = dtype == DT_F32 ? 16 : many > 2 * few || count(128, 0) * c.nkv < 128 ? FEW_ROWS : c.d > 64 && many >= 512 * count(128, 0) ? 256 : 128;
-    if (p.rows <= FEW_ROWS && count(p.rows, 0) * c.nkv < 512 && longest > 32) {
-        const long want = std::max(few * c.nkv / 1024, 8l);      // blocks of 32 keys a workgroup
+    // Long walks of few rows are cut so that there are no more workgroups than fit on the chip at once (bf16: one per compute unit; where two rounds are needed anyway,
+    // two).  us, at most 256 / 512 / 1024 workgroups, one token a run: 16 runs of 6144 keys, 8 heads of 128 85 / 84 / 91; 5 of 4000 21 / 25 / 29; 48 that see 5000 keys,
+    // four in a row the same 60 / 62 / 70.  A chunk has 8 blocks of 32 keys at least (fp32: 4): one run of 4 heads of 128, 1152 keys, uncut / 16 / 8 / 4 blocks
+    // 13.1 / 12.7 / 11.2 / 10.7, 4600 keys 34.7 / 13.5 / 12.5 / 13.2; fp32, heads of 80, 1152 keys 26.6 / 19.0 / 13.7 / 12.3.  Shorter walks stay whole (uncut / cut: 1152
+    // keys of 64-wide heads 8.2 / 11.0, of 128 13.2 / 12.0).
+    const bool f32 = dtype == DT_F32;
+    const long uncut = count(p.rows, 0) * c.nkv;
+    if (p.rows <= FEW_ROWS && uncut < 512 && longest > (f32 ? 12 : c.d <= 64 ? 64 : 32)) {
+        const long most = f32 ? 1024 : uncut < 192 ? 256 : 512, want = std::max(few * c.nkv / most, f32 ? 4l : 8l);
         p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
+        while (p.chunk < longest * 32 && count(p.rows, p.chunk) * c.nkv > most) p.chunk += std::max(p.chunk / 16 / 128 * 128, 128);
         if (p.chunk >= longest * 32) p.chunk = 0;
     }
     p.items = (int)count(p.rows, p.chunk);
@@ -140,13 +168,13 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     // us, uncut / cut, the whole backward pass, one run of 8 heads of 128: 100 tokens, 768 keys 36 / 30, 2304 keys 79 / 32; 1500 tokens, 768 keys 53 / 55, 2304 keys
     // 113 / 91; fp32, heads of 64, 100 tokens, 2304 keys 86 / 66.
     long walk = 0, longest = 0;
-    for (int s = 0; s < c.S; ++s) {
-        const int n = items_of(c.cu[s + 1] - c.cu[s], 0, group, p.rows, 0);
-        const long keys = (c.end[s] - c.begin[s] + 63) / 64;
+    each_sequence(c, [&](int c0, int c1, int n_keys) {
+        const int n = items_of(c1 - c0, 0, group, p.rows, 0);
+        const long keys = (n_keys + 63) / 64;
         p.items += n;
         walk += n * keys;
         if (n) longest = std::max(longest, keys);
-    }
+    });
     if ((long)p.items * c.nkv < 256 && longest >= 12) {
         const long want = std::max(walk * c.nkv / 512, dtype == DT_F32 ? 2l : 4l);
         if (want < longest) {
@@ -164,7 +192,7 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     Piece pieces[MOST_PIECES];
     int n_pieces = 0;
     int at = 0;
-    auto blocks_of = [&](int s, int rows) { return ((long)(c.cu[s + 1] - c.cu[s]) * group + rows - 1) / rows; };
+    auto blocks_of = [&](int s, int rows) { return ((long)(c.cu[behind(c, s)] - c.cu[s]) * group + rows - 1) / rows; };
     auto cut = [&](int place) {
         const long n = (place - at + TILE_KEYS - 1) / TILE_KEYS;
         tiles += n;
@@ -173,19 +201,19 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
         at = place;
     };
     int b = 0, e = 0;
-    auto next = [&](int s) { while (s < c.S && c.begin[s] == c.end[s]) ++s; return s; };
+    auto next = [&](int s) { while (s < c.S && c.begin[s] == c.end[s]) s = behind(c, s); return s; };
     for (b = next(0), e = b; e < c.S;) {
         if (b < c.S && c.begin[b] <= c.end[e]) {
             cut(c.begin[b]);
             steps += blocks_of(b, STEP_ROWS);
             open += blocks_of(b, STEP_ROWS);
             open16 += blocks_of(b, 16);
-            b = next(b + 1);
+            b = next(behind(c, b));
         } else {
             cut(c.end[e]);
             open -= blocks_of(e, STEP_ROWS);
             open16 -= blocks_of(e, 16);
-            e = next(e + 1);
+            e = next(behind(c, e));
         }
     }
     cut(c.Tk);

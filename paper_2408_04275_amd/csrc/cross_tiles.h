@@ -40,6 +40,15 @@ struct Item {
     int index, first;           // the item's number within its run; of the run's first item among all
 };
 
+// Of the 64 runs from a multiple of 64 on, one per lane: is it the first that sees its keys, and which is the first behind those that see the same
+__device__ __forceinline__ bool first_of_sequence(const CrossArgs &a, int s) {
+    return (s & 63) == 0 || (s < a.S && (a.begin[s] != a.begin[s - 1] || a.end[s] != a.end[s - 1]));
+}
+__device__ __forceinline__ int behind_sequence(const CrossArgs &a, int s, bool first) {
+    const uint64_t firsts = __builtin_amdgcn_ballot_w64(first), later = firsts & (~0ull << (s & 63)) & ~(1ull << (s & 63));
+    return min((s & ~63) + (later ? __builtin_ctzll(later) : 64), a.S);
+}
+
 // Item y of all runs' items.  Up to 64 runs: one per lane, those with the most keys first (the workgroups that start last are then the
 // shortest), their items added up across the wavefront; more: from the table that cross_prefix_kernel left.
 __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_rows, int chunk) {
@@ -47,13 +56,13 @@ __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_ro
     Item it;
     if (a.S <= 64) {
         int c0 = 0, c1 = 0, lo = 0, hi = 0;
-        const int from = a.order[lane] * 4;                  // the lane's place, from the run of that number
+        const int from = a.order[lane] * 4, to = a.last[lane] * 4;       // the lane's place, from the runs of those numbers
         if (lane < a.S) { c0 = a.cu[lane]; c1 = a.cu[lane + 1]; lo = a.begin[lane]; hi = a.end[lane]; }
         c0 = __builtin_amdgcn_ds_bpermute(from, c0);
-        c1 = __builtin_amdgcn_ds_bpermute(from, c1);
+        c1 = __builtin_amdgcn_ds_bpermute(to, c1);
         lo = __builtin_amdgcn_ds_bpermute(from, lo);
         hi = __builtin_amdgcn_ds_bpermute(from, hi);
-        const int n = lane < a.S ? items_of(c1 - c0, hi - lo, group, tile_rows, chunk) : 0;
+        const int n = lane < a.n_sequences ? items_of(c1 - c0, hi - lo, group, tile_rows, chunk) : 0;
         const int sum = wave_scan(n);
         const int s = min(__popcll(__builtin_amdgcn_ballot_w64(sum <= y)), 63);
         it.q0 = __builtin_amdgcn_readlane(c0, s);
@@ -64,7 +73,7 @@ __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_ro
     } else {
         const int s = __builtin_amdgcn_readfirstlane(find_segment(a.prefix, a.S, y));
         it.q0 = __builtin_amdgcn_readfirstlane(a.cu[s]);
-        it.rows = (__builtin_amdgcn_readfirstlane(a.cu[s + 1]) - it.q0) * group;
+        it.rows = (__builtin_amdgcn_readfirstlane(a.cu[a.prefix[a.S + 1 + s]]) - it.q0) * group;
         it.lo = __builtin_amdgcn_readfirstlane(a.begin[s]);
         it.hi = __builtin_amdgcn_readfirstlane(a.end[s]);
         it.first = __builtin_amdgcn_readfirstlane(a.prefix[s]);
@@ -156,10 +165,10 @@ __device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool uppe
 // ---- dK, dV: what is walked ---------------------------------------------------------------------------------------------------
 // The runs that see something begin and end in their order; the others get the last one's beginning and end (nb, ne).  All those places
 // together, sorted, cut the keys into pieces (cuts, [2 S + 2]) whose keys are seen by the same runs, and these follow one another.  A tile is up to
-// 128 keys of a piece: {key, end of the piece, first step, steps}; a step up to 64 rows of a run: {token, head of the group, rows}.
+// 128 keys of a piece: {key, end of the piece, first step, steps}; a step up to 64 rows of a sequence of runs: {token, head of the group, rows}.
 // One workgroup makes both lists; it stands in front of dQ's, which do not need them.
 constexpr int PLAN_LDS_RUNS = 256;      // as many runs' places are kept in LDS while they are searched (more: in the workspace)
-constexpr int PLAN_INTS(int runs) { return 3 * (runs + 1) + 2 * (2 * runs + 2); }
+constexpr int PLAN_INTS(int runs) { return 4 * (runs + 1) + 2 * (2 * runs + 2); }
 constexpr int PLAN_SORTED = 1024;
 constexpr int PLAN_LDS = (PLAN_INTS(PLAN_LDS_RUNS) + 32 + PLAN_SORTED) * 4;
 template <int THREADS>
@@ -182,16 +191,19 @@ template <int THREADS>
 __device__ void make_plan(const CrossArgs &a, int *lds) {
     int *const sums = lds, *const carry = lds + 16;
     const int group = a.nh / a.nkv, S = a.S;
-    int *const nb = S <= PLAN_LDS_RUNS ? lds + 32 : a.plan, *const ne = nb + S + 1, *const first_step = ne + S + 1, *const cuts = first_step + S + 1,
+    int *const nb = S <= PLAN_LDS_RUNS ? lds + 32 : a.plan, *const ne = nb + S + 1, *const first_step = ne + S + 1, *const behind = first_step + S + 1, *const cuts = behind + S + 1,
         *const first_tile = cuts + 2 * S + 2;
     if (threadIdx.x < 3) carry[threadIdx.x] = 0;
     __syncthreads();
     for (int s0 = 0; s0 < S; s0 += THREADS) {
         const int s = s0 + threadIdx.x;
         int b = 0, e = 0, n = 0;
+        const bool first = first_of_sequence(a, s);
+        const int end = behind_sequence(a, s, first);
         if (s < S) {
-            const int lo = a.begin[s], hi = a.end[s], c0 = a.cu[s], c1 = a.cu[s + 1];
-            if (lo < hi) { b = lo; e = hi; n = ((c1 - c0) * group + STEP_ROWS - 1) / STEP_ROWS; }
+            const int lo = a.begin[s], hi = a.end[s], c0 = a.cu[s], c1 = a.cu[end];
+            if (lo < hi) { b = lo; e = hi; n = first ? ((c1 - c0) * group + STEP_ROWS - 1) / STEP_ROWS : 0; }
+            behind[s] = end;
         }
         b = max(block_scan<THREADS>(b, true, sums), carry[0]);
         e = max(block_scan<THREADS>(e, true, sums), carry[1]);
@@ -247,7 +259,7 @@ __device__ void make_plan(const CrossArgs &a, int *lds) {
     }
     for (int i = threadIdx.x; i < a.n_steps; i += THREADS) {
         const int s = find_segment(first_step, S, i), row = (i - first_step[s]) * STEP_ROWS, tok = row / group, c0 = a.cu[s];
-        a.steps[i] = make_int4(c0 + tok, row - tok * group, min((a.cu[s + 1] - c0) * group - row, STEP_ROWS), 0);
+        a.steps[i] = make_int4(c0 + tok, row - tok * group, min((a.cu[behind[s]] - c0) * group - row, STEP_ROWS), 0);
     }
 }
 
@@ -317,7 +329,7 @@ __global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossArgs a) {
     }
 }
 
-inline size_t table_bytes(int runs) { return ((size_t)(runs + 1) * sizeof(int) + 255) & ~size_t(255); }
+inline size_t table_bytes(int runs) { return ((size_t)(2 * runs + 1) * sizeof(int) + 255) & ~size_t(255); }
 
 }  // namespace
 

@@ -114,8 +114,10 @@ struct CrossArgs {
     void *dk; long lddk;
     void *dv; long lddv;
     float *D;                       // backward scratch [nh, Tq]: rowsum(dO * O)
-    uint8_t order[64];              // runs by falling number of keys, where there are at most 64
-    const int *prefix;              // first item of each run [S + 1], where there are more than 64 runs
+    // Runs that follow one another and see the same keys are worked on as one (within 64 runs from a multiple of 64 on)
+    uint8_t order[64], last[64];    // up to 64 runs: first and last of each such sequence, by falling number of keys
+    int n_sequences;
+    const int *prefix;              // more: first item of each run [S + 1], none of those behind a sequence's first; first run behind its sequence [S]
     int chunk;                      // keys of a workgroup; 0: all of its run's
     float *part; float2 *part_ml;   // partial results of the chunks [item, head][rows][d], their maxima and sums (forward)
     // dK and dV: see make_plan
