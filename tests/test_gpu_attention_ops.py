@@ -569,3 +569,127 @@ def test_cross_dispatch_from_two_streams_and_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(x, want[0][n]) for n, x in c.out.items()), i
         wf.fill_(i), wb.fill_(i)
+
+
+# ---- cross attention: the forms that a call takes ----------------------------------------------------------------------------
+@DTYPES
+def test_cross_gradients_of_few_rows_and_long_walks(dtype):
+    """dQ in chunks of keys: runs that have several, one or none; few keys and no keys among them; and without dQ."""
+    for nh, nkv, d in ((4, 2, 64), (3, 3, 80), (4, 1, 128)):
+        c = Cross(dtype, nh, nkv, d, runs([20, 1, 0, 7, 3], [1500, 60, 900, 0, 1031], tail=9), seed=40, pad=8).verify()
+        first = {n: t.clone() for n, t in c.out.items()}
+        for want in (("dq",), ("dk", "dv")):
+            for n in ("dq", "dk", "dv"):
+                c.out[n].fill_(5.0)
+            c.bwd(want)
+            assert all(torch.equal(c.out[n], first[n]) if n in want else torch.all(c.out[n] == 5.0) for n in ("dq", "dk", "dv"))
+    S = 70
+    lk = np.full(S, 3)
+    lk[[0, 40, 69]] = 1300, 900, 1100
+    Cross(dtype, 2, 1, 64, runs([1] * S, lk), seed=41).verify()
+
+
+@DTYPES
+@pytest.mark.parametrize("lq,lk,nh,nkv", [(900, 100, 8, 2), (700, 260, 4, 4), (333, 1, 6, 1)])
+def test_cross_gradients_of_many_rows_and_few_keys(dtype, lq, lk, nh, nkv):
+    """dK and dV of a tile from several workgroups (bf16)."""
+    for d in (64, 112):
+        Cross(dtype, nh, nkv, d, runs([lq, 5, lq // 2], [lk, 70, lk]), seed=lq + d).verify()
+    Cross(dtype, nh, nkv, 128, runs([lq, lq // 3, 64], [lk, lk, lk], "previous"), seed=lq).verify()
+
+
+def test_cross_fp32_gradients_of_short_runs():
+    """A wavefront for each 16 keys: pieces that end inside a workgroup's keys."""
+    rng = np.random.default_rng(42)
+    Cross(mm.F32, 16, 8, 64, runs(rng.integers(0, 7, 40), rng.integers(90, 160, 40), tail=70), seed=43).verify()
+    Cross(mm.F32, 8, 8, 80, runs(rng.integers(1, 4, 30), rng.integers(140, 180, 30), "previous", tail=3), seed=44).verify()
+
+
+@DTYPES
+@pytest.mark.parametrize("S,group", [(5, 5), (63, 7), (64, 64), (65, 65), (130, 9), (200, 200), (300, 3)])
+def test_cross_neighbouring_runs_with_the_same_keys(dtype, S, group):
+    """As many continuations of a prompt; some have no token."""
+    rng = np.random.default_rng(S)
+    shape = runs(rng.integers(0, 4, S), rng.integers(0, 300, -(-S // group)), "shared", group, tail=2)
+    Cross(dtype, 4, 2, 64, shape, seed=S).verify()
+    cu, begin, end, Tk = shape
+    begin, end = begin.copy(), end.copy()
+    begin[S // 2] = end[S // 2] = 0                    # one among them sees nothing
+    Cross(dtype, 2, 2, 128, (cu, begin, end, Tk), seed=S + 1).verify()
+    end[0] = begin[0]                                  # ... and the first
+    Cross(dtype, 2, 1, 80, (cu, begin, end, Tk), seed=S + 2).verify()
+
+
+@DTYPES
+@pytest.mark.parametrize("S", [255, 256, 257, 700, 1100])
+def test_cross_many_runs(dtype, S):
+    rng = np.random.default_rng(S)
+    Cross(dtype, 2, 1, 64, runs(rng.integers(0, 4, S), rng.integers(0, 20, S), tail=200), seed=S).verify()
+    Cross(dtype, 2, 2, 64, runs(rng.integers(0, 3, S), rng.integers(0, 9, S), "previous", 40), seed=S + 1).verify()
+
+
+@DTYPES
+def test_cross_more_tiles_than_are_sorted(dtype):
+    Cross(dtype, 2, 1, 64, runs([2, 1, 3], [45000, 60000, 30001], tail=400), seed=45).verify()
+
+
+def test_cross_forward_of_long_runs_of_rows_and_keys():
+    """Workgroups of 256 rows."""
+    Cross(mm.BF16, 64, 4, 128, runs([300, 1], [4200, 33]), seed=46).verify(back=False)
+
+
+@pytest.mark.parametrize("T", [15, 16, 17, 4095, 4096, 4097, 32767, 32768, 32769])
+def test_embed_where_its_order_and_chunks_change(T):
+    test_embed_long(T, 5000, 70)
+
+
+@pytest.mark.parametrize("T,H", [(1024, 4096), (1025, 4096), (2048, 2048), (2049, 2048), (16400, 2048)])
+def test_embed_chunks_of_wide_rows(T, H):
+    """Sums of small whole numbers, exact in fp32."""
+    rng = np.random.default_rng(T)
+    ids = torch.from_numpy(rng.integers(0, 40, T).astype(np.int32)).to("cuda")
+    dy = torch.from_numpy(rng.integers(-2, 3, (T, H)).astype(np.float32)).to("cuda", torch.bfloat16)
+    desc = mm.make_embed_desc(mm.BF16, H, 40, 0, 1.0)
+    wsb = mm.mmtrain_embed_workspace_bytes(desc, T)
+    ws, d_table = torch.full((wsb,), 0xA5, dtype=torch.uint8, device="cuda"), torch.empty((40, H), device="cuda")
+    check(mm.mmtrain_embed_bwd(desc, T, ids, dy, d_table, None, mm.BWD_WGRAD_F32, ws, wsb), "embed_bwd")
+    assert torch.equal(d_table, torch.zeros((40, H), device="cuda").index_add_(0, ids.long(), dy.float()))
+
+
+def test_embed_and_norms_in_a_graph():
+    """Captured and replayed with other tokens; eager calls with a workspace of their own in between."""
+    T, H, V, nq, nk, d = 5000, 256, 300, 2, 1, 64
+    gen = torch.Generator(device="cuda").manual_seed(47)
+    new = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    desc, norms, rope = mm.make_embed_desc(mm.BF16, H, V, 0, 1.0), mm.make_qk_norm_desc(mm.BF16, nq, nk, d), mm.make_rope_desc(mm.BF16, nq + nk, d)
+    batch = mm.PackedBatch.on_device(np.array([0, 4000, 5000], dtype=np.int32))
+    table, w = new(V, H), {"q_w": new(d), "k_w": new(d)}
+    ids, dy = torch.zeros(T, dtype=torch.int32, device="cuda"), new(T, H)
+    out = {"x": torch.empty_like(dy), "y": torch.zeros_like(dy), "dx": torch.zeros_like(dy), "table": torch.empty((V, H), device="cuda"),
+           "q_w": torch.empty(d, device="cuda"), "k_w": torch.empty(d, device="cuda")}
+    wsb = max(mm.mmtrain_embed_workspace_bytes(desc, T), mm.mmtrain_qk_norm_rope_workspace_bytes(norms, T))
+    spaces = [torch.full((wsb,), 0xA5, dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def call(ws):
+        cw = mm.make_qk_norm_weights(w)
+        check(mm.mmtrain_embed_fwd(desc, T, ids, table, None, out["x"]), "embed_fwd")
+        check(mm.mmtrain_qk_norm_rope_fwd(norms, rope, T, batch, None, cw, out["x"], H, out["y"], H), "fwd")
+        check(mm.mmtrain_qk_norm_rope_bwd(norms, rope, T, batch, None, cw, out["x"], H, dy, H, out["dx"], H, mm.make_qk_norm_grads({k: out[k] for k in w}), mm.BWD_WGRAD_F32,
+                                          ws, wsb), "bwd")
+        check(mm.mmtrain_embed_bwd(desc, T, ids, out["dx"], out["table"], None, mm.BWD_WGRAD_F32, ws, wsb), "embed_bwd")
+    call(spaces[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(spaces[0])
+    for i in range(4):
+        ids.copy_(torch.randint(-1, V + 1, (T,), generator=gen, device="cuda", dtype=torch.int32))
+        dy.copy_(new(T, H))
+        call(spaces[1])
+        torch.cuda.synchronize()
+        want = {k: t.clone() for k, t in out.items()}
+        for k in ("table", "q_w", "k_w", "x"):
+            out[k].fill_(float(i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, want[k]) for k, t in out.items()), i
