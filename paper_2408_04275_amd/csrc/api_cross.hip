@@ -36,10 +36,13 @@ int check_cross_batch(const mmtrain_cross_batch *b, bool ordered) {
     return MMTRAIN_OK;
 }
 
-// rows of a run and key/value head, log-sum-exps of a group: 32-bit numbers and byte offsets
+// rows of a run and key/value head, log-sum-exps of a group: 32-bit numbers and byte offsets; workgroups of up to 512 threads: fewer than 2^32 threads
 int check_sizes(const mmtrain_cross_attn_desc &d, const mmtrain_cross_batch &b) {
-    return (int64_t)b.q_tokens * (d.n_heads / d.n_kv_heads) > 1 << 28 || ((int64_t)b.q_tokens + b.n_segments) * d.n_heads > INT32_MAX ||
-           ((int64_t)b.kv_tokens / 16 + 16 * ((int64_t)b.n_segments + 1)) * d.n_kv_heads > INT32_MAX ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
+    const int64_t S = b.n_segments, most = ((int64_t)1 << 23) - 2;
+    const int rows = d.dtype == MMTRAIN_F32 ? 16 : 32, keys = d.dtype == MMTRAIN_F32 ? 16 : 128;
+    return (int64_t)b.q_tokens * (d.n_heads / d.n_kv_heads) > 1 << 28 || ((int64_t)b.q_tokens + S) * d.n_heads > INT32_MAX ||
+           (int64_t)b.q_tokens * d.n_heads / rows + S * d.n_kv_heads > most || (b.kv_tokens / keys + 128 / keys * (2 * S + 1)) * d.n_kv_heads > most
+               ? MMTRAIN_ERR_UNSUPPORTED : MMTRAIN_OK;
 }
 
 int check_rows(const mmtrain_cross_attn_desc &d, int heads, const void *p, int64_t ld) {

@@ -20,7 +20,7 @@ __device__ __forceinline__ int source_of(const EmbedArgs &a, int id) {
 template <typename T>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(EmbedArgs a) {
     const int chunks = a.H / 8;
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    const long i = ((long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
     if (i >= (long)a.T * chunks) return;
     const int t = (int)(i / chunks), c = (int)(i % chunks), src = source_of(a, a.ids[t]);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -325,10 +325,10 @@ constexpr int SUM_ROWS = 8;
 template <typename T, typename G>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s) {
     const int slabs = (a.H + s.columns - 1) / s.columns, none = a.vocab + a.features;
-    const int chunk = blockIdx.x / slabs;
+    const int block = blockIdx.y * gridDim.x + blockIdx.x, chunk = block / slabs;
     if (chunk >= s.chunks) {
         __shared__ int clear[64];
-        const int first = (a.accumulate || !a.d_table ? a.vocab : 0) + (blockIdx.x - s.chunks * slabs) * s.fill_rows;
+        const int first = (a.accumulate || !a.d_table ? a.vocab : 0) + (block - s.chunks * slabs) * s.fill_rows;
         const int rows = min(s.fill_rows, (a.d_rows ? none : a.vocab) - first);
         if ((int)threadIdx.x < rows) clear[threadIdx.x] = !is_named(s.key, a.T, first + threadIdx.x);
         __syncthreads();
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedSums s
         }
         return;
     }
-    const int column = (blockIdx.x % slabs) * s.columns + threadIdx.x * 8;
+    const int column = (block % slabs) * s.columns + threadIdx.x * 8;
     const bool live = column < a.H;
     const int c = live ? column : 0;                   // (a wavefront stays whole: its lanes hold the places)
     const int p0 = chunk * s.chunk, p1 = min(p0 + s.chunk, a.T), lane = threadIdx.x & 63;
@@ -461,12 +461,15 @@ int chunk_of(int T, int H) {
 size_t aligned(size_t n) { return (n + 255) & ~size_t(255); }
 int radix_blocks(int T) { return ceil_div(T, RADIX_BLOCK); }
 
+// a launch holds fewer than 2^32 threads along x
+dim3 rows_grid(long blocks) { return dim3((unsigned)std::min(blocks, 1l << 20), (unsigned)((blocks + (1l << 20) - 1) >> 20)); }
+
 template <typename T, typename G>
 hipError_t sums(const EmbedArgs &a, const EmbedSums &s, hipStream_t st) {
     const int threads = std::min(256, (a.H / 8 + 63) / 64 * 64), slabs = ceil_div(a.H, s.columns);
     const int first = a.accumulate || !a.d_table ? a.vocab : 0, rows = (a.d_rows ? a.vocab + a.features : a.vocab) - first;
     const int blocks = s.chunks * slabs + ceil_div(rows, s.fill_rows);
-    if (blocks) embed_sum_kernel<T, G><<<blocks, threads, 0, st>>>(a, s);
+    if (blocks) embed_sum_kernel<T, G><<<rows_grid(blocks), threads, 0, st>>>(a, s);
     if (s.chunks > 1) embed_join_kernel<T, G><<<s.chunks * ceil_div(a.H, JOIN_COLUMNS), 256, 0, st>>>(a, s);
     return blocks ? hipGetLastError() : hipSuccess;
 }
@@ -475,7 +478,7 @@ hipError_t sums(const EmbedArgs &a, const EmbedSums &s, hipStream_t st) {
 
 hipError_t embed_fwd(int dtype, const EmbedArgs &a, hipStream_t st) {
     if (a.T == 0) return hipSuccess;
-    const int grid = ceil_div((long)a.T * (a.H / 8), 256);
+    const dim3 grid = rows_grid(((long)a.T * (a.H / 8) + 255) / 256);
     if (dtype == DT_F32) embed_fwd_kernel<float><<<grid, 256, 0, st>>>(a);
     else embed_fwd_kernel<bf16_t><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();

@@ -239,3 +239,19 @@ def test_cross_attention_refuses_more():
     d = mm.make_cross_attn_desc(**CROSS)
     assert mm.mmtrain_cross_attn_workspace_bytes(d, cross_batch(), 1) > 0 and mm.mmtrain_cross_attn_workspace_bytes(None, cross_batch(), 1) == 0
     assert mm.mmtrain_cross_attn_workspace_bytes(d, empty, 0) > 0
+
+
+@pytest.mark.parametrize("dtype,tokens,kv_tokens,nh,nkv,S,status", [
+    (mm.BF16, 1 << 22, 9, 64, 64, 1, UNSUP), (mm.BF16, (1 << 22) - 64, 9, 64, 64, 1, mm.OK), (mm.F32, 1 << 21, 9, 64, 64, 1, UNSUP), (mm.F32, (1 << 21) - 64, 9, 64, 64, 1, mm.OK),
+    (mm.BF16, 8, 1 << 30, 1, 1, 1, UNSUP), (mm.BF16, 8, (1 << 30) - 1024, 1, 1, 1, mm.OK), (mm.F32, 8, 1 << 27, 1, 1, 1, UNSUP), (mm.BF16, 65536, 9, 128, 128, 65536, UNSUP),
+    (mm.BF16, 65536, 9, 32, 32, 65536, mm.OK)])
+def test_cross_attention_calls_that_no_launch_holds(dtype, tokens, kv_tokens, nh, nkv, S, status):
+    """2^32 threads; the workspace's size is 0 where a call would be refused."""
+    b = mm.CrossBatch(np.linspace(0, tokens, S + 1).astype(np.int64), np.zeros(S, np.int64), np.full(S, 9), kv_tokens, FAKE, FAKE, FAKE)
+    d = mm.make_cross_attn_desc(dtype, nh, nkv, 16)
+    for back in (0, 1):
+        assert (mm.mmtrain_cross_attn_workspace_bytes(d, b, back) > 0) == (status == mm.OK)
+    if status != mm.OK:
+        t = mm.CrossAttnTensors(q=FAKE, ld_q=nh * 16, k=2 * FAKE, ld_k=nkv * 16, v=3 * FAKE, ld_v=nkv * 16, o=4 * FAKE, ld_o=nh * 16, lse=FAKE)
+        g = mm.CrossAttnGrads(d_o=6 * FAKE, ld_do=nh * 16, d_q=7 * FAKE, ld_dq=nh * 16, d_k=8 * FAKE, ld_dk=nkv * 16, d_v=9 * FAKE, ld_dv=nkv * 16)
+        assert mm.mmtrain_cross_attn_fwd(d, b, t, 5 * FAKE, 1 << 40, 0) == status and mm.mmtrain_cross_attn_bwd(d, b, t, g, 5 * FAKE, 1 << 40, 0) == status

@@ -693,3 +693,32 @@ def test_embed_and_norms_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(t, want[k]) for k, t in out.items()), i
+
+
+def test_embed_of_more_workgroups_than_a_launch_has_along_x():
+    # rows to clear, 16 to a workgroup, behind 2^20 workgroups; rows written from more than 2^28 pieces
+    V = (1 << 24) + 5000
+    ids = torch.tensor([V - 1, 3, V - 1, 1 << 24], dtype=torch.int32, device="cuda")
+    desc = mm.make_embed_desc(mm.BF16, 8, V, 0, 1.0)
+    dy, d_table = torch.ones((4, 8), dtype=torch.bfloat16, device="cuda"), torch.full((V, 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wsb = mm.mmtrain_embed_workspace_bytes(desc, 4)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    check(mm.mmtrain_embed_bwd(desc, 4, ids, dy, d_table, None, 0, ws, wsb), "embed_bwd")
+    assert float(d_table.float().sum()) == 32.0 and torch.all(d_table[V - 1] == 2) and torch.all(d_table[3] == 1) and torch.all(d_table[1 << 24] == 1)
+    T, H, V = 140000, 16384, 50
+    ids = torch.arange(T, dtype=torch.int32, device="cuda") % V
+    table, y = torch.randn((V, H), device="cuda").to(torch.bfloat16), torch.zeros((T, H), dtype=torch.bfloat16, device="cuda")
+    check(mm.mmtrain_embed_fwd(mm.make_embed_desc(mm.BF16, H, V, 0, 1.0), T, ids, table, None, y), "embed_fwd")
+    assert torch.equal(y.view(-1, V, H), table.expand(T // V, V, H))
+
+
+@pytest.mark.parametrize("nq,nk", [(2, 1), (0, 1), (3, 0)])
+def test_qk_norm_no_tokens_writes_zero_gradients(nq, nk):
+    w = {k + "_w": torch.ones(64, device="cuda") for k, n in (("q", nq), ("k", nk)) if n}
+    desc = mm.make_qk_norm_desc(mm.F32, nq, nk, 64)
+    wsb = mm.mmtrain_qk_norm_rope_workspace_bytes(desc, 0)
+    ws = torch.full((wsb,), 0xA5, dtype=torch.uint8, device="cuda")
+    for flags, want in ((0, 0.0), (mm.BWD_ACCUMULATE_WGRAD, 3.0)):
+        grads = {k: torch.full((64,), 3.0, device="cuda") for k in w}
+        check(mm.mmtrain_qk_norm_rope_bwd(desc, None, 0, None, None, mm.make_qk_norm_weights(w), None, 512, None, 512, None, 512, mm.make_qk_norm_grads(grads), flags, ws, wsb), "bwd")
+        assert all(torch.all(t == want) for t in grads.values())
