@@ -145,8 +145,9 @@ __device__ __forceinline__ void get_gains(const float *g, const Place<V, LANES> 
     for (int i = 0; i < V; ++i) { lo[i] = g[p.o0 + i]; hi[i] = g[p.o1 + i]; }
 }
 
-// The (token, head) pairs of a tile that a group of threads has, one after the other; behind the last it stays at a pair that exists, so that
-// a load ahead needs no branch (with one the compiler waits for all loads on their way in each turn).
+// The (token, head) pairs of a tile that a group of threads has, one after the other; behind the last a load ahead takes the gains, so that
+// it needs no branch (with one the compiler waits for all loads on their way in each turn) and no memory (a pair of the tile once more: HBM reads an eighth
+// to a quarter more, as rows that have been read do not stay in the cache).
 struct Walk {
     int tok, head, tokens, heads, step_tokens, step_heads;
     __device__ __forceinline__ Walk(int g, int groups, int tokens_, int heads_)
@@ -156,7 +157,10 @@ struct Walk {
         tok += step_tokens; head += step_heads;
         if (head >= heads) { head -= heads; ++tok; }
     }
-    __device__ __forceinline__ long row() const { return min(tok, tokens - 1); }
+    // the pair's features in rows ld apart, x being the tile's first; or d others
+    template <typename T> __device__ __forceinline__ const T *at(const T *x, long ld, int d, const void *others) const {
+        return live() ? x + tok * ld + (long)head * d : (const T *)others;
+    }
 };
 
 // The first heads' rows are requested in front of everything else, and the next ones' in front of each turn's arithmetic, into the other of
@@ -173,7 +177,7 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a, QkShape 
     const Place<V, LANES> p(s, r.half, u);
     const float inv_d = 1.f / r.d;
     Walk w(threadIdx.x / lanes, 256 / lanes, tokens, r.heads);
-    auto request = [&](Pair<T, V, LANES> &to) { to.load((const T *)r.x + (t0 + w.row()) * r.ldx + (long)w.head * r.d, p); };
+    auto request = [&](Pair<T, V, LANES> &to) { to.load(w.at((const T *)r.x + t0 * r.ldx, r.ldx, r.d, a.nq ? a.q_w : a.k_w), p); };
     auto turn = [&](const Pair<T, V, LANES> &now, Pair<T, V, LANES> &next) {
         T *const y = (T *)r.y + (t0 + w.tok) * r.ldy + (long)w.head * r.d;
         const float2 *cs = turned + w.tok * r.half;
@@ -235,8 +239,9 @@ __global__ __launch_bounds__(BWD_THREADS<LAYER>, LAYER ? 3 : 4) void qk_norm_bwd
         Walk w(g, groups, tokens, heads);
         struct Rows { Pair<T, V, LANES> x, d; } even, odd;
         auto request = [&](Rows &to) {
-            to.x.load((const T *)r.x + (t0 + w.row()) * r.ldx + (long)(h0 + w.head) * r.d, p);
-            to.d.load((const T *)a.dy + (t0 + w.row()) * a.lddy + (long)(h0 + w.head) * r.d, p);
+            const void *const others = kind ? a.k_w : a.q_w;
+            to.x.load(w.at((const T *)r.x + t0 * r.ldx + (long)h0 * r.d, r.ldx, r.d, others), p);
+            to.d.load(w.at((const T *)a.dy + t0 * a.lddy + (long)h0 * r.d, a.lddy, r.d, others), p);
         };
         auto turn = [&](const Rows &now, Rows &next) {
             const float2 *cs = turned + w.tok * r.half;

@@ -5,6 +5,9 @@
     python -m paper_2408_04275_amd.opbench rope --config 3 [--interleaved] [--rot 64]
     python -m paper_2408_04275_amd.opbench join --config 3 [--post rms] [--pre rms] [--gate none]
     python -m paper_2408_04275_amd.opbench clip --config 3 --layers 1 [--dtype f32]
+    python -m paper_2408_04275_amd.opbench embed --config 3 [--vocab 32768] [--main]
+    python -m paper_2408_04275_amd.opbench qknorm --config 3 [--rot 64] [--norm layer]
+    python -m paper_2408_04275_amd.opbench cross --config 3 [--kv 1152] [--tokens 1]
     python -m paper_2408_04275_amd.opbench copy --mb 512          (a plain copy kernel, for counter calibration)
 
 Prints one JSON line per run.  Meant to be run alone or under rocprofv3 (kernel trace or --pmc).
@@ -178,6 +181,78 @@ def bench_clip(a):
     print(json.dumps(out))
 
 
+def bench_embed(a):
+    """A workload's pack through a table of `vocab` rows, its images' rows from an encoder's output; and the gradients of both."""
+    shape = wl.SHAPES[a.config]
+    cu, _, kinds = wl.make_segments(a.config, wl.longtail_seed() if a.config == 4 else 0)
+    T, H = int(cu[-1]), shape.hidden
+    image = np.repeat([k == "image" for k in kinds], np.diff(cu))
+    F = int(image.sum())
+    ids = np.random.default_rng(0).integers(0, a.vocab, T)
+    ids[image] = -1 - np.arange(F)
+    ids = torch.from_numpy(ids.astype(np.int32)).to("cuda")
+    desc = mm.make_embed_desc(mm.BF16, H, a.vocab, F, 1.0)
+    table, dy = (torch.randn((n, H), device="cuda").to(torch.bfloat16) for n in (a.vocab, T))
+    feats = torch.randn((F, H), device="cuda").to(torch.bfloat16) if F else None
+    y, d_feats = torch.empty_like(dy), torch.empty_like(feats) if F else None
+    d_table = torch.zeros((a.vocab, H), device="cuda", dtype=torch.float32 if a.main else torch.bfloat16)
+    flags = mm.BWD_WGRAD_F32 | mm.BWD_ACCUMULATE_WGRAD if a.main else 0
+    wsb = mm.mmtrain_embed_workspace_bytes(desc, T)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    ms_f = _time(lambda: check(mm.mmtrain_embed_fwd(desc, T, ids, table, feats, y), "embed fwd"), a.iters)
+    ms_b = _time(lambda: check(mm.mmtrain_embed_bwd(desc, T, ids, dy, d_table, d_feats, flags, ws, wsb), "embed bwd"), a.iters)
+    touched = len(torch.unique(ids[ids >= 0]))
+    bytes_b = 2 * (T + F) * H + (8 * touched * H if a.main else 2 * a.vocab * H)
+    print(json.dumps({"op": "embed", "config": a.config, "T": T, "hidden": H, "vocab": a.vocab, "features": F, "main": a.main, "fwd_ms": ms_f, "bwd_ms": ms_b,
+                      "fwd_GBps": 4 * T * H / ms_f / 1e6, "bwd_GBps": bytes_b / ms_b / 1e6}))
+
+
+def bench_qknorm(a):
+    """Norms of a workload's query and key heads with their rotation, out of its packed qkv, and back with the gains' gradients."""
+    shape, cu = wl.SHAPES[a.config], _segments(a.config)
+    T, d, nq, nk = int(cu[-1]), shape.head_dim, shape.n_heads, shape.n_kv_heads
+    batch = mm.PackedBatch.on_device(cu)
+    desc = mm.make_qk_norm_desc(mm.BF16, nq, nk, d, mm.NORM_LAYER if a.norm == "layer" else mm.NORM_RMS)
+    rope = mm.make_rope_desc(mm.BF16, nq + nk, d, a.rot) if a.rot != 0 else None
+    x, y, dy, dx = (torch.randn((T, shape.nqkv), device="cuda").to(torch.bfloat16) for _ in range(4))
+    w = {k: torch.ones(d, device="cuda", dtype=torch.bfloat16) for k in mm.QK_NORM_FIELDS if a.norm == "layer" or k.endswith("_w")}
+    grads = {k: torch.empty(d, device="cuda") for k in w}
+    cw, cg = mm.make_qk_norm_weights(w), mm.make_qk_norm_grads(grads)
+    wsb = mm.mmtrain_qk_norm_rope_workspace_bytes(desc, T)
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    ld = shape.nqkv
+    ms_f = _time(lambda: check(mm.mmtrain_qk_norm_rope_fwd(desc, rope, T, batch, None, cw, x, ld, y, ld), "qk norm fwd"), a.iters)
+    ms_b = _time(lambda: check(mm.mmtrain_qk_norm_rope_bwd(desc, rope, T, batch, None, cw, x, ld, dy, ld, dx, ld, cg, mm.BWD_WGRAD_F32, ws, wsb), "qk norm bwd"), a.iters)
+    row = 2 * T * (nq + nk) * d
+    print(json.dumps({"op": "qknorm", "config": a.config, "T": T, "heads": nq + nk, "head_dim": d, "rot_dim": rope.rot_dim if rope else 0, "norm": a.norm, "fwd_ms": ms_f,
+                      "bwd_ms": ms_b, "fwd_GBps": 2 * row / ms_f / 1e6, "bwd_GBps": 3 * row / ms_b / 1e6}))
+
+
+def bench_cross(a):
+    """A workload's heads; each segment of its pack (or `tokens` of it) attends to `kv` encoder states of its own."""
+    shape, cu = wl.SHAPES[a.config], _segments(a.config)
+    S = len(cu) - 1
+    if a.tokens:
+        cu = np.arange(S + 1) * a.tokens
+    T, d, nh, nkv = int(cu[-1]), shape.head_dim, shape.n_heads, shape.n_kv_heads
+    at = np.arange(S + 1) * a.kv
+    batch = mm.CrossBatch.on_device(cu, at[:-1], at[1:], int(at[-1]))
+    desc = mm.make_cross_attn_desc(mm.BF16, nh, nkv, d)
+    q, o, do, dq = (torch.randn((T, nh * d), device="cuda").to(torch.bfloat16) for _ in range(4))
+    kv, dkv = (torch.randn((int(at[-1]), 2 * nkv * d), device="cuda").to(torch.bfloat16) for _ in range(2))
+    lse = torch.empty((nh, T), device="cuda")
+    n = nkv * d
+    t = mm.make_cross_attn_tensors(q, kv[:, :n], kv[:, n:], o, lse)
+    g = mm.make_cross_attn_grads(do, dq, dkv[:, :n], dkv[:, n:])
+    wsb = [mm.mmtrain_cross_attn_workspace_bytes(desc, batch, b) for b in (0, 1)]
+    ws = torch.empty(max(wsb), dtype=torch.uint8, device="cuda")
+    ms_f = _time(lambda: check(mm.mmtrain_cross_attn_fwd(desc, batch, t, ws, wsb[0]), "cross fwd"), a.iters)
+    ms_b = _time(lambda: check(mm.mmtrain_cross_attn_bwd(desc, batch, t, g, ws, wsb[1]), "cross bwd"), a.iters)
+    flops = 4.0 * T * a.kv * nh * d
+    print(json.dumps({"op": "cross", "config": a.config, "T": T, "runs": S, "kv": a.kv, "heads": nh, "kv_heads": nkv, "head_dim": d, "fwd_ms": ms_f, "bwd_ms": ms_b,
+                      "fwd_tflops": flops / ms_f / 1e9, "bwd_tflops": 2.5 * flops / ms_b / 1e9, "fwd_kv_GBps": 4 * int(at[-1]) * n / ms_f / 1e6}))
+
+
 def bench_copy(a):
     n = a.mb * (1 << 20)
     src = torch.empty(n, dtype=torch.uint8, device="cuda").fill_(1)
@@ -220,12 +295,28 @@ def main(argv=None):
     cl.add_argument("--layers", type=int, default=1)
     cl.add_argument("--dtype", default="f32", choices=["f32", "bf16"])
     cl.add_argument("--iters", type=int, default=20)
+    e = sub.add_parser("embed")
+    e.add_argument("--config", type=int, default=3)
+    e.add_argument("--vocab", type=int, default=32768)
+    e.add_argument("--main", action="store_true", help="the table's gradient is added to an fp32 buffer (default: written as bf16)")
+    e.add_argument("--iters", type=int, default=20)
+    q = sub.add_parser("qknorm")
+    q.add_argument("--config", type=int, default=3)
+    q.add_argument("--rot", type=int, default=None, help="rotated features of a head (default: all; 0: no rotation)")
+    q.add_argument("--norm", default="rms", choices=["rms", "layer"])
+    q.add_argument("--iters", type=int, default=20)
+    x = sub.add_parser("cross")
+    x.add_argument("--config", type=int, default=3)
+    x.add_argument("--kv", type=int, default=1152, help="encoder states that a run sees (two images of 576)")
+    x.add_argument("--tokens", type=int, default=0, help="tokens a run (default: the workload's segments)")
+    x.add_argument("--iters", type=int, default=20)
     c = sub.add_parser("copy")
     c.add_argument("--mb", type=int, default=512)
     c.add_argument("--iters", type=int, default=10)
     a = ap.parse_args(argv)
     mm.load_library()
-    {"gemm": bench_gemm, "attn": bench_attn, "copy": bench_copy, "adam": bench_adam, "rope": bench_rope, "join": bench_join, "clip": bench_clip}[a.op](a)
+    {"gemm": bench_gemm, "attn": bench_attn, "copy": bench_copy, "adam": bench_adam, "rope": bench_rope, "join": bench_join, "clip": bench_clip,
+     "embed": bench_embed, "qknorm": bench_qknorm, "cross": bench_cross}[a.op](a)
 
 
 if __name__ == "__main__":
