@@ -309,9 +309,10 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
 }
 
 // dK_j = scale * sum_i dS_ij q_i,   dV_j = sum_i P_ij dO_i over the rows i of the runs that see the keys
-// OWN: each wavefront has 16 keys to itself and walks all rows, without LDS
+// OWN: each wavefront has 16 keys to itself and walks all rows, without LDS; up to 64 features three wavefronts a SIMD (us, left to the compiler / three: 1000 rows
+// of 16 heads in eight runs of 1000 keys 147 / 136, 294 in runs that see 29760 keys 178 / 164; with 80 features 51.5 / 55).
 template <int KB, int NW, bool OWN>
-__global__ __launch_bounds__(64 * NW) void cross_f32_dkv_kernel(CrossArgs a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OWN && KB <= 4 ? 3 : 1, OWN && KB <= 4 ? 3 : 8))) void cross_f32_dkv_kernel(CrossArgs a) {
     __shared__ __attribute__((aligned(16))) std::conditional_t<OWN, int, Partials<KB, NW>> part;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = ((threadIdx.x & 48) >> 4) * 4;
     const int head = blockIdx.x % a.nkv, dh = a.d, block = blockIdx.x / a.nkv;
