@@ -48,6 +48,8 @@ __device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[C
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 // Four wavefronts of 32 rows, two workgroups a compute unit (eight and one are nowhere faster: us, 128 / 256 rows, both backward kernels: 4096 tokens of 32 heads
 // of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284).
+// 8192 tokens of 32 heads of 128 in 12 runs of 1152 keys 250 us (0.64 PFLOP/s): Q, dO, O and dQ alone take 47 (5.7 TB/s), a step of 64 keys of both workgroups 2.6 (1.24 PFLOP/s),
+// bound by the matrix cores.  Q and dO on their way together instead of one after the other, and tiles of 32 keys: no difference.
 // LDS: two slots of a K and a V tile; the Q, dO and O rows stand in the second slot, one after the other.
 template <int D> constexpr int DQ_LDS = 2 * 2 * KEYS * D * 2;
 
@@ -203,7 +205,9 @@ __device__ __forceinline__ void store_dkv(const CrossArgs &a, uint8_t *smem, int
 
 // ---- dK, dV for heads wider than 64 features ----------------------------------------------------------------------------------
 // As in attn_mfma.hip: 32 keys belong to a pair of wavefronts on one SIMD, of which the first turns 32 rows at a time into P and dS
-// and the second adds dO^T P and Q^T dS, one block behind; P and dS go through LDS, rows round three slots of 64.
+// and the second adds dO^T P and Q^T dS, one block behind; P and dS go through LDS, rows round three slots of 64.  The same pack as above 375 us (0.56 PFLOP/s):
+// 2 us a step (1.08 PFLOP/s), bound by the matrix cores, and 5 us at the beginning and end of each of a compute unit's 14 tiles, with nothing beside it (LDS holds one
+// workgroup).
 template <int D> constexpr int DKV_SLOT = 2 * STEP_ROWS * D * 2 + 2 * STEP_ROWS * 4;        // Q tile, dO tile, lse[64], D[64]
 constexpr int PDS_BYTES = 4 * 1024;                                                        // P and dS of one block of one pair
 template <int D> constexpr int DKV_PAIR_LDS = 3 * DKV_SLOT<D> + 2 * 4 * PDS_BYTES;

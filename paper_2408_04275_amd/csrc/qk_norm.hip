@@ -2,8 +2,9 @@
 //
 // A head belongs to a group of `lanes` threads of one wavefront (a power of two), each of which holds two chunks of V elements as in
 // rope.hip: features that rotate with one another, so that only the head's sums go across lanes.  A workgroup takes whole tokens: first the
-// rotations of its tokens go into LDS (an angle in fp64 each, reduced to a turn), then its threads walk over the query heads and then over the
-// key heads, a kind's gains in registers.
+// rotations of its tokens go into LDS (an angle in fp64 each, reduced to a turn), then its threads walk over the heads: forward over all, the gains in LDS, backward over those of
+// one kind, its gains in registers.  Bound by memory: 16411 tokens of 72 heads of 128, LayerNorm, 120 us (5.0 TB/s), back 8192 of 64, RMSNorm, 86 (4.7) and 4 for the
+// sums of the partial gains.
 #include "ops.h"
 #include "chunk.h"
 #include <algorithm>
