@@ -19,7 +19,7 @@ __device__ __forceinline__ void copy_rows_part(const bf16_t *p, long ld, int dh,
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int row = (first + i) * PER + lrow, unit = pos ^ swz_unit<D>(row);
-        const uint32_t off = row < at.left && unit * 8 < dh ? (at.offset(g, row, ld, dh) + unit * 8) * 2u : 0x80000000u;
+        const uint32_t there = (at.offset(g, row, ld, dh) + unit * 8) * 2u, off = row < at.left && unit * 8 < dh ? there : 0x80000000u;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(tile + (first + i) * PER * 2 * D), 16, (int)off, 0, 0, 0);
     }
 }
@@ -37,11 +37,18 @@ __device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[C
             *reinterpret_cast<f32x4 *>(stage + l32 * RS + (32 * c + 8 * gq + 4 * half) * 4) =
                 f32x4{acc[c][4 * gq], acc[c][4 * gq + 1], acc[c][4 * gq + 2], acc[c][4 * gq + 3]};
     const int r0 = lane / LPR, cb = (lane % LPR) * 4;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(dst, 0, 0x7fff0000, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i) {
-        const int r = i * RPI + r0;
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(stage + r * RS + cb * 4);
-        if (r < rows && cb < dh) *reinterpret_cast<f32x4 *>(dst + (long)r * ld + cb) = v;
+    for (int i0 = 0; i0 < 32 / RPI; i0 += 8) {
+        u32x4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const u32x4 *>(stage + ((i0 + i) * RPI + r0) * RS + cb * 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (i0 + i) * RPI + r0;
+            const uint32_t off = (uint32_t)(r * (int)ld + cb) * 4u;
+            __builtin_amdgcn_raw_buffer_store_b128(v[i], rs, (int)(r < rows && cb < dh ? off : 0x80000000u), 0, 0);
+        }
     }
 }
 

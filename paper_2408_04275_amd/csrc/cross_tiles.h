@@ -82,13 +82,14 @@ __device__ __forceinline__ Item find_item(const CrossArgs &a, int y, int tile_ro
     return it;
 }
 
-// Division of a small number (below group + 128) by the group: a product's high half (exact while number * group < 2^32)
+// Division of a small number (below group + 128) by the group: the high half of a product with ceil(2^31 / group), exact while number * group < 2^31, for
+// every group (a case of its own for groups of one becomes a branch at each row)
 struct Group {
     int n;
     uint32_t magic;
-    __device__ __forceinline__ explicit Group(int n_) : n(n_), magic(0xffffffffu / (uint32_t)n_ + 1u) {}
+    __device__ __forceinline__ explicit Group(int n_) : n(n_), magic((0x80000000u + (uint32_t)n_ - 1u) / (uint32_t)n_) {}
     __device__ __forceinline__ explicit Group(const CrossArgs &a) : Group(a.nh / a.nkv) {}
-    __device__ __forceinline__ int token(int r) const { return n == 1 ? r : (int)__umulhi((uint32_t)r, magic); }
+    __device__ __forceinline__ int token(int r) const { return (int)__umulhi((uint32_t)r * 2u, magic); }
 };
 
 // 32 rows of a run from row0 on: row i is token t + token(j + i), head of the group (j + i) % group
@@ -123,7 +124,7 @@ __device__ __forceinline__ void copy_rows(const bf16_t *p, long ld, int dh, cons
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int row = i * PER + lrow, unit = pos ^ swz_unit<D>(row);
-        const uint32_t off = row < at.left && unit * 8 < dh ? (at.offset(g, row, ld, dh) + unit * 8) * 2u : 0x80000000u;
+        const uint32_t there = (at.offset(g, row, ld, dh) + unit * 8) * 2u, off = row < at.left && unit * 8 < dh ? there : 0x80000000u;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)(to + i * PER * 2 * D), 16, (int)off, 0, 0, 0);
     }
 }
@@ -143,12 +144,17 @@ __device__ __forceinline__ void store_rows_at(uint8_t *stage, const f32x16 (&acc
             *reinterpret_cast<uint2 *>(stage + l32 * RS + (32 * c + 8 * gq + 4 * half) * 2) = w;
         }
     const int r0 = lane / LPR, cb = (lane % LPR) * 8;
-    bf16_t *const first = p + at.t * ld;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(p + at.t * ld, 0, 0x7fff0000, 0x00020000);
+    Rows here = at;
+    asm volatile("" : "+s"(here.j));                   // (offsets kept from the copies in front of the walk would fill its registers)
+    u32x4 v[32 / RPI];
 #pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i) {
+    for (int i = 0; i < 32 / RPI; ++i) v[i] = *reinterpret_cast<const u32x4 *>(stage + (i * RPI + r0) * RS + cb * 2);
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {               // (rows that do not exist are behind the buffer's end: a branch each would make every read wait for the store in front)
         const int r = i * RPI + r0;
-        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * RS + cb * 2);
-        if (r < at.left && cb < dh) *reinterpret_cast<uint4 *>(first + at.offset(g, r, ld, dh) + cb) = v;
+        const uint32_t off = (here.offset(g, r, ld, dh) + cb) * 2u;
+        __builtin_amdgcn_raw_buffer_store_b128(v[i], rs, (int)(r < at.left && cb < dh ? off : 0x80000000u), 0, 0);
     }
 }
 
