@@ -69,9 +69,13 @@ __device__ __forceinline__ Block row_block(const float *p, long ld, int dh, cons
     Block b;
     b.rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(p + at.t * ld), 0, 0x7fff0000, 0x00020000);
     const int x = threadIdx.x & 15, q4 = ((threadIdx.x & 48) >> 4) * 4;
-    b.row = x < at.left ? at.offset(g, x, ld, dh) * 4u : NO_ROW;
+    const uint32_t row = at.offset(g, x, ld, dh) * 4u;
+    b.row = x < at.left ? row : NO_ROW;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b.quad[j] = q4 + j < at.left ? at.offset(g, q4 + j, ld, dh) * 4u : NO_ROW;
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t quad = at.offset(g, q4 + j, ld, dh) * 4u;
+        b.quad[j] = q4 + j < at.left ? quad : NO_ROW;
+    }
     return b;
 }
 
@@ -248,12 +252,13 @@ __global__ __launch_bounds__(256) void cross_f32_combine_kernel(CrossArgs a) {
     }
 }
 
-// 1031 tokens of 16 heads of 80 in five runs of 420 keys: dQ 47 us, dK and dV 78, a third of the matrix rate.  Larger packs reach 60 and 42 % of it: each operand
-// is loaded by the wavefront that uses it, twice where it is a row of both products, in several rounds of loads and waits an iteration; more registers for loads ahead leave fewer
+// 1031 tokens of 16 heads of 80 in five runs of 420 keys: dQ 47 us, dK and dV 63, two fifths of the matrix rate; larger packs reach 60 % of it.  Each operand is loaded by the
+// wavefront that uses it, twice where it is a row of both products, in several rounds of loads and waits an iteration; more registers for loads ahead leave fewer
 // wavefronts (dQ 50 us).
+// Four wavefronts a SIMD (left to the compiler 1 to 10 % slower: 294 rows of 16 heads of 64 in runs that see 29760 keys 110 -> 99 us).
 // dQ_i = scale * sum_j dS_ij k_j,  dS_ij = P_ij (dO_i . v_j - D_i),  D_i = dO_i . O_i (kept in a.D),  P_ij = exp(s_ij - lse_i)
 template <int KB, int NW>
-__global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(KB <= 5 ? 4 : 1, KB <= 5 ? 4 : 8))) void cross_f32_dq_kernel(CrossArgs a) {
     __shared__ __attribute__((aligned(16))) union { Partials<KB, NW> part; int plan[PLAN_LDS / 4]; } lds;
     Partials<KB, NW> &part = lds.part;
     int block = blockIdx.x;
@@ -313,7 +318,7 @@ __global__ __launch_bounds__(64 * NW) void cross_f32_dq_kernel(CrossArgs a) {
 
 // dK_j = scale * sum_i dS_ij q_i,   dV_j = sum_i P_ij dO_i over the rows i of the runs that see the keys
 // OWN: each wavefront has 16 keys to itself and walks all rows, without LDS; up to 64 features three wavefronts a SIMD (us, left to the compiler / three: 1000 rows
-// of 16 heads in eight runs of 1000 keys 147 / 136, 294 in runs that see 29760 keys 178 / 164; with 80 features 51.5 / 55).
+// of 16 heads in eight runs of 1000 keys 124 / 120, 294 in runs that see 29760 keys 167 / 163; with 80 features 51.5 / 55).
 template <int KB, int NW, bool OWN>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OWN && KB <= 4 ? 3 : 1, OWN && KB <= 4 ? 3 : 8))) void cross_f32_dkv_kernel(CrossArgs a) {
     __shared__ __attribute__((aligned(16))) std::conditional_t<OWN, int, Partials<KB, NW>> part;
@@ -339,6 +344,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OWN && 
         const int first = step.j + quarter * 16, tok = g.token(first);
         at.t = step.t + tok; at.j = first - tok * g.n; at.left = step.left - quarter * 16;
         if (at.left <= 0) continue;
+        f32x4 lse, D;
+        const long first_head = (long)head * g.n * a.Tq + at.t;
+        const __amdgpu_buffer_rsrc_t lses = __builtin_amdgcn_make_buffer_rsrc(a.lse + first_head, 0, 0x7fff0000, 0x00020000),
+                                     Ds = __builtin_amdgcn_make_buffer_rsrc(a.D + first_head, 0, 0x7fff0000, 0x00020000);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = g.token(at.j + q4 + e), h = at.j + q4 + e - t * g.n;
+            const uint32_t there = (uint32_t)(h * a.Tq + t) * 4u, off = q4 + e < at.left ? there : NO_ROW;
+            lse[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lses, (int)off, 0, 0));
+            D[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(Ds, (int)off, 0, 0));
+        }
         Pieces<KB> q, go;
         Columns<KB> qc, gc;
         const Block qb = row_block((const float *)a.q + col, a.ldq, dh, at, g), gb = row_block((const float *)a.d_o + col, a.lddo, dh, at, g);
@@ -346,13 +362,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OWN && 
         pieces(gb, go);
         columns(qb, qc);
         columns(gb, gc);
-        f32x4 lse, D, p, ds;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int r = min(q4 + e, at.left - 1), t = g.token(at.j + r), h = head * g.n + at.j + r - t * g.n;
-            lse[e] = a.lse[(long)h * a.Tq + at.t + t];
-            D[e] = a.D[(long)h * a.Tq + at.t + t];
-        }
+        f32x4 p, ds;
         const f32x4 s = dot_rows(q, k) * a.scale, dp = dot_rows(go, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

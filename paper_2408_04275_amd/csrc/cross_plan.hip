@@ -220,10 +220,11 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     p.tiles = (int)tiles;
     p.steps = (int)steps;
     if (dtype == DT_F32) {
-        // A workgroup for each 16 keys, or, where that gives every SIMD two wavefronts and there are few rows to share out, a wavefront.  us, workgroup / wavefront,
-        // the whole backward pass, heads of 64: 400 tokens of 16 heads in 40 runs of 200 keys 154 / 73, of 4 heads 54 / 30; 1000 of 16 heads in eight runs of 1000 keys
-        // 314 / 232; heads of 80: 1031 tokens of 16 heads in five runs of 420 keys 115 / 135, 1000 in one of 8000 keys 1931 / 1997.
-        p.own = (long)p.tiles * (TILE_KEYS / 16) * c.nkv >= 2048 && walk16 <= 8 * tiles;
+        // A workgroup for each 16 keys, or, where the keys are many and there are few rows to share out, a wavefront.  us, workgroup / wavefront, the whole backward
+        // pass, heads of 64: 400 tokens of 16 heads in 40 runs of 200 keys 122 / 71, of 4 heads in 40 of 75 28 / 21; 1000 of 16 heads in eight runs of 1000 keys 252 / 205;
+        // 60 of 4 heads in twelve runs of 83 keys 16.5 / 16.0; 549 in twelve of 168 27 / 29; heads of 80: 1031 tokens of 16 heads in five runs of 420 keys 121 / 130, 1000 in one of
+        // 8000 keys 1565 / 1673.
+        p.own = (long)p.tiles * (TILE_KEYS / 16) * c.nkv >= 512 && walk16 <= 8 * tiles;
         return p;
     }
     p.parts = dkv_parts(c, pieces, n_pieces, tiles);
