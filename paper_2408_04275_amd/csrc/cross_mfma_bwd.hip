@@ -212,8 +212,8 @@ __device__ __forceinline__ void store_dkv(const CrossArgs &a, uint8_t *smem, int
 
 // ---- dK, dV for heads wider than 64 features ----------------------------------------------------------------------------------
 // As in attn_mfma.hip: 32 keys belong to a pair of wavefronts on one SIMD, of which the first turns 32 rows at a time into P and dS
-// and the second adds dO^T P and Q^T dS, one block behind; P and dS go through LDS, rows round three slots of 64.  The same pack as above 375 us (0.56 PFLOP/s):
-// 2 us a step (1.08 PFLOP/s), bound by the matrix cores, and 5 us at the beginning and end of each of a compute unit's 14 tiles, with nothing beside it (LDS holds one
+// and the second adds dO^T P and Q^T dS, one block behind; P and dS go through LDS, rows round three slots of 64.  The same pack as above 355 us (0.60 PFLOP/s):
+// 1.9 us a step (1.13 PFLOP/s), bound by the matrix cores, and 5 us at the beginning and end of each of a compute unit's 14 tiles, with nothing beside it (LDS holds one
 // workgroup).
 template <int D> constexpr int DKV_SLOT = 2 * STEP_ROWS * D * 2 + 2 * STEP_ROWS * 4;        // Q tile, dO tile, lse[64], D[64]
 constexpr int PDS_BYTES = 4 * 1024;                                                        // P and dS of one block of one pair

@@ -134,8 +134,8 @@ constexpr int MOST_PIECES = 1024;      // (a call with more tiles than this has 
 
 // How many workgroups share a tile's rows.  `slots` workgroups run at a time, those with the most steps first: they take at least as long as the k-th round's
 // longest k times over, or all steps spread evenly.  A step takes about 2 us (64-wide heads 1.4), a workgroup's beginning and end 5, and what several share
-// is written and read once more.  us, 1 / 2 / 4 / 8 parts, the whole backward pass: 4096 tokens of 16 heads of 128 in a run of 700 keys 144 / 111 / 123 / 129,
-// 4000 tokens of 16 heads of 64, on 4 in five runs that see 2000 keys 376 / 216 / 137 / 105, 4096 of 64 heads of 128, on 8 in eight runs of 625 320 / 344 / 358 / 425.
+// is written and read once more.  us, 1 / 2 / 4 / 8 parts, the whole backward pass: 4096 tokens of 16 heads of 128 in a run of 700 keys 140 / 107 / 119 / 129,
+// 4000 tokens of 16 heads of 64, on 4 in five runs that see 2000 keys 357 / 206 / 134 / 102, 4096 of 64 heads of 128, on 8 in eight runs of 625 309 / 333 / 346 / 407.
 int dkv_parts(const CrossShape &c, Piece *pieces, int n_pieces, long tiles) {
     const long slots = c.d > 64 ? 256 : 512, all = tiles * c.nkv;
     if (all == 0 || all >= 2 * slots) return 1;
@@ -165,8 +165,8 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     CrossBwdPlan p = {};
     p.rows = dtype == DT_F32 ? 16 : 128;
     // Keys are cut into chunks where tiles of rows leave the chip empty and some walk 12 steps of 64 keys and more; a chunk has four steps at least (fp32: two).
-    // us, uncut / cut, the whole backward pass, one run of 8 heads of 128: 100 tokens, 768 keys 36 / 30, 2304 keys 79 / 32; 1500 tokens, 768 keys 53 / 55, 2304 keys
-    // 113 / 91; fp32, heads of 64, 100 tokens, 2304 keys 86 / 66.
+    // us, uncut / cut, the whole backward pass, one run of 8 heads of 128: 100 tokens, 768 keys 35 / 28, 2304 keys 78 / 30; 1500 tokens, 768 keys 51 / 54, 2304 keys
+    // 109 / 88; fp32, heads of 64, 100 tokens, 2304 keys 76 / 59.
     long walk = 0, longest = 0;
     each_sequence(c, [&](int c0, int c1, int n_keys) {
         const int n = items_of(c1 - c0, 0, group, p.rows, 0);
