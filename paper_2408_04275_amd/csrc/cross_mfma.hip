@@ -188,17 +188,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cross_fwd_kernel(CrossArgs a) {
 }
 
 // ---- forward, few rows ----------------------------------------------------------------------------------------------------
-// Up to 32 rows per workgroup, whose wavefronts (eight with 64-wide heads, four with wider ones) share out the blocks of 32 keys, each with two LDS slots of its
+// Up to 32 rows per workgroup, whose wavefronts (eight with 64-wide heads, four with wider ones; two or one where there are many workgroups) share out the blocks of 32 keys, each with two LDS slots of its
 // own and no barrier on the way: the next block is in flight while one is multiplied.  Three tokens of 16 heads of 64, 577 keys each: 6.7 us, 8.6 with four
 // wavefronts and four slots.  16 tokens of 64 heads of 128, on 8, each over 6144 keys: 80 us, 5.1 TB/s of keys and values, which is what bounds it.  Where that leaves the chip empty or one workgroup with a long walk, the keys are cut into chunks, one per workgroup, whose partial
 // results (32 rows of fp32, maximum and sum) cross_combine_kernel joins.
 constexpr int FEW_SLOTS = 2;
 template <int D> constexpr int FEW_WAVES = D <= 64 ? 8 : 4;
-template <int D> constexpr int FEW_LDS = FEW_WAVES<D> * FEW_SLOTS * 2 * ROWS32<D>;
+template <int D, int NW> constexpr int FEW_LDS = NW * FEW_SLOTS * 2 * ROWS32<D>;
 
-template <int D, int KS, int CB>
-__global__ __launch_bounds__(64 * FEW_WAVES<D>, 1) void cross_fwd_few_kernel(CrossArgs a) {
-    constexpr int N = ROWS32<D> / 1024, SLOT = 2 * ROWS32<D>, SLOTS = FEW_SLOTS, MINE = SLOTS * SLOT, NW = FEW_WAVES<D>, NEXT = 32 * NW;
+template <int D, int KS, int CB, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void cross_fwd_few_kernel(CrossArgs a) {
+    constexpr int N = ROWS32<D> / 1024, SLOT = 2 * ROWS32<D>, SLOTS = FEW_SLOTS, MINE = SLOTS * SLOT, NEXT = 32 * NW;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_all[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     uint8_t *const smem = smem_all + wave * MINE;
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES<D>, 1) void cross_fwd_few_kernel(Cro
             kb += NEXT;
         });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    // four partial softmaxes over disjoint keys become one: each wavefront joins one block of 32 features
+    // the wavefronts' partial softmaxes over disjoint keys become one: each joins blocks of 32 features
     put_acc(smem, oacc);
     const float l_own = sum_across_halves(l_run);
     float2 *const ml = reinterpret_cast<float2 *>(smem + SLOT);
@@ -320,15 +320,17 @@ __global__ __launch_bounds__(64 * FEW_WAVES<D>, 1) void cross_fwd_few_kernel(Cro
     }
     const int tok = g.token(mine.j + l32), h = mine.j + l32 - tok * g.n;
     const bool live = l32 < mine.left;
-    if (wave < CB) {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        if (cb % NW != wave) continue;
         f32x4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < NW; ++w) x[i] += reinterpret_cast<const f32x4 *>(smem_all + w * MINE)[(4 * wave + i) * 64 + lane] * f[w];
+            for (int w = 0; w < NW; ++w) x[i] += reinterpret_cast<const f32x4 *>(smem_all + w * MINE)[(4 * cb + i) * 64 + lane] * f[w];
         }
-        const int c0 = 32 * wave + 4 * half;
+        const int c0 = 32 * cb + 4 * half;
         if (parts > 1) {
             float *out = a.part + ((size_t)blockIdx.x * FEW_ROWS + l32) * dh + c0;
 #pragma unroll
@@ -410,20 +412,22 @@ hipError_t launch_tiles(const CrossArgs &a, int items, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int D, int KS, int CB>
+template <int D, int KS, int CB, int NW>
 hipError_t launch_few(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
-    const hipError_t e = set_smem(done, cross_fwd_few_kernel<D, KS, CB>, FEW_LDS<D>);
+    const hipError_t e = set_smem(done, cross_fwd_few_kernel<D, KS, CB, NW>, FEW_LDS<D, NW>);
     if (e != hipSuccess) return e;
-    cross_fwd_few_kernel<D, KS, CB><<<items * a.nkv, 64 * FEW_WAVES<D>, FEW_LDS<D>, st>>>(a);
+    cross_fwd_few_kernel<D, KS, CB, NW><<<items * a.nkv, 64 * NW, FEW_LDS<D, NW>, st>>>(a);
     if (a.chunk) cross_combine_kernel<<<items * a.nkv, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <int D, int KS, int CB>
 hipError_t launch_fwd(const CrossArgs &a, const CrossPlan &p, hipStream_t st) {
-    return p.rows == FEW_ROWS ? launch_few<D, KS, CB>(a, p.items, st)
-                              : p.rows == 256 ? launch_tiles<D, KS, CB, 8>(a, p.items, st) : launch_tiles<D, KS, CB, 4>(a, p.items, st);
+    if (p.rows == FEW_ROWS)
+        return p.waves == 1 ? launch_few<D, KS, CB, 1>(a, p.items, st) : p.waves == 2 ? launch_few<D, KS, CB, 2>(a, p.items, st)
+                                                                                       : launch_few<D, KS, CB, FEW_WAVES<D>>(a, p.items, st);
+    return p.rows == 256 ? launch_tiles<D, KS, CB, 8>(a, p.items, st) : launch_tiles<D, KS, CB, 4>(a, p.items, st);
 }
 
 }  // namespace

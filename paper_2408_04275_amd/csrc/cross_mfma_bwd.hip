@@ -53,25 +53,27 @@ __device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[C
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
-// Four wavefronts of 32 rows, two workgroups a compute unit (eight and one are nowhere faster: us, 128 / 256 rows, both backward kernels: 4096 tokens of 32 heads
-// of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284).
+// Four wavefronts of 32 rows, two workgroups a compute unit; one and eight for many short runs (see cross_bwd_plan).  Eight and one are nowhere faster: us, 128 / 256 rows, both
+// backward kernels: 4096 tokens of 32 heads
+// of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284.
 // 8192 tokens of 32 heads of 128 in 12 runs of 1152 keys 250 us (0.64 PFLOP/s): Q, dO, O and dQ alone take 47 (5.7 TB/s), a step of 64 keys of both workgroups 2.6 (1.24 PFLOP/s),
 // bound by the matrix cores.  Q and dO on their way together instead of one after the other, and tiles of 32 keys: no difference.
 // LDS: two slots of a K and a V tile; the Q, dO and O rows stand in the second slot, one after the other.
-template <int D> constexpr int DQ_LDS = 2 * 2 * KEYS * D * 2;
+template <int WAVES> constexpr int DQ_STEP = WAVES == 4 ? 64 : 32;
+template <int D, int WAVES> constexpr int DQ_LDS = 2 * 2 * DQ_STEP<WAVES> * D * 2;
 
-template <int D, int KS, int CB>
-__global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
-    constexpr int TILE = KEYS * D * 2, SLOT = 2 * TILE, COPIES = TILE / 1024 / 4;
+template <int D, int KS, int CB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void cross_dq_kernel(CrossArgs a) {
+    constexpr int ROWS = 32 * WAVES, STEP = DQ_STEP<WAVES>, TILE = STEP * D * 2, SLOT = 2 * TILE, COPIES = TILE / 1024 / WAVES;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
     int block = blockIdx.x;
-    if (a.n_tiles > 0 && block-- == 0) { make_plan<256>(a, (int *)smem); return; }
+    if (a.n_tiles > 0 && block-- == 0) { make_plan<64 * WAVES>(a, (int *)smem); return; }
     const int head = block % a.nkv, dh = a.d;
-    const Item it = find_item(a, block / a.nkv, 128, a.chunk);
+    const Item it = find_item(a, block / a.nkv, ROWS, a.chunk);
     const int parts = a.chunk ? max((it.hi - it.lo + a.chunk - 1) / a.chunk, 1) : 1, part = it.index % parts;
     const Group g(a);
-    const Rows mine(it, g, it.index / parts * 128 + wave * 32);
+    const Rows mine(it, g, it.index / parts * ROWS + wave * 32);
     const int kbeg = it.lo + part * a.chunk, kend = !a.dq ? kbeg : parts > 1 ? min(kbeg + a.chunk, it.hi) : it.hi;
     const bf16_t *const K = (const bf16_t *)a.k + (long)head * dh, *const V = (const bf16_t *)a.v + (long)head * dh;
     const long col = (long)head * g.n * dh;
@@ -134,11 +136,11 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
     tr.init((uint32_t)(uintptr_t)(lds_void *)smem);
 
     int slot = 0;
-    for (int kt = kbeg; kt < kend; kt += KEYS, slot ^= 1) {
+    for (int kt = kbeg; kt < kend; kt += STEP, slot ^= 1) {
         const uint8_t *sK = smem + slot * SLOT, *sV = sK + TILE;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this step's tiles have landed
         lds_barrier();                                               // ... and everyone is done with the other slot
-        if (kt + KEYS < kend) copy_kv(smem + (slot ^ 1) * SLOT, kt + KEYS);
+        if (kt + STEP < kend) copy_kv(smem + (slot ^ 1) * SLOT, kt + STEP);
         auto block = [&](auto B_) {
             constexpr int b = decltype(B_)::value;
             const int kb = kt + 32 * b;
@@ -178,10 +180,10 @@ __global__ __launch_bounds__(256, 2) void cross_dq_kernel(CrossArgs a) {
             }
         };
         block(std::integral_constant<int, 0>{});
-        block(std::integral_constant<int, 1>{});
+        if constexpr (STEP > 32) block(std::integral_constant<int, 1>{});
     }
     lds_barrier();                                     // the tiles are done with: LDS now stages the output rows
-    if (parts > 1) store_part<D, CB>(smem + wave * STAGE32<D>, dq, a.part + ((size_t)block * 128 + wave * 32) * dh, dh, mine.left, dh);
+    if (parts > 1) store_part<D, CB>(smem + wave * STAGE32<D>, dq, a.part + ((size_t)block * ROWS + wave * 32) * dh, dh, mine.left, dh);
     else store_rows_at<D, CB>(smem + wave * STAGE<D>, dq, a.scale, (bf16_t *)a.dq + col, a.lddq, dh, mine, g);
 }
 
@@ -525,22 +527,22 @@ __global__ __launch_bounds__(256) void cross_dkv_sum_kernel(CrossArgs a) {
     *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
-template <int D, int KS, int CB>
+template <int D, int KS, int CB, int WAVES>
 hipError_t launch_dq(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
-    constexpr int LDS = std::max(DQ_LDS<D>, 4 * STAGE32<D>);
-    static_assert(PLAN_LDS <= LDS, "room for the plan");
-    const hipError_t e = set_smem(done, cross_dq_kernel<D, KS, CB>, LDS);
+    constexpr int LDS = std::max({DQ_LDS<D, WAVES>, WAVES * STAGE32<D>, PLAN_LDS});
+    const hipError_t e = set_smem(done, cross_dq_kernel<D, KS, CB, WAVES>, LDS);
     if (e != hipSuccess) return e;
-    cross_dq_kernel<D, KS, CB><<<items * a.nkv + (a.n_tiles > 0), 256, LDS, st>>>(a);
-    if (a.chunk) cross_dq_sum_kernel<bf16_t, 128><<<items * a.nkv, 256, 0, st>>>(a);
+    cross_dq_kernel<D, KS, CB, WAVES><<<items * a.nkv + (a.n_tiles > 0), 64 * WAVES, LDS, st>>>(a);
+    if constexpr (WAVES == 4)                            // (with fewer there are workgroups enough)
+        if (a.chunk) cross_dq_sum_kernel<bf16_t, 128><<<items * a.nkv, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <int D, int KS, int CB>
 hipError_t launch_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st) {
     hipError_t e = hipSuccess;
-    if (p.items || a.n_tiles) e = launch_dq<D, KS, CB>(a, p.items, st);
+    if (p.items || a.n_tiles) e = p.rows == FEW_ROWS ? launch_dq<D, KS, CB, 1>(a, p.items, st) : launch_dq<D, KS, CB, 4>(a, p.items, st);
     if (e != hipSuccess || !a.n_tiles) return e;
     static std::atomic<bool> done{false};
     const dim3 grid(p.tiles * a.nkv, a.parts);

@@ -131,6 +131,7 @@ struct CrossArgs {
 struct CrossShape { int Tq, Tk, S, nh, nkv, d; const int *cu, *begin, *end; };
 struct CrossPlan {
     int rows, chunk, items;         // rows of a workgroup, keys of a chunk (0: not cut), workgroups per key/value head
+    int waves;                      // bf16, few rows: wavefronts of a workgroup
     bool table;                     // items are found in a table
 };
 struct CrossBwdPlan {

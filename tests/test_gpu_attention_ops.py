@@ -722,3 +722,10 @@ def test_qk_norm_no_tokens_writes_zero_gradients(nq, nk):
         grads = {k: torch.full((64,), 3.0, device="cuda") for k in w}
         check(mm.mmtrain_qk_norm_rope_bwd(desc, None, 0, None, None, mm.make_qk_norm_weights(w), None, 512, None, 512, None, 512, mm.make_qk_norm_grads(grads), flags, ws, wsb), "bwd")
         assert all(torch.all(t == want) for t in grads.values())
+
+
+@pytest.mark.parametrize("S,nh,nkv,d,longest", [(20, 32, 32, 64, 300), (90, 32, 32, 64, 70), (15, 32, 32, 128, 200), (20, 32, 32, 128, 60), (20, 32, 32, 128, 900), (40, 64, 32, 80, 90), (70, 48, 24, 96, 40)])
+def test_cross_many_workgroups_of_few_rows(S, nh, nkv, d, longest):
+    """Workgroups of two wavefronts and of one; some runs without tokens or keys, and walks of one block and of many."""
+    rng = np.random.default_rng(S + d)
+    Cross(mm.BF16, nh, nkv, d, runs(rng.integers(0, 7, S), rng.integers(0, longest, S), tail=5), std=2.0, seed=S).verify()
