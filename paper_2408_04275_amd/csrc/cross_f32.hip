@@ -385,6 +385,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OWN && 
             part.each(scale, to);
         }
     };
+    if (!OWN && a.parts > 1) {
+        const int nk = a.nkv * dh;
+        float *const out = a.dkv_part + (size_t)blockIdx.y * a.Tk * 2 * nk;
+        store(dk, out, 2 * nk, 1.f);
+        store(dv, out + nk, 2 * nk, 1.f);
+        return;
+    }
     store(dk, a.dk, a.lddk, a.scale);
     store(dv, a.dv, a.lddv, 1.f);
 }
@@ -425,7 +432,8 @@ hipError_t cross_f32_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t 
         if (a.chunk) cross_dq_sum_kernel<float, 16><<<p.items * a.nkv, 256, 0, st>>>(a);
         if (!a.n_tiles) return hipGetLastError();
         if (p.own) cross_f32_dkv_kernel<KB, 4, true><<<a.n_tiles * (TILE_KEYS / 64) * a.nkv, 256, 0, st>>>(a);
-        else cross_f32_dkv_kernel<KB, WAVES<KB>, false><<<a.n_tiles * (TILE_KEYS / 16) * a.nkv, 64 * WAVES<KB>, 0, st>>>(a);
+        else cross_f32_dkv_kernel<KB, WAVES<KB>, false><<<dim3(a.n_tiles * (TILE_KEYS / 16) * a.nkv, a.parts), 64 * WAVES<KB>, 0, st>>>(a);
+        if (a.parts > 1) cross_dkv_sum_kernel<float><<<ceil_div((long)a.Tk * (2 * a.nkv * a.d / 4), 256), 256, 0, st>>>(a);
         return hipGetLastError();
     });
 }

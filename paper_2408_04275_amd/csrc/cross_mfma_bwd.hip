@@ -511,22 +511,6 @@ __global__ __launch_bounds__(256, 2) void cross_dkv_plain_kernel(CrossArgs a) {
     store_dkv<D, CB>(a, smem, wave, head, key, kt.end - key, dk, dv);
 }
 
-// The parts of dK (scaled) and dV, added in order, as bf16 rows; a thread has four features
-__global__ __launch_bounds__(256) void cross_dkv_sum_kernel(CrossArgs a) {
-    const int nk = a.nkv * a.d, quads = 2 * nk / 4;
-    const long idx = (long)blockIdx.x * 256 + threadIdx.x;
-    if (idx >= (long)a.Tk * quads) return;
-    const int t = (int)(idx / quads), c = (int)(idx % quads) * 4;
-    const size_t stride = (size_t)a.Tk * 2 * nk;
-    const float *p = a.dkv_part + (size_t)t * 2 * nk + c;
-    f32x4 x = *reinterpret_cast<const f32x4 *>(p);
-    for (int i = 1; i < a.parts; ++i) x += *reinterpret_cast<const f32x4 *>(p + i * stride);
-    const bool is_k = c < nk;
-    if (is_k) x *= a.scale;
-    bf16_t *out = is_k ? (bf16_t *)a.dk + t * a.lddk + c : (bf16_t *)a.dv + t * a.lddv + c - nk;
-    *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-}
-
 template <int D, int KS, int CB, int WAVES>
 hipError_t launch_dq(const CrossArgs &a, int items, hipStream_t st) {
     static std::atomic<bool> done{false};
@@ -555,7 +539,7 @@ hipError_t launch_bwd(const CrossArgs &a, const CrossBwdPlan &p, hipStream_t st)
         if ((e = set_smem(done, cross_dkv_kernel<D, KS, CB>, DKV_PAIR_LDS<D>)) != hipSuccess) return e;
         cross_dkv_kernel<D, KS, CB><<<grid, 512, DKV_PAIR_LDS<D>, st>>>(a);
     }
-    if (a.parts > 1) cross_dkv_sum_kernel<<<ceil_div((long)a.Tk * (2 * a.nkv * a.d / 4), 256), 256, 0, st>>>(a);
+    if (a.parts > 1) cross_dkv_sum_kernel<bf16_t><<<ceil_div((long)a.Tk * (2 * a.nkv * a.d / 4), 256), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

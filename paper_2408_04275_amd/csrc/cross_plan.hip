@@ -234,7 +234,11 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
         // pass, heads of 64: 400 tokens of 16 heads in 40 runs of 200 keys 122 / 71, of 4 heads in 40 of 75 28 / 21; 1000 of 16 heads in eight runs of 1000 keys 252 / 205;
         // 60 of 4 heads in twelve runs of 83 keys 16.5 / 16.0; 549 in twelve of 168 27 / 29; heads of 80: 1031 tokens of 16 heads in five runs of 420 keys 121 / 130, 1000 in one of
         // 8000 keys 1565 / 1673.
-        p.own = (long)p.tiles * (TILE_KEYS / 16) * c.nkv >= 512 && walk16 <= 8 * tiles;
+        p.own = tiles * (TILE_KEYS / 16) * c.nkv >= 512 && walk16 <= 8 * tiles;
+        // Few keys and many rows: several workgroups share the rows (us, one / several, the whole backward pass: 491 tokens of 64 heads of 80, on 8 in two runs that see 78 keys
+        // 197 / 78, 1000 of 16 heads of 64 in one run of 64 keys 53 / 43; from 256 workgroups on 500 keys, 8 heads 57 / 58, 2000 keys, 4 heads 108 / 120).
+        const long all = tiles * (TILE_KEYS / 16) * c.nkv;
+        while (all < 256 && p.parts < 16 && all * p.parts * 2 <= 1024 && walk16 >= 32 * tiles * p.parts && part_bytes(c) * p.parts * 2 <= size_t(96) << 20) p.parts *= 2;
         return p;
     }
     p.parts = dkv_parts(c, pieces, n_pieces, tiles);

@@ -335,6 +335,24 @@ __global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossArgs a) {
     }
 }
 
+// The parts of dK (scaled) and dV, added in order, as bf16 rows; a thread has four features
+template <typename T>
+__global__ __launch_bounds__(256) void cross_dkv_sum_kernel(CrossArgs a) {
+    const int nk = a.nkv * a.d, quads = 2 * nk / 4;
+    const long idx = (long)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= (long)a.Tk * quads) return;
+    const int t = (int)(idx / quads), c = (int)(idx % quads) * 4;
+    const size_t stride = (size_t)a.Tk * 2 * nk;
+    const float *p = a.dkv_part + (size_t)t * 2 * nk + c;
+    f32x4 x = *reinterpret_cast<const f32x4 *>(p);
+    for (int i = 1; i < a.parts; ++i) x += *reinterpret_cast<const f32x4 *>(p + i * stride);
+    const bool is_k = c < nk;
+    if (is_k) x *= a.scale;
+    T *out = is_k ? (T *)a.dk + t * a.lddk + c : (T *)a.dv + t * a.lddv + c - nk;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4 *>(out) = x;
+    else *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+}
+
 inline size_t table_bytes(int runs) { return ((size_t)(2 * runs + 1) * sizeof(int) + 255) & ~size_t(255); }
 
 }  // namespace

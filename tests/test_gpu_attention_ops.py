@@ -592,7 +592,7 @@ def test_cross_gradients_of_few_rows_and_long_walks(dtype):
 @DTYPES
 @pytest.mark.parametrize("lq,lk,nh,nkv", [(900, 100, 8, 2), (700, 260, 4, 4), (333, 1, 6, 1)])
 def test_cross_gradients_of_many_rows_and_few_keys(dtype, lq, lk, nh, nkv):
-    """dK and dV of a tile from several workgroups (bf16)."""
+    """dK and dV of a tile from several workgroups."""
     for d in (64, 112):
         Cross(dtype, nh, nkv, d, runs([lq, 5, lq // 2], [lk, 70, lk]), seed=lq + d).verify()
     Cross(dtype, nh, nkv, 128, runs([lq, lq // 3, 64], [lk, lk, lk], "previous"), seed=lq).verify()
