@@ -342,7 +342,7 @@ __global__ __launch_bounds__(512, 2) void cross_dkv_kernel(CrossArgs a) {
 #pragma unroll
             for (int x = 0; x < TrReader<D>::N; ++x) trc[x] = tr.off[x] + tile;
             lds_read16<0>(pf[0], box); lds_read16<2048>(dsf[0], box);
-            lds_read16<1024>(pf[1], box); lds_read16<3072>(dsf[1], box);
+            lds_read16<1024>(pf[1], box); lds_read16<3 * 1024>(dsf[1], box);
             auto issue = [&](auto G_) {
                 constexpr int gi = decltype(G_)::value, m = gi / CB, c = gi % CB;
                 o[gi][0] = TrReader<D>::template read_at<b, m, c, 0, TILE>(trc); o[gi][1] = TrReader<D>::template read_at<b, m, c, 1, TILE>(trc);

@@ -89,21 +89,22 @@ CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
     // of 32 heads in four runs of 2304 175 / 184; of 80, 8 runs of 1024 38 / 42; of 64, 16 runs of 576 34 / 42.
     // Tiles of 32 rows where those of 128 would be less than a third full (us, 128 / 32 rows, 60 runs of 1152 keys, 32 heads of 128, 20 rows each 201 / 196, 45 rows 209 / 231; of 64
     // 130 keys 19 / 15, 21 / 20) or too few.
-    p.rows = dtype == DT_F32 ? 16 : many > 3 * few || count(128, 0) * c.nkv < 128 ? FEW_ROWS : c.d > 64 && many >= 512 * count(128, 0) ? 256 : 128;
+    const long of128 = count(128, 0);
+    p.rows = dtype == DT_F32 ? 16 : many > 3 * few || of128 * c.nkv < 128 ? FEW_ROWS : c.d > 64 && many >= 512 * of128 ? 256 : 128;
     // Long walks of few rows are cut so that there are no more workgroups than fit on the chip at once (bf16: one per compute unit; where two rounds are needed anyway,
     // two).  us, at most 256 / 512 / 1024 workgroups, one token a run: 16 runs of 6144 keys, 8 heads of 128 85 / 84 / 91; 5 of 4000 21 / 25 / 29; 48 that see 5000 keys,
     // four in a row the same 60 / 62 / 70.  A chunk has 8 blocks of 32 keys at least (fp32: 4): one run of 4 heads of 128, 1152 keys, uncut / 16 / 8 / 4 blocks
     // 13.1 / 12.7 / 11.2 / 10.7, 4600 keys 34.7 / 13.5 / 12.5 / 13.2; fp32, heads of 80, 1152 keys 26.6 / 19.0 / 13.7 / 12.3.  Shorter walks stay whole (uncut / cut: 1152
     // keys of 64-wide heads 8.2 / 11.0, of 128 13.2 / 12.0).
     const bool f32 = dtype == DT_F32;
-    const long uncut = count(p.rows, 0) * c.nkv;
+    const long uncut = (p.rows == 128 ? of128 : count(p.rows, 0)) * c.nkv;
     if (p.rows <= FEW_ROWS && uncut < 512 && longest > (f32 ? 12 : c.d <= 64 ? 64 : 32)) {
         const long most = f32 ? 1024 : uncut < 192 ? 256 : 512, want = std::max(few * c.nkv / most, f32 ? 4l : 8l);
         p.chunk = (int)std::min((want + 3) / 4 * 128, 1l << 20);
         while (p.chunk < longest * 32 && count(p.rows, p.chunk) * c.nkv > most) p.chunk += std::max(p.chunk / 16 / 128 * 128, 128);
         if (p.chunk >= longest * 32) p.chunk = 0;
     }
-    p.items = (int)count(p.rows, p.chunk);
+    p.items = (int)(p.chunk ? count(p.rows, p.chunk) : uncut / c.nkv);
     p.table = c.S > 64;
     // Wavefronts share a walk as far as the chip holds all workgroups at once: 256 of eight (wide heads four), of wide heads 512 of two and 1024 of one, of 64-wide ones
     // 1280 and 2560.  us, most / 2 / 1, S runs of three tokens, n keys each, heads: S 20, 8 heads of 128, n 260 10.5 / 11.1 / 16; S 20, 32 of 128, n 20 15 / 11 / 7, n 577 41 / 36 / 41;
@@ -173,7 +174,8 @@ CrossBwdPlan cross_bwd_plan(int dtype, const CrossShape &c, bool dkv) {
     p.rows = dtype == DT_F32 ? 16 : 128;
     // dQ of many short runs: tiles of 32 rows where those of 128 would be less than a third full and there are two rounds of them.  us, 128 / 32 rows, the whole backward pass,
     // 60 runs of 32 heads of 128, 20 keys each: 5 tokens each 58 / 48, 20 tokens 59 / 50, 45 tokens 69 / 66, 90 tokens 96 / 102; 577 keys, 20 tokens 363 / 359; eight runs 14 / 13, 577 keys 62 / 62.
-    if (dtype != DT_F32 && items(c, 128, 0) * (long)c.nkv >= 512 && items(c, 128, 0) * 4l > items(c, FEW_ROWS, 0) * 3l) p.rows = FEW_ROWS;
+    const long of128 = dtype == DT_F32 ? 0 : items(c, 128, 0);
+    if (of128 * c.nkv >= 512 && of128 * 4 > items(c, FEW_ROWS, 0) * 3l) p.rows = FEW_ROWS;
     // Keys are cut into chunks where tiles of rows leave the chip empty and some walk 12 steps of 64 keys and more; a chunk has four steps at least (fp32: two).
     // us, uncut / cut, the whole backward pass, one run of 8 heads of 128: 100 tokens, 768 keys 35 / 28, 2304 keys 78 / 30; 1500 tokens, 768 keys 51 / 54, 2304 keys
     // 109 / 88; fp32, heads of 64, 100 tokens, 2304 keys 76 / 59.
