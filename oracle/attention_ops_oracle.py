@@ -43,6 +43,12 @@ def _stats(x, norm, eps):
     return mean, 1.0 / np.sqrt(((x - mean) ** 2).mean(-1, keepdims=True) + eps)
 
 
+def _mean_mag(x, norm):
+    """What the mean's rounding errors are proportional to: each of its additions rounds a partial sum, which is at most the sum of the absolute values
+    (the mean itself may be as small as it likes)."""
+    return np.abs(x).mean(-1, keepdims=True) if norm == "layer" else 0.0
+
+
 def _gains(w, name, nq, nk, d, default):
     return np.concatenate([np.broadcast_to(np.asarray(w.get(k + name, np.full(d, default)), F64), (h, d)) for k, h in (("q", nq), ("k", nk))])
 
@@ -54,7 +60,7 @@ def qk_norm_fwd(x, w, nq, nk, norm, eps, turn=None):
     mean, r = _stats(x, norm, eps)
     gain, bias = _gains(w, "_w", nq, nk, d, 1.0), _gains(w, "_b", nq, nk, d, 0.0)
     y = (x - mean) * r * gain + bias
-    mag = (np.abs(x) + np.abs(mean)) * r * np.abs(gain) + np.abs(bias)
+    mag = (np.abs(x) + _mean_mag(x, norm)) * r * np.abs(gain) + np.abs(bias)
     if turn is None:
         return y, mag
     pos, theta, layout, m = turn
@@ -78,7 +84,7 @@ def qk_norm_bwd(x, dy, w, nq, nk, norm, eps, turn=None):
         pos, theta, layout, m = turn
         g, mg = rope(g, pos, theta, layout, m, gradient=True)[0], rope_mag(mg, theta, layout, m)
     mean, r = _stats(x, norm, eps)
-    hat, mhat = (x - mean) * r, (np.abs(x) + np.abs(mean)) * r
+    hat, mhat = (x - mean) * r, (np.abs(x) + _mean_mag(x, norm)) * r
     gain = _gains(w, "_w", nq, nk, d, 1.0)
     back, mback = g * gain, mg * np.abs(gain)
     s1, ms1 = (back * hat).mean(-1, keepdims=True), (mback * mhat).mean(-1, keepdims=True)

@@ -729,3 +729,10 @@ def test_cross_many_workgroups_of_few_rows(S, nh, nkv, d, longest):
     """Workgroups of two wavefronts and of one; some runs without tokens or keys, and walks of one block and of many."""
     rng = np.random.default_rng(S + d)
     Cross(mm.BF16, nh, nkv, d, runs(rng.integers(0, 7, S), rng.integers(0, longest, S), tail=5), std=2.0, seed=S).verify()
+
+
+def test_qk_norm_features_beside_a_small_mean():
+    """A feature and its head's mean are both near zero among features of 1: the mean's rounding errors, which the other features make, are all that
+    is off."""
+    qk_case(mm.F32, 6, 1, 248, 0, "half", "layer", T=240, other=64, main=True, seed=5365)
+    qk_case(mm.F32, 2, 2, 80, 40, "interleaved", "layer", T=700, positions=np.arange(700), seed=48)
