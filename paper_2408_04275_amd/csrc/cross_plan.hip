@@ -58,7 +58,11 @@ void each_sequence(const CrossShape &c, F f) {
 void order_runs(const CrossShape &c, CrossArgs &a) {
     if (c.S > 64) return;
     for (int s = 0; s < c.S; s = behind(c, s)) a.order[a.n_sequences++] = (uint8_t)s;
-    std::stable_sort(a.order, a.order + a.n_sequences, [&](uint8_t x, uint8_t y) { return c.end[x] - c.begin[x] > c.end[y] - c.begin[y]; });
+    // (their numbers settle the order of equal ones: a sort that keeps it by itself asks the heap for a buffer)
+    std::sort(a.order, a.order + a.n_sequences, [&](uint8_t x, uint8_t y) {
+        const int n = c.end[x] - c.begin[x], m = c.end[y] - c.begin[y];
+        return n != m ? n > m : x < y;
+    });
     for (int i = 0; i < a.n_sequences; ++i) a.last[i] = (uint8_t)(behind(c, a.order[i]) - 1);
 }
 
