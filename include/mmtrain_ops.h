@@ -255,7 +255,7 @@ MMTRAIN_API int mmtrain_qk_norm_rope_bwd(const mmtrain_qk_norm_desc *desc, const
  * Grouped heads as in mmtrain_layer_desc: query head h reads key/value head h / (n_heads / n_kv_heads).
  * One token for each of many sequences is a call with runs of one token: with few queries the keys are shared out over the chip.
  * Supported: head_dim a multiple of 16 up to 128, n_heads % n_kv_heads = 0, at most 4096 heads, 65536 runs, 2^28 rows of a key/value head (query
- * tokens times the heads that share it), 2^31 query tokens times heads, 2^30 key tokens, strides multiples of 8 (bf16) or 4 (fp32) elements below
+ * tokens times the heads that share it), 2^30 key tokens, query tokens and runs together times heads below 2^31, strides multiples of 8 (bf16) or 4 (fp32) elements below
  * 2^24, and fewer than 2^23 - 1 workgroups, counted as q_tokens n_heads / 32 + runs n_kv_heads and as (kv_tokens / 128 + 2 runs + 1) n_kv_heads (fp32: / 16, and / 16
  * and 8 times the runs' part); anything else: MMTRAIN_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------ */

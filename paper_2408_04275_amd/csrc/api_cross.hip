@@ -21,7 +21,7 @@ int check_cross(const mmtrain_cross_attn_desc *d) {
 int check_cross_batch(const mmtrain_cross_batch *b, bool ordered) {
     if (!b || b->q_tokens < 0 || b->kv_tokens < 0 || b->n_segments < 0 || !b->cu_q_host) return MMTRAIN_ERR_INVALID_ARG;
     if (b->n_segments > 0 && (!b->kv_begin_host || !b->kv_end_host)) return MMTRAIN_ERR_INVALID_ARG;
-    if (b->n_segments > CROSS_MAX_SEGMENTS || b->q_tokens > 1 << 27 || b->kv_tokens > 1 << 30) return MMTRAIN_ERR_UNSUPPORTED;
+    if (b->n_segments > CROSS_MAX_SEGMENTS || b->q_tokens > 1 << 28 || b->kv_tokens > 1 << 30) return MMTRAIN_ERR_UNSUPPORTED;
     const int32_t *cu = b->cu_q_host, *lo = b->kv_begin_host, *hi = b->kv_end_host;
     if (cu[0] != 0) return MMTRAIN_ERR_BAD_SEGMENTS;
     int32_t last_lo = 0, last_hi = 0;
