@@ -681,7 +681,7 @@ def _rows(t):
         return None, 0
     if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("rows of neighbouring elements")
-    return _ptr(t), t.stride(0)
+    return _ptr(t), t.stride(0) if len(t) > 1 else t.shape[1]          # (of one row torch keeps any stride)
 
 
 def make_cross_attn_tensors(q, k, v, o, lse=None) -> CrossAttnTensors:
