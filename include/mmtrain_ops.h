@@ -252,6 +252,9 @@ MMTRAIN_API int mmtrain_qk_norm_rope_bwd(const mmtrain_qk_norm_desc *desc, const
  * A pack whose samples have their own images: kv_begin = cu_kv, kv_end = cu_kv + 1 (the same array).  Runs may see the same keys (several
  * continuations of one prompt) or overlapping ranges (text that sees the images so far).  kv_begin[s] = kv_end[s]: the run sees
  * nothing, o = 0, lse = -infinity, no gradient.  What a query does not see does not reach it, not even an infinity or NaN.
+ * Scores, softmax statistics and sums are fp32.  With MMTRAIN_BF16 the operands of all products are bf16, so the probabilities (and, for the gradients, P and dS) are
+ * rounded to bf16 before they meet V, dO, K and Q: each is off by half a step, 2^-8 of its value, at most; o by l2 0.0023 of its norm where its own rounding makes
+ * 0.0017.  MMTRAIN_F32 rounds nothing to fewer bits.
  * Grouped heads as in mmtrain_layer_desc: query head h reads key/value head h / (n_heads / n_kv_heads).
  * One token for each of many sequences is a call with runs of one token: with few queries the keys are shared out over the chip.
  * Supported: head_dim a multiple of 16 up to 128, n_heads % n_kv_heads = 0, at most 4096 heads, 65536 runs, 2^28 rows of a key/value head (query

@@ -2,7 +2,8 @@
 // cross_mfma.hip, two kernels.  dQ holds one row per lane and walks the keys of its run; it also writes -D, D = rowsum(dO * O).
 // dK/dV holds one key per lane and walks the rows that see its keys.  For that the keys are cut wherever a run's range begins or ends
 // (make_plan): all keys of a tile are seen by the same runs, which follow one another, so again nothing is masked.  Keys that several runs
-// see, and heads of a group, are summed in registers, in the order of the runs: nothing needs atomics.
+// see, and heads of a group, are summed in registers, in the order of the runs: nothing needs atomics.  P and dS are rounded to bf16 as operands of their products with dO, Q
+// and K, for the reason that cross_mfma.hip gives; each gradient is off by 0.0022 to 0.0024 of its norm.
 #include "cross_tiles.h"
 #include <algorithm>
 
@@ -53,9 +54,8 @@ __device__ __forceinline__ void store_part(uint8_t *stage, const f32x16 (&acc)[C
 }
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
-// Four wavefronts of 32 rows, two workgroups a compute unit; one and eight for many short runs (see cross_bwd_plan).  Eight and one are nowhere faster: us, 128 / 256 rows, both
-// backward kernels: 4096 tokens of 32 heads
-// of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284.
+// Four wavefronts of 32 rows, two workgroups a compute unit; one wavefront for many short runs, where it is faster (see cross_bwd_plan).  Eight were nowhere faster than four and
+// are not built: us, 128 / 256 rows, both backward kernels: 4096 tokens of 32 heads of 128, on 8 in one run of 8192 keys 1785 / 1792, four runs of 2304 603 / 635; 2111 tokens in 61 runs of 300 237 / 284.
 // 8192 tokens of 32 heads of 128 in 12 runs of 1152 keys 250 us (0.64 PFLOP/s): Q, dO, O and dQ alone take 47 (5.7 TB/s), a step of 64 keys of both workgroups 2.6 (1.24 PFLOP/s),
 // bound by the matrix cores.  Q and dO on their way together instead of one after the other, and tiles of 32 keys: no difference.
 // LDS: two slots of a K and a V tile; the Q, dO and O rows stand in the second slot, one after the other.

@@ -110,8 +110,10 @@ CrossPlan cross_fwd_plan(int dtype, const CrossShape &c) {
     }
     p.items = (int)(p.chunk ? count(p.rows, p.chunk) : uncut / c.nkv);
     p.table = c.S > 64;
-    // Wavefronts share a walk as far as the chip holds all workgroups at once: 256 of eight (wide heads four), of wide heads 512 of two and 1024 of one, of 64-wide ones
-    // 1280 and 2560.  us, most / 2 / 1, S runs of three tokens, n keys each, heads: S 20, 8 heads of 128, n 260 10.5 / 11.1 / 16; S 20, 32 of 128, n 20 15 / 11 / 7, n 577 41 / 36 / 41;
+    // Wavefronts share a walk as far as the chip holds all workgroups at once: 256 of eight (wide heads four), 512 of two with wide heads and 1280 with 64-wide ones; beyond those
+    // one, or two again where wide heads walk twelve blocks of 32 keys and more on average.  us, 2 / 1, S 60, n 260 / 390 / 577 / 1500: 32 heads of 80 44 / 46, 60 / 64, 89 / 96,
+    // 219 / 228, of 128 48 / 44, 75 / 73, 106 / 105, 258 / 258; with 640 workgroups one is faster, S 20, 32 of 80 20 / 18, 26 / 24, 34 / 33, 81 / 85, of 128 24 / 19, 28 / 25, 38 / 33,
+    // 107 / 92.  us, most / 2 / 1, S runs of three tokens, n keys each, heads: S 20, 8 heads of 128, n 260 10.5 / 11.1 / 16; S 20, 32 of 128, n 20 15 / 11 / 7, n 577 41 / 36 / 41;
     // S 60, 32 of 128, n 130 48 / 35 / 29, n 577 103 / 98 / 98; S 20, 32 of 64, n 260 18 / 12 / 13; S 60, 32 of 64, n 20 30 / 10 / 8, n 577 67 / 55 / 56.
     const long all = p.items * (long)c.nkv;
     p.waves = all <= 256 || p.chunk ? (c.d <= 64 ? 8 : 4) : c.d <= 64 ? (all <= 1280 ? 2 : 1) : all <= 512 || few >= 12 * uncut / c.nkv ? 2 : 1;

@@ -172,7 +172,8 @@ __device__ __forceinline__ int lower_bound(const int *x, int n, int v, bool uppe
 // The runs that see something begin and end in their order; the others get the last one's beginning and end (nb, ne).  All those places
 // together, sorted, cut the keys into pieces (cuts, [2 S + 2]) whose keys are seen by the same runs, and these follow one another.  A tile is up to
 // 128 keys of a piece: {key, end of the piece, first step, steps}; a step up to 64 rows of a sequence of runs: {token, head of the group, rows}.
-// One workgroup makes both lists; it stands in front of dQ's, which do not need them.
+// One workgroup makes both lists; it stands in front of dQ's, which do not need them, but dK/dV's launch waits for it: with several hundred runs it is what dQ's launch takes (32 heads
+// of 128, 8 tokens and 64 keys each: 300 runs 164 us, 92 without the lists; 1000 runs 820 and 284).
 constexpr int PLAN_LDS_RUNS = 256;      // as many runs' places are kept in LDS while they are searched (more: in the workspace)
 constexpr int PLAN_INTS(int runs) { return 4 * (runs + 1) + 2 * (2 * runs + 2); }
 constexpr int PLAN_SORTED = 1024;

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void embed_rank_kernel(EmbedArgs a, int *order
         key_of[i] = __builtin_amdgcn_readlane(mine, i);
         count[i] = 0;
     }
-    // eight loads on their way: one at a time the kernel waited for memory (8192 tokens 27.5 us)
+    // eight loads on their way: one at a time the kernel waits for memory (the whole backward pass of 4096 tokens, 1024 wide, added to an fp32 gradient 19.9 us, 18.7 so)
     for (int first = 64 * wave; first < a.T; first += 256 * RANK_LOADS) {
         int other[RANK_LOADS];
 #pragma unroll
